@@ -75,10 +75,12 @@ typedef enum {
     RS_SEQ_TOO_MANY_CHILDREN = 7, /* a node with more than RS_MAX_CANDIDATES children */
     RS_SEQ_GROUP_TIMEOUT = 8,    /* row groups: a workgroup did not receive the others'
                                     slot totals of a pass within 20 ms */
-    RS_SEQ_DEFERRED = 9          /* node outcomes of resispec_decide_nodes only: the node
+    RS_SEQ_DEFERRED = 9,         /* node outcomes of resispec_decide_nodes only: the node
                                     rejected its one candidate, or is a leaf, and its draw
                                     is left to the walk (resispec_walk_draw), which makes it
                                     only where a walk ends */
+    RS_SEQ_BAD_PARAM = 10        /* rows with sampling settings of their own (rs_filter): one
+                                    of them is out of its range */
 } rs_seq_status;
 
 typedef enum { RS_MODE_RESISPEC = 0, RS_MODE_SPECINFER = 1 } rs_mode;
@@ -464,6 +466,92 @@ rs_status resispec_verify_tree_debug(const void* target_logits, const void* draf
                                      void* workspace, size_t workspace_bytes,
                                      int32_t* node_child, int32_t* node_token_out,
                                      int32_t* node_status, float* residual_out, void* stream);
+
+/*
+ * Sampling settings of rows of logits.  Each is one number for all rows, or (its array not
+ * NULL, which wins) a device array with an entry for every `rows_per_entry` consecutive
+ * rows: ceil(R / rows_per_entry) entries; the N node rows of a tree share a request's with
+ * rows_per_entry = N.
+ *
+ * What they keep of a row l of V logits: with m its maximum and w_j = exp((l_j - m) / T),
+ * order the finite elements by logit, equal ones by ascending index.  top_k keeps the first
+ * top_k of that order; top_p, of what top_k keeps, the shortest prefix whose mass reaches
+ * top_p times that of what top_k keeps; min_p those with w_j >= min_p (the maximum has w =
+ * 1).  The first element is always kept.  All sums and comparisons are in 64 bits.
+ */
+typedef struct {
+    int32_t logits_dtype;        /* rs_dtype */
+    int32_t rows_per_entry;      /* >= 1 */
+    float   temperature;         /* finite, > 0 */
+    int32_t top_k;               /* >= 0; 0 = off */
+    float   top_p;               /* in (0, 1]; 1 = off */
+    float   min_p;               /* in [0, 1]; 0 = off */
+    const float*   temperatures; /* device arrays; NULL = the number above for all rows */
+    const int32_t* top_ks;
+    const float*   top_ps;
+    const float*   min_ps;
+} rs_filter;
+
+/*
+ * Draws from rows of logits under sampling settings: the token of a position that has no
+ * draft (k = 1), or the candidates that resispec_verify takes (k > 1, drawn with
+ * replacement).
+ *   logits      : R rows of V elements, `row_stride` (>= V) elements from row to row; what
+ *                 lies between rows is not read
+ *   u           : [R][k] fp32 in [0, 1), one for each draw
+ *   out_token   : [R][k] int32: the smallest index j (vocabulary order) at which the kept
+ *                 masses' running sum exceeds u times their total; the last kept index with
+ *                 mass if rounding leaves none
+ *   out_logprob : [R][k] fp32, may be NULL: the token's log-probability among what is kept
+ *   out_kept    : [R] int32, may be NULL: how many elements are kept
+ *   out_status  : [R] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_PARAM: a setting out of
+ *                 its range; RS_SEQ_BAD_UNIFORM; RS_SEQ_UNDERFLOW: the row has no finite
+ *                 logit, or a NaN or +inf.  Such a row's tokens and count are -1 and its
+ *                 log-probabilities NaN.
+ * RS_ERR_INVALID_ARG for a NULL pointer, R < 0, V <= 0, k <= 0, row_stride < V, or a number
+ * in `filter` out of its range (a device array's entries are checked on the device);
+ * RS_ERR_UNSUPPORTED for V > RS_MAX_VOCAB or k > RS_MAX_CANDIDATES.  R = 0 is a no-op.
+ */
+rs_status resispec_sample(const void* logits, int64_t row_stride, const float* u, int32_t R,
+                          int32_t V, int32_t k, const rs_filter* filter, int32_t* out_token,
+                          float* out_logprob, int32_t* out_kept, int32_t* out_status,
+                          void* stream);
+
+/*
+ * Rows of logits cut to what their sampling settings keep: kept logits unchanged, every
+ * other element -inf.  Target and draft rows cut this way go through
+ * resispec_draft_candidates and every resispec_verify entry point as they are (-inf has
+ * exactly zero mass there), at the same temperature: speculative decoding under top-k, top-p
+ * and min-p.
+ *   out, out_row_stride : R rows of V elements of the same type; may be `logits` itself with
+ *                 the same stride; must not overlap it otherwise.  What lies between rows is
+ *                 not written.
+ *   out_kept, out_status: as resispec_sample (no uniforms here); a row with a status other
+ *                 than RS_SEQ_OK is filled with -inf
+ * Errors as resispec_sample.
+ */
+rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t R, int32_t V,
+                                 const rs_filter* filter, void* out, int64_t out_row_stride,
+                                 int32_t* out_kept, int32_t* out_status, void* stream);
+
+/*
+ * Log-probabilities and ranks of given tokens, such as those a verification returned, under
+ * the temperature softmax of their rows (filtered rows give the filtered distribution's).
+ *   tokens      : [R][k] int32; -1 = no token (the padding of resispec_verify_tree's
+ *                 out_tokens): log-probability 0, rank 0
+ *   filter      : the rows' type and temperature; its top_k, top_p and min_p must be off
+ *   out_logprob : [R][k] fp32: (l_x - m) / T - ln sum_j exp((l_j - m) / T)
+ *   out_rank    : [R][k] int32, may be NULL: 1 + the number of elements before the token in
+ *                 the order of rs_filter
+ *   out_status  : [R] int32, may be NULL: RS_SEQ_BAD_TOKEN for an id outside [-1, V),
+ *                 RS_SEQ_BAD_PARAM or RS_SEQ_UNDERFLOW as resispec_sample; such a row's
+ *                 log-probabilities are NaN and its ranks -1
+ * Errors as resispec_sample.
+ */
+rs_status resispec_token_logprobs(const void* logits, int64_t row_stride, const int32_t* tokens,
+                                  int32_t R, int32_t V, int32_t k, const rs_filter* filter,
+                                  float* out_logprob, int32_t* out_rank, int32_t* out_status,
+                                  void* stream);
 
 /* Static description of a status code. */
 const char* resispec_status_string(int32_t status);

@@ -8,7 +8,7 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", "resispec.hip"), os.path.join(HERE, "csrc", "draft.hip")]
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("resispec.hip", "draft.hip", "sample.hip")]
 LIB = os.path.join(HERE, "libresispec.so")
 # the benchmark's read-bandwidth probe, a library of its own
 PROBE_SRCS = [os.path.join(HERE, "csrc", "probe.hip")]

@@ -15,7 +15,7 @@ LIB_PATH = os.environ.get("RESISPEC_LIBRARY") or os.path.join(HERE, "libresispec
 RS_OK, RS_ERR_INVALID_ARG, RS_ERR_WORKSPACE, RS_ERR_UNSUPPORTED, RS_ERR_HIP = range(5)
 (RS_SEQ_OK, RS_SEQ_BAD_TOKEN, RS_SEQ_ZERO_DRAFT, RS_SEQ_UNDERFLOW, RS_SEQ_BAD_TREE,
  RS_SEQ_BAD_UNIFORM, RS_SEQ_DEPTH_EXCEEDED, RS_SEQ_TOO_MANY_CHILDREN, RS_SEQ_GROUP_TIMEOUT,
- RS_SEQ_DEFERRED) = range(10)
+ RS_SEQ_DEFERRED, RS_SEQ_BAD_PARAM) = range(11)
 RS_MODE_RESISPEC, RS_MODE_SPECINFER = 0, 1
 RS_F32, RS_BF16 = 0, 1
 RS_MAX_CANDIDATES = 64
@@ -35,13 +35,22 @@ EXPORTS = ("resispec_verify", "resispec_verify_tree", "resispec_verify_tree_noal
            "resispec_draft_candidates",
            "resispec_verify_nodes", "resispec_walk", "resispec_node_outcomes",
            "resispec_workspace_bytes", "resispec_validate_tree_host",
-           "resispec_verify_tree_debug", "resispec_status_string", "resispec_abi_version")
+           "resispec_verify_tree_debug", "resispec_sample", "resispec_filter_logits",
+           "resispec_token_logprobs", "resispec_status_string", "resispec_abi_version")
 
 
 class RsParams(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int32), ("logits_dtype", ctypes.c_int32),
                 ("temperature", ctypes.c_float), ("without_replacement", ctypes.c_int32),
                 ("bonus", ctypes.c_int32)]
+
+
+class RsFilter(ctypes.Structure):
+    _fields_ = [("logits_dtype", ctypes.c_int32), ("rows_per_entry", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
+                ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p)]
 
 
 class ResiSpecError(RuntimeError):
@@ -111,6 +120,13 @@ def _load():
     lib.resispec_workspace_bytes.restype = sz
     lib.resispec_validate_tree_host.argtypes = [P, P, i32, i32, i32, ctypes.POINTER(i64)]
     lib.resispec_validate_tree_host.restype = i32
+    flt = ctypes.POINTER(RsFilter)
+    lib.resispec_sample.argtypes = [P, i64, P, i32, i32, i32, flt, P, P, P, P, P]
+    lib.resispec_sample.restype = i32
+    lib.resispec_filter_logits.argtypes = [P, i64, i32, i32, flt, P, i64, P, P, P]
+    lib.resispec_filter_logits.restype = i32
+    lib.resispec_token_logprobs.argtypes = [P, i64, P, i32, i32, i32, flt, P, P, P, P]
+    lib.resispec_token_logprobs.restype = i32
     lib.resispec_status_string.argtypes = [i32]
     lib.resispec_status_string.restype = ctypes.c_char_p
     lib.resispec_abi_version.argtypes = []
@@ -692,3 +708,173 @@ def resispec_verify_tree_debug(target_logits, draft_logits, node_token, parent, 
     return {"tokens": out_tokens, "accepted_len": out_len, "status": out_status,
             "node_child": node_child, "node_token": node_tok, "node_status": node_status,
             "residual": resid}
+
+
+# ----------------------------------------------------------------- sampling --
+
+def _rows(t, name):
+    """Rows of a [R, V] or [B, N, V] tensor whose rows lie one stride apart: (pointer,
+    stride, leading shape, R, V)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dtype != torch.float32 and t.dtype != torch.bfloat16:
+        raise TypeError("%s must be float32 or bfloat16" % name)
+    shape, stride = t.shape, t.stride()
+    if not 2 <= len(shape) <= 3:
+        raise ValueError("%s must be [R, V] or [B, N, V]" % name)
+    V = shape[-1]
+    if V > 1 and stride[-1] != 1:
+        raise ValueError("%s: the elements of a row must be adjacent" % name)
+    if len(shape) == 2:
+        R, step = shape[0], stride[0]
+    else:
+        R, step = shape[0] * shape[1], stride[1] if shape[1] > 1 else stride[0]
+        if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
+            raise ValueError("%s: all rows must lie one stride apart" % name)
+    if R < 2:
+        step = V
+    elif step < V:
+        raise ValueError("%s: rows must not overlap" % name)
+    return t.data_ptr(), step, shape[:-1], R, V
+
+
+def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
+    """rs_filter of settings that are numbers, or device tensors with an entry a row ([R] or
+    [B, N]) or a sequence ([B])."""
+    import torch
+    f = RsFilter(RS_BF16 if logits.dtype == torch.bfloat16 else RS_F32, 1, 1.0, 0, 1.0, 0.0)
+    shape = None
+    for v, number, array, dtype in ((temperature, "temperature", "temperatures", torch.float32),
+                                    (top_k, "top_k", "top_ks", torch.int32),
+                                    (top_p, "top_p", "top_ps", torch.float32),
+                                    (min_p, "min_p", "min_ps", torch.float32)):
+        if not isinstance(v, torch.Tensor):
+            setattr(f, number, v)
+            continue
+        if shape is None:
+            shape = v.shape
+            if shape != lead and shape != lead[:1]:
+                raise ValueError("%s has shape %s, expected %s or %s" % (number, tuple(shape), tuple(lead),
+                                                                        tuple(lead[:1])))
+            f.rows_per_entry = max(1, R // max(1, v.numel()))
+        elif v.shape != shape:
+            raise ValueError("settings given as tensors must have one shape")
+        if v.device != logits.device:
+            raise ValueError("all tensors must be on one device, got %s" % {v.device, logits.device})
+        setattr(f, array, _dev(v, dtype, number))
+    return f
+
+
+class _On:
+    """The device of the rows made current, and `stream` (or its current stream) the one that
+    temporary and returned tensors belong to."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.guards = []
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, device))
+            self.guards.append(torch.cuda.stream(stream))
+        elif torch.cuda.current_device() != device.index:
+            self.guards.append(torch.cuda.device(device))
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _out(t, shape, dtype, device, name):
+    """An output of the caller's, checked, or a new one."""
+    import torch
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _shape(t, shape, name)
+    _dev(t, dtype, name)
+    if t.device != device:
+        raise ValueError("all tensors must be on one device, got %s" % {t.device, device})
+    return t
+
+
+def resispec_sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out_token=None,
+                    out_logprob=None, out_kept=None, out_status=None, stream=None):
+    """Draws from rows of logits under temperature, top-k, top-p and min-p, one for each of the
+    k uniforms of a row.
+
+    logits: [R, V] or [B, N, V], the rows one stride apart (padding between them is not
+    read); u: fp32, the leading shape and k.  Each setting is a number, or a device tensor
+    with an entry a row or a sequence (fp32; top_k int32).  top_k 0, top_p 1 and min_p 0 are
+    off; top_k 1 is the likeliest token.  Returns (token and log-probability, shaped as u;
+    number of elements kept and status, the leading shape)."""
+    import torch
+    ptr, step, lead, R, V = _rows(logits, "logits")
+    if u.dim() != len(lead) + 1 or u.shape[:-1] != lead:
+        raise ValueError("u has shape %s, expected %s and the number of draws" % (tuple(u.shape), tuple(lead)))
+    dev, k = logits.device, u.shape[-1]
+    f = _settings(logits, lead, R, temperature, top_k, top_p, min_p)
+    _same_device(logits, u)
+    with _On(dev, stream):
+        out_token = _out(out_token, u.shape, torch.int32, dev, "out_token")
+        out_logprob = _out(out_logprob, u.shape, torch.float32, dev, "out_logprob")
+        out_kept = _out(out_kept, lead, torch.int32, dev, "out_kept")
+        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
+        _check(lib.resispec_sample(ptr, step, _dev(u, torch.float32, "u"), R, V, k, ctypes.byref(f),
+                                   out_token.data_ptr(), out_logprob.data_ptr(), out_kept.data_ptr(),
+                                   out_status.data_ptr(), _stream(stream)))
+    return out_token, out_logprob, out_kept, out_status
+
+
+def resispec_filter_logits(logits, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None,
+                           out_kept=None, out_status=None, stream=None):
+    """Rows of logits with -inf outside what their settings (as resispec_sample) keep: target
+    and draft rows for the draft step and the verification.  `out` may be `logits` itself.
+    Returns (out, number of elements kept, status)."""
+    import torch
+    ptr, step, lead, R, V = _rows(logits, "logits")
+    dev = logits.device
+    f = _settings(logits, lead, R, temperature, top_k, top_p, min_p)
+    with _On(dev, stream):
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        to, to_step, _, _, _ = _rows(out, "out")
+        _shape(out, logits.shape, "out")
+        _same_device(logits, out)
+        if out.dtype != logits.dtype:
+            raise TypeError("out must be %s" % logits.dtype)
+        if R and not (to == ptr and to_step == step):
+            size = logits.element_size()
+            if to < ptr + ((R - 1) * step + V) * size and ptr < to + ((R - 1) * to_step + V) * size:
+                raise ValueError("out must not overlap logits, unless it is the same rows")
+        out_kept = _out(out_kept, lead, torch.int32, dev, "out_kept")
+        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
+        _check(lib.resispec_filter_logits(ptr, step, R, V, ctypes.byref(f), to, to_step, out_kept.data_ptr(),
+                                          out_status.data_ptr(), _stream(stream)))
+    return out, out_kept, out_status
+
+
+def resispec_token_logprobs(logits, tokens, *, temperature=1.0, out_logprob=None, out_rank=None,
+                            out_status=None, stream=None):
+    """Log-probabilities, under the temperature softmax of their rows, and ranks of given
+    tokens (int32, the leading shape of `logits` and k; -1 = no token, which gives 0 and 0).
+    Returns (log-probability, rank, status)."""
+    import torch
+    ptr, step, lead, R, V = _rows(logits, "logits")
+    if tokens.dim() != len(lead) + 1 or tokens.shape[:-1] != lead:
+        raise ValueError("tokens has shape %s, expected %s and the number of tokens" %
+                         (tuple(tokens.shape), tuple(lead)))
+    dev, k = logits.device, tokens.shape[-1]
+    f = _settings(logits, lead, R, temperature, 0, 1.0, 0.0)
+    _same_device(logits, tokens)
+    with _On(dev, stream):
+        out_logprob = _out(out_logprob, tokens.shape, torch.float32, dev, "out_logprob")
+        out_rank = _out(out_rank, tokens.shape, torch.int32, dev, "out_rank")
+        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
+        _check(lib.resispec_token_logprobs(ptr, step, _dev(tokens, torch.int32, "tokens"), R, V, k,
+                                           ctypes.byref(f), out_logprob.data_ptr(), out_rank.data_ptr(),
+                                           out_status.data_ptr(), _stream(stream)))
+    return out_logprob, out_rank, out_status

@@ -1,0 +1,420 @@
+"""Draws from filtered rows, filtered rows and log-probabilities of tokens on the GPU against
+the plain 64-bit definition (sampling_util).
+
+Tokens, kept sets and ranks are compared exactly: kernel and definition both sum in 64 bits,
+so they part only where a draw or a cut lies within about 1e-13 of a border, which no row
+here does by chance (rows of equal values have exact sums on both sides).
+
+Tolerances.  A log-probability of a draw is a 64-bit value rounded once to 32 bits: half a
+step, 2^-24 of it, and 1e-12 for the exponentials (3.7e-14 each) and the sums.  One of a
+given token comes from a sum of 32-bit exponentials: the exponent's rounding is at most 2^-24
+of up to 64 (what is smaller than 2^-64 does not count), 64 * 2^-24 * ln 2 = 2.7e-6 of a
+term; the exponential's own 2^-23; a 32-bit sum of up to 32 terms 32 * 2^-24 = 1.9e-6.
+Together 4.8e-6 of the sum, as much in its logarithm."""
+import numpy as np
+import pytest
+import torch
+
+from sampling_util import border, draw, kept, logprob, make_rows, to64
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+SETTINGS = [dict(), dict(temperature=0.7, top_k=50, top_p=0.95), dict(top_k=1), dict(top_k=7),
+            dict(temperature=1.3, top_p=0.9), dict(temperature=0.05, top_p=0.999), dict(temperature=0.6, min_p=0.05),
+            dict(top_k=300, top_p=0.5, min_p=0.001), dict(temperature=50.0, top_p=0.3), dict(top_p=1e-6),
+            dict(min_p=1.0), dict(top_p=1.0 - 2.0 ** -24), dict(top_k=1000000)]
+
+
+def uniforms(R, k, seed=0):
+    g = np.random.default_rng([seed, R, k])
+    u = (g.integers(0, 1 << 24, (R, k)) * 2.0 ** -24).astype(np.float32)
+    if k > 1:
+        u[:, 0], u[:, 1] = 0.0, 1.0 - 2.0 ** -24
+    return torch.as_tensor(u, device="cuda")
+
+
+def check_sample(native, rows, u, each=None, **kw):
+    """One call on rows [R, V] against the definition; `each`: the settings of every row."""
+    tok, lp, n, st = native.resispec_sample(rows, u, **kw)
+    torch.cuda.synchronize()
+    l, uu = to64(rows), u.cpu().numpy()
+    for r in range(rows.shape[0]):
+        s = each[r] if each else {k: v for k, v in kw.items() if not isinstance(v, torch.Tensor)}
+        check_row(native, l[r], uu[r], s, tok[r].tolist(), lp[r].tolist(), int(n[r]), int(st[r]))
+
+
+def check_row(native, l, u, s, tok, lp, n, st):
+    s = {"T" if k == "temperature" else k: v for k, v in s.items()}
+    mask = kept(l, **s)
+    if mask is None:
+        assert st == native.RS_SEQ_UNDERFLOW and n == -1
+        assert all(t == -1 for t in tok) and all(np.isnan(lp))
+        return
+    assert st == native.RS_SEQ_OK
+    assert n == mask.sum()
+    for i, x in enumerate(u):
+        j, p = draw(l, s.get("T", 1.0), mask, x)
+        assert tok[i] == j, (tok[i], j, x, border(l, s.get("T", 1.0), mask, x))
+        assert abs(lp[i] - p) <= abs(p) * 2.0 ** -24 + 1e-12, (lp[i], p)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["zipf", "flat", "peaked", "equal", "few", "masked", "lowest", "all-lowest", "large"])
+def test_sample_kinds_of_rows(gpu_lib, kind, dtype):
+    """Every kind of row under every setting, a vocabulary of several slots."""
+    rows = make_rows(3, 5003, dtype, 1, kind)
+    for i, s in enumerate(SETTINGS):
+        check_sample(gpu_lib, rows, uniforms(3, 5, i), **s)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 3, 4, 7, 8, 9, 63, 64, 65, 511, 512, 1023, 1025, 2047, 2048, 2049, 16384, 32001])
+def test_sample_sizes(gpu_lib, V, dtype):
+    for pad, offset in ((0, 0), (5, 0), (16 - V % 8, 8), (1, 3)):
+        rows = make_rows(2, V, dtype, V, pad=pad, offset=offset)
+        for s in (dict(temperature=0.8), dict(top_k=max(1, V // 3)), dict(top_p=0.7), dict(min_p=0.1, top_p=0.99)):
+            check_sample(gpu_lib, rows, uniforms(2, 3, V), **s)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_sample_many_draws(gpu_lib, dtype):
+    rows = make_rows(2, 40003, dtype, 9)
+    for s in (dict(), dict(top_p=0.97), dict(top_k=17)):
+        check_sample(gpu_lib, rows, uniforms(2, 64), **s)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("top_k", [0, 5, 2000, 20000])
+def test_long_rows(gpu_lib, dtype, top_k):
+    """The longest vocabularies of real checkpoints, and far past them."""
+    for V in (151936, 262145, 1 << 20):
+        rows = make_rows(2, V, dtype, V)
+        check_sample(gpu_lib, rows, uniforms(2, 4), temperature=0.9, top_k=top_k, top_p=0.95)
+    rows = make_rows(1, 300001, dtype, 4, "few")     # ties by the ten thousand
+    check_sample(gpu_lib, rows, uniforms(1, 4), top_k=top_k, top_p=0.6)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_largest_vocabulary(gpu_lib, dtype):
+    V = 1 << 22
+    rows = make_rows(1, V, dtype, 3)
+    check_sample(gpu_lib, rows, uniforms(1, 2), top_p=0.9)
+    check_sample(gpu_lib, rows, uniforms(1, 2), top_k=100)
+    out, n, st = gpu_lib.resispec_filter_logits(rows, top_k=100)
+    torch.cuda.synchronize()
+    assert int(torch.isfinite(out).sum()) == 100 == int(n[0])
+
+
+def row_settings(R, device="cuda"):
+    each = [SETTINGS[r % len(SETTINGS)] for r in range(R)]
+    full = [dict(dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0), **s) for s in each]
+    t = dict(temperature=torch.tensor([s["temperature"] for s in full], dtype=F32, device=device),
+             top_k=torch.tensor([s["top_k"] for s in full], dtype=torch.int32, device=device),
+             top_p=torch.tensor([s["top_p"] for s in full], dtype=F32, device=device),
+             min_p=torch.tensor([s["min_p"] for s in full], dtype=F32, device=device))
+    return each, t
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("R", [13, 300])
+def test_settings_of_each_row(gpu_lib, R, dtype):
+    """Every row has settings of its own; all four arrays, and one of them beside numbers."""
+    rows = make_rows(R, 3001, dtype, R)
+    each, t = row_settings(R)
+    check_sample(gpu_lib, rows, uniforms(R, 2), each, **t)
+    for name in t:
+        one = [dict(temperature=0.8, top_k=40, top_p=0.9, min_p=0.01) for _ in range(R)]
+        kw = dict(one[0])
+        for r in range(R):
+            one[r][name] = t[name][r].item()
+        kw[name] = t[name]
+        check_sample(gpu_lib, rows, uniforms(R, 2), one, **kw)
+
+
+def test_settings_of_each_sequence(gpu_lib):
+    """[B, N, V] rows: an entry a sequence covers its N rows; an entry a row is taken too."""
+    B, N, V = 5, 7, 2111
+    rows = make_rows(B * N, V, BF16, 2).view(B, N, V)
+    each, t = row_settings(B)
+    u = uniforms(B * N, 3).view(B, N, 3)
+    got = gpu_lib.resispec_sample(rows, u, **t)
+    spread = {k: v.repeat_interleave(N).view(B, N) for k, v in t.items()}
+    again = gpu_lib.resispec_sample(rows, u, **spread)
+    torch.cuda.synchronize()
+    for x, y in zip(got, again):
+        assert torch.equal(x, y)
+    assert got[0].shape == (B, N, 3) and got[2].shape == (B, N)
+    l, uu = to64(rows), u.cpu().numpy()
+    for b in range(B):
+        for n in range(N):
+            check_row(gpu_lib, l[b, n], uu[b, n], each[b], got[0][b, n].tolist(), got[1][b, n].tolist(),
+                      int(got[2][b, n]), int(got[3][b, n]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_rows_without_a_distribution(gpu_lib, dtype):
+    """NaN, +inf and rows of -inf are reported, and do not touch their neighbours."""
+    rows = make_rows(9, 4099, dtype, 6)
+    rows[1, 4098] = float("nan")
+    rows[2, 0] = float("inf")
+    rows[4] = float("-inf")
+    rows[5] = float("nan")
+    rows[7] = float("-inf")
+    rows[7, 77] = -3.0                     # one finite element: always drawn
+    for s in SETTINGS:
+        check_sample(gpu_lib, rows, uniforms(9, 3), **s)
+    tok, lp, n, st = gpu_lib.resispec_sample(rows, uniforms(9, 3), top_p=0.5)
+    torch.cuda.synchronize()
+    assert tok[7].tolist() == [77] * 3 and lp[7].tolist() == [0.0] * 3 and int(n[7]) == 1
+    out, n, st = gpu_lib.resispec_filter_logits(rows, top_p=0.5)
+    lpt, rank, st2 = gpu_lib.resispec_token_logprobs(rows, torch.zeros((9, 2), dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for r in (1, 2, 4, 5):
+        assert (out[r] == float("-inf")).all() and int(n[r]) == -1
+        assert int(st[r]) == int(st2[r]) == gpu_lib.RS_SEQ_UNDERFLOW
+        assert torch.isnan(lpt[r]).all() and (rank[r] == -1).all()
+    assert (st[[0, 3, 6, 7, 8]] == 0).all() and (st2[[0, 3, 6, 7, 8]] == 0).all()
+
+
+def test_bad_uniforms_and_settings(gpu_lib):
+    rows = make_rows(6, 1000, F32, 8)
+    u = uniforms(6, 3)
+    u[1, 2], u[2, 0], u[3, 1] = 1.0, -0.25, float("nan")
+    tok, lp, n, st = gpu_lib.resispec_sample(rows, u)
+    torch.cuda.synchronize()
+    bad = gpu_lib.RS_SEQ_BAD_UNIFORM
+    assert st.tolist() == [0, bad, bad, bad, 0, 0]
+    assert (tok[1:4] == -1).all() and torch.isnan(lp[1:4]).all() and (n[1:4] == -1).all()
+    assert (tok[[0, 4, 5]] >= 0).all()
+    f = dict(device="cuda", dtype=F32)
+    for kw in (dict(temperature=torch.tensor([1, 0, -1, float("inf"), float("nan"), 1.0], **f)),
+               dict(top_k=torch.tensor([0, -1, -5, -2 ** 31, -3, 4], device="cuda", dtype=torch.int32)),
+               dict(top_p=torch.tensor([1, 0, -1, 1.01, float("nan"), 0.5], **f)),
+               dict(min_p=torch.tensor([0, -0.1, 1.01, -float("inf"), float("nan"), 0.5], **f))):
+        bad = gpu_lib.RS_SEQ_BAD_PARAM
+        tok, lp, n, st = gpu_lib.resispec_sample(rows, uniforms(6, 3), **kw)
+        out, n2, st2 = gpu_lib.resispec_filter_logits(rows, **kw)
+        torch.cuda.synchronize()
+        assert st.tolist() == st2.tolist() == [0, bad, bad, bad, bad, 0]
+        assert (tok[1:5] == -1).all() and (n[1:5] == -1).all() and (n2[1:5] == -1).all()
+        assert (out[1:5] == float("-inf")).all() and (out[0] == rows[0]).any()
+        if "temperature" in kw:
+            lp, rank, st3 = gpu_lib.resispec_token_logprobs(rows, tok, **kw)
+            torch.cuda.synchronize()
+            assert st3.tolist() == st.tolist() and torch.isnan(lp[1:5]).all() and (rank[1:5] == -1).all()
+
+
+def same_bits(a, b):
+    t = torch.int16 if a.dtype == BF16 else torch.int32
+    return torch.equal(a.contiguous().view(t), b.contiguous().view(t))
+
+
+def expected_filter(rows, each):
+    l, out, n = to64(rows), rows.clone(), []
+    for r in range(rows.shape[0]):
+        s = {"T" if k == "temperature" else k: v for k, v in each[r].items()}
+        mask = kept(l[r], **s)
+        out[r][torch.as_tensor(~mask, device=rows.device)] = float("-inf")
+        n.append(int(mask.sum()))
+    return out, n
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["zipf", "equal", "few", "masked", "lowest", "all-lowest"])
+def test_filter_kinds_of_rows(gpu_lib, kind, dtype):
+    rows = make_rows(13, 5003, dtype, 11, kind)
+    each, t = row_settings(13)
+    want, count = expected_filter(rows, each)
+    out, n, st = gpu_lib.resispec_filter_logits(rows, **t)
+    torch.cuda.synchronize()
+    assert same_bits(out, want) and n.tolist() == count and (st == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 8, 9, 64, 513, 2048, 2051, 4096, 32001])
+def test_filter_sizes_strides_and_places(gpu_lib, V, dtype):
+    """Padded and shifted inputs and outputs, and in place: what lies between rows stays."""
+    each, t = row_settings(13)
+    for pad, offset, opad, ooffset in ((0, 0, 0, 0), (3, 1, 5, 2), (8, 8, 0, 1), (0, 0, 16 - V % 8, 8)):
+        rows = make_rows(13, V, dtype, V, pad=pad, offset=offset)
+        want, count = expected_filter(rows, each)
+        store = torch.full((ooffset + 13 * (V + opad) + 9,), 7.0, dtype=dtype, device="cuda")
+        out = store[ooffset:ooffset + 13 * (V + opad)].view(13, V + opad)[:, :V]
+        got, n, st = gpu_lib.resispec_filter_logits(rows, out=out, **t)
+        torch.cuda.synchronize()
+        assert got is out and same_bits(out, want) and n.tolist() == count
+        out.fill_(7.0)
+        assert (store == 7.0).all()                       # nothing outside the rows was written
+        whole = rows.as_strided((13 * (V + pad),), (1,)) if pad else None
+        got, n, st = gpu_lib.resispec_filter_logits(rows, out=rows, **t)
+        torch.cuda.synchronize()
+        assert same_bits(rows, want) and n.tolist() == count
+        if pad:
+            assert torch.isnan(whole.view(13, V + pad)[:, V:]).all()
+
+
+def test_filter_signed_zeros(gpu_lib):
+    """-0 and +0 are equal in the order, and are written as they were."""
+    for dtype in (F32, BF16):
+        rows = torch.full((1, 600), -5.0, dtype=dtype, device="cuda")
+        rows[0, 100:110] = 0.0
+        rows[0, 105:300] = -0.0
+        out, n, _ = gpu_lib.resispec_filter_logits(rows, top_k=8)
+        torch.cuda.synchronize()
+        want = torch.full_like(rows, float("-inf"))
+        want[0, 100:108] = rows[0, 100:108]
+        assert same_bits(out, want) and int(n[0]) == 8
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 2049, 32001, 151936])
+def test_token_logprobs(gpu_lib, V, dtype):
+    g = np.random.default_rng(V)
+    for kind, pad, k, T in (("zipf", 0, 1, 1.0), ("few", 5, 6, 0.7), ("lowest", 3, 64, 1.3), ("large", 0, 3, 2.0),
+                            ("masked", 1, 5, 0.3), ("peaked", 0, 20, 0.6)):
+        rows = make_rows(4, V, dtype, V, kind, pad)
+        tokens = g.integers(-1, V, (4, k)).astype(np.int32)
+        tokens[0, 0], tokens[1, 0], tokens[2, 0] = V - 1, 0, -1
+        lp, rank, st = gpu_lib.resispec_token_logprobs(rows, torch.as_tensor(tokens, device="cuda"), temperature=T)
+        torch.cuda.synchronize()
+        assert (st == 0).all()
+        l = to64(rows)
+        for r in range(4):
+            for i in range(k):
+                got = (float(lp[r, i]), int(rank[r, i]))
+                if tokens[r, i] < 0:
+                    assert got == (0.0, 0)
+                    continue
+                p, n = logprob(l[r], T, tokens[r, i])
+                assert got[1] == n
+                if p == -np.inf or p < -3.4e38:
+                    assert got[0] == -np.inf
+                else:
+                    assert abs(got[0] - p) <= abs(p) * 2.0 ** -24 + 4.8e-6, (got[0], p, kind)
+
+
+def test_token_logprobs_bad_tokens(gpu_lib):
+    rows = make_rows(4, 100, F32, 1)
+    tokens = torch.tensor([[0, 99], [5, 100], [-2, 3], [-1, -1]], dtype=torch.int32, device="cuda")
+    lp, rank, st = gpu_lib.resispec_token_logprobs(rows, tokens)
+    torch.cuda.synchronize()
+    bad = gpu_lib.RS_SEQ_BAD_TOKEN
+    assert st.tolist() == [0, bad, bad, 0]
+    assert torch.isnan(lp[1:3]).all() and (rank[1:3] == -1).all() and (rank[3] == 0).all() and (lp[3] == 0).all()
+
+
+def test_offsets_past_32_bits(gpu_lib):
+    """Rows whose elements lie past 2^32 bytes and 2^31 elements of the first."""
+    V, step = 1001, (1 << 26) + 8
+    R = 40
+    flat = torch.zeros((R - 1) * step + V + 8, dtype=BF16, device="cuda")
+    rows = flat.as_strided((R, V), (step, 1))
+    rows.copy_(make_rows(R, V, BF16, 21))
+    each, t = row_settings(R)
+    check_sample(gpu_lib, rows, uniforms(R, 2), each, **t)
+    want, count = expected_filter(rows.contiguous(), each)
+    tokens = torch.randint(0, V, (R, 2), dtype=torch.int32, device="cuda")
+    a = gpu_lib.resispec_token_logprobs(rows, tokens)
+    b = gpu_lib.resispec_token_logprobs(rows.contiguous(), tokens)
+    gpu_lib.resispec_filter_logits(rows, out=rows, **t)
+    torch.cuda.synchronize()
+    assert same_bits(rows.contiguous(), want)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_same_results_on_every_call_stream_and_batch(gpu_lib):
+    """A row's outputs do not depend on the call it is in: alone, among others, on another
+    stream, with two calls under way at once."""
+    R, V = 300, 40961
+    rows = make_rows(R, V, BF16, 31)
+    each, t = row_settings(R)
+    u = uniforms(R, 4)
+    tokens = torch.randint(-1, V, (R, 4), dtype=torch.int32, device="cuda")
+    first = (*gpu_lib.resispec_sample(rows, u, **t), *gpu_lib.resispec_filter_logits(rows, **t),
+             *gpu_lib.resispec_token_logprobs(rows, tokens, temperature=t["temperature"]))
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        a = (*gpu_lib.resispec_sample(rows, u, **t, stream=s1), *gpu_lib.resispec_filter_logits(rows, **t, stream=s2),
+             *gpu_lib.resispec_token_logprobs(rows, tokens, temperature=t["temperature"], stream=s1))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a, first))
+    for lo, hi in ((0, 1), (5, 6), (17, 40), (12, 13), (0, 150)):
+        part = {k: v[lo:hi] for k, v in t.items()}
+        a = (*gpu_lib.resispec_sample(rows[lo:hi], u[lo:hi], **part),
+             *gpu_lib.resispec_filter_logits(rows[lo:hi], **part),
+             *gpu_lib.resispec_token_logprobs(rows[lo:hi], tokens[lo:hi], temperature=part["temperature"]))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y[lo:hi]) for x, y in zip(a, first))
+
+
+@pytest.mark.parametrize("R", [2, 300])
+def test_captured_and_replayed(gpu_lib, R):
+    """All three operators in one graph, replayed with new inputs and the program's own work in
+    between; each replay equals the eager calls."""
+    V = 20011
+    rows = make_rows(R, V, F32, 41)
+    each, t = row_settings(R)
+    u = uniforms(R, 2)
+
+    def calls(x, v):
+        y, n, st = gpu_lib.resispec_filter_logits(x, **t)
+        s = gpu_lib.resispec_sample(x, v, **t)
+        return (y, n, st, *s, *gpu_lib.resispec_token_logprobs(y, s[0], temperature=t["temperature"]))
+
+    calls(rows, u)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls(rows, u)
+    for seed in (42, 43, 44, 45):
+        rows.copy_(make_rows(R, V, F32, seed))
+        u.copy_(uniforms(R, 2, seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = calls(rows, u)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, want))
+        torch.randn(1 << 20, device="cuda").sum().item()
+
+
+def test_empty_batches(gpu_lib):
+    x = torch.empty((0, 100), device="cuda")
+    tok, lp, n, st = gpu_lib.resispec_sample(x, torch.empty((0, 2), device="cuda"))
+    assert tok.shape == (0, 2) and st.shape == (0,)
+    out, n, st = gpu_lib.resispec_filter_logits(x)
+    assert out.shape == (0, 100)
+    lp, rank, st = gpu_lib.resispec_token_logprobs(x, torch.empty((0, 3), dtype=torch.int32, device="cuda"))
+    assert lp.shape == (0, 3)
+
+
+def test_binding_refusals(gpu_lib):
+    x = make_rows(4, 64, F32, 1)
+    u = uniforms(4, 1)
+    tok = torch.zeros((4, 1), dtype=torch.int32, device="cuda")
+    bad = [lambda: gpu_lib.resispec_sample(x.double(), u), lambda: gpu_lib.resispec_sample(x.half(), u),
+           lambda: gpu_lib.resispec_sample(x[0], u[0]), lambda: gpu_lib.resispec_sample(x, u[:3]),
+           lambda: gpu_lib.resispec_sample(x, u[:, 0]), lambda: gpu_lib.resispec_sample(x.t(), u),
+           lambda: gpu_lib.resispec_sample(x, u.double()), lambda: gpu_lib.resispec_sample(x, u.cpu()),
+           lambda: gpu_lib.resispec_sample(x, u.expand(4, 65)),
+           lambda: gpu_lib.resispec_sample(x, u[:, :0]), lambda: gpu_lib.resispec_sample(x[:1].expand(4, 64), u),
+           lambda: gpu_lib.resispec_sample(x, u, temperature=0.0), lambda: gpu_lib.resispec_sample(x, u, top_p=1.5),
+           lambda: gpu_lib.resispec_sample(x, u, top_k=-1), lambda: gpu_lib.resispec_sample(x, u, min_p=-1.0),
+           lambda: gpu_lib.resispec_sample(x, u, top_k=torch.ones(4, device="cuda")),
+           lambda: gpu_lib.resispec_sample(x, u, top_p=torch.ones(3, device="cuda")),
+           lambda: gpu_lib.resispec_sample(x, u, top_p=torch.ones(4)),
+           lambda: gpu_lib.resispec_sample(x, u, out_token=tok[:3]),
+           lambda: gpu_lib.resispec_sample(x, u, out_token=tok.float()),
+           lambda: gpu_lib.resispec_filter_logits(x, out=x[:3]),
+           lambda: gpu_lib.resispec_filter_logits(x, out=x.bfloat16()),
+           lambda: gpu_lib.resispec_filter_logits(x[:3], out=x[1:]),
+           lambda: gpu_lib.resispec_filter_logits(x, out=x.cpu()),
+           lambda: gpu_lib.resispec_token_logprobs(x, tok.long()),
+           lambda: gpu_lib.resispec_token_logprobs(x, tok[:2]),
+           lambda: gpu_lib.resispec_token_logprobs(x, tok, temperature=-1.0),
+           lambda: gpu_lib.resispec_token_logprobs(x.view(2, 2, 64), tok)]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, TypeError, gpu_lib.ResiSpecError)):
+            call()
+            print("refusal", i, "was not made")
