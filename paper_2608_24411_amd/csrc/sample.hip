@@ -18,8 +18,14 @@ namespace {
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
-constexpr float kBinsPerUnit = 64;  // of the first search: bins in a unit of logits below the maximum
 constexpr int kUnrRow = 4;          // 16-byte loads a lane and chunk
+
+// Bins of bf16 values, from the highest to the lowest: one for every value with 2^-38 < |l| <
+// 1020, one for those between (where both zeros are), one at each end for those outside
+// (-inf in the last).  Unused: bin 0.
+constexpr int kHalf = 6144, kValueBins = 2 * kHalf;
+constexpr uint16_t kLoMag = (127 - 38) << 7, kTopMag = kHalf - 1;
+constexpr int kTopBin = 1, kZeroBin = kHalf, kLastBin = kValueBins - 1;
 
 struct SParams {
     const void* logits;
@@ -40,9 +46,16 @@ struct SParams {
 };
 
 struct RowSmem {
-    float hist[kBins];
+    union {
+        float hist[kBins];            // search within a range of keys
+        uint32_t count[kValueBins];   // how often each bf16 value occurs
+        double table[kValueBins / 2]; // their masses, from the highest value of the row
+        int32_t list[kValueBins];     // indices of equal elements
+    };
     double slot[kRowSlots];
     int32_t ties[kRowSlots];
+    double cut_above, cut_mass;       // what lies above the crossing bin, and the prefix's mass
+    int32_t cut_bin, cut_keep, cut_all, nlist;
     double red[2][kMaxWaves];
     int32_t redi[2][kMaxWaves];
     uint32_t redk[2][kMaxWaves];
@@ -84,11 +97,37 @@ struct Cut {
     __device__ __forceinline__ bool keeps(float l, int j) const { return l > tau || (l == tau && j <= limit); }
 };
 
+// The same before the ties' last index is looked for: the first `keep` of the `all` elements
+// equal to tau are kept.
+struct Ties {
+    float tau;
+    int32_t keep, all;
+};
+
+// Byte offsets into the counts of the bins of the two bf16 values in a word.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 bin_bytes(uint32_t word) {
+    const u16x2 lo = {kLoMag, kLoMag}, top = {kTopMag, kTopMag};
+    const u16x2 one = {(uint16_t)(kHalf + 1), (uint16_t)(kHalf + 1)};
+    const u16x2 mag = __builtin_bit_cast(u16x2, word & 0x7fff7fffu);
+    const u16x2 t = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, lo), top);
+    const u16x2 neg = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, word) >> 15);
+    // kHalf - t for positive values, kHalf + t for negative ones
+    return (~(t ^ neg) + neg + one) << 2;
+}
+__device__ __forceinline__ float bin_value(int bin) {
+    const int t = bin < kHalf ? kHalf - bin : bin - kHalf;
+    if (t == 0) return 0.0f;
+    return __uint_as_float((uint32_t)(t + kLoMag) << 16 | (bin > kHalf ? 0x80000000u : 0u));
+}
+
 template <typename In, int VEC, int UNR, int BLOCK>
 struct Row {
     using W = Vec<In, VEC>;
     static constexpr int CHUNK = 64 * VEC * UNR;
     static constexpr int kWaves = BLOCK / 64;
+    static constexpr int PER = kValueBins / BLOCK;   // bins a thread
     const In* row;
     int V, G, nslots;
     float m;       // the row's maximum
@@ -97,10 +136,10 @@ struct Row {
 
     __device__ __forceinline__ double mass(float l) const { return exp2_64(((double)l - md) * c); }
 
-    // body(v, j): a vector of VEC elements from index j (-inf at and past V); flush(slot)
-    // after a slot's last.  A wave's slots are the same in every pass.
+    // body(t, j): a vector of VEC elements from index j as loaded (-inf at and past V);
+    // flush(slot) after a slot's last.  A wave's slots are the same in every pass.
     template <typename Body, typename Flush>
-    __device__ __forceinline__ void sweep(Body&& body, Flush&& flush) const {
+    __device__ __forceinline__ void sweep_raw(Body&& body, Flush&& flush) const {
         const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
         typename W::raw a[UNR], b[UNR];
         auto load = [&](int s, int g, typename W::raw(&t)[UNR]) {
@@ -110,10 +149,8 @@ struct Row {
             const int j0 = (s * G + g) * CHUNK + lane * VEC;
 #pragma unroll
             for (int u = 0; u < UNR; ++u) {
-                float v[VEC];
                 W::settle(t[u], row, j0 + u * 64 * VEC, V);
-                W::unpack(t[u], v);
-                body(v, j0 + u * 64 * VEC);
+                body(t[u], j0 + u * 64 * VEC);
             }
             if (g == G - 1) flush(s);
         };
@@ -132,6 +169,16 @@ struct Row {
             process(s2, g2, b);
             if (s >= nslots) break;
         }
+    }
+
+    // The same with the elements as floats.
+    template <typename Body, typename Flush>
+    __device__ __forceinline__ void sweep(Body&& body, Flush&& flush) const {
+        sweep_raw([&](const typename W::raw& t, int j) {
+            float v[VEC];
+            W::unpack(t, v);
+            body(v, j);
+        }, flush);
     }
 
     // Sums over the workgroup in a fixed order, to every thread.
@@ -233,22 +280,17 @@ struct Row {
         return sm.bin;
     }
 
-    // The cut at which the order's prefix reaches `target`: its number of elements (MASS
-    // false) or its mass.  Bins of a histogram narrow the range of keys until one value is
+    // The cut at which the order's prefix reaches `target`, its number of elements (MASS
+    // false) or its mass, known to lie among the keys from lo to hi, with `above` of the
+    // target's units above them.  Bins of a histogram narrow the range until one value is
     // left; the mass above a bin is summed in fp64 in a fixed order, and the histogram's
     // 32-bit sums only say where to look.  `total_mass`: of the prefix, where wanted.
     template <bool MASS>
-    __device__ __forceinline__ Cut select(double target, bool want_mass, double& total_mass) const {
+    __device__ __forceinline__ Ties select(double target, uint32_t lo, uint32_t hi, double above, bool want_mass,
+                                           double& total_mass) const {
         const int tid = threadIdx.x;
-        uint32_t lo = 0, hi = ~0u;     // the range of keys searched; everything above it is kept
-        double above = 0.0, ma = 0.0;  // what is above it, in units of the target, and its mass
-        for (int level = 0;; ++level) {
-            const int shift = level == 0 ? 0 : max(0, 32 - __clz((int)(hi - lo)) - 11);
-            // a key's or value's bin; every thread and pass maps alike
-            auto bin_of = [&](float l, uint32_t k) -> int {
-                if (level == 0) return (int)fminf((m - l) * kBinsPerUnit, (float)(kBins - 1));
-                return (int)((hi - k) >> shift);
-            };
+        for (;;) {
+            const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
             __syncthreads();
             for (int i = tid; i < kBins; i += BLOCK) sm.hist[i] = 0.0f;
             __syncthreads();
@@ -258,7 +300,7 @@ struct Row {
                     const uint32_t k = key_of(v[e]);
                     if (v[e] > -INFINITY && k >= lo && k <= hi) {
                         const float w = MASS ? exp2_fast((v[e] - m) * (float)fmin(c, (double)FLT_MAX)) : 1.0f;
-                        unsafeAtomicAdd(&sm.hist[bin_of(v[e], k)], w);
+                        unsafeAtomicAdd(&sm.hist[(hi - k) >> shift], w);
                     }
                 }
             }, [](int) {});
@@ -279,7 +321,7 @@ struct Row {
                         if (!(v[e] > -INFINITY)) continue;
                         const uint32_t k = key_of(v[e]);
                         if (k < lo) continue;
-                        const int b = k > hi ? -1 : bin_of(v[e], k);
+                        const int b = k > hi ? -1 : (int)((hi - k) >> shift);
                         if (b > bin) continue;
                         const double w = MASS || want_mass ? mass(v[e]) : 0.0;
                         if (b < bin) {
@@ -301,7 +343,7 @@ struct Row {
                 if (MASS && a >= target && turned <= 0) {
                     int b = bin - 1;
                     while (b > 0 && sm.hist[b] == 0.0f) --b;
-                    if (b >= 0) {
+                    if (b >= 0 && sm.hist[b] != 0.0f) {
                         bin = b;
                         turned = -1;
                         continue;
@@ -319,23 +361,195 @@ struct Row {
                 break;
             }
             above = a;
-            ma = mass_a;
             lo = kmin;
             hi = kmax;
-            if (lo == hi) {
+            if (lo >= hi) {
                 // nin equal values: how many of them are kept
                 const float tau = value_of(lo);
                 const double w = mass(tau);
-                int keep = nin;
-                if (!MASS) keep = (int)(target - above);
-                else if (w > 0.0 && above + in > target) {
-                    const double t = ceil((target - above) / w);
-                    keep = t < 1.0 ? 1 : t > (double)nin ? nin : (int)t;
-                }
-                total_mass = ma + (double)keep * w;
-                return {tau, keep < nin ? tie_limit(tau, keep) : INT_MAX};
+                const int keep = MASS ? ties_for(target - above, w, nin) : (int)(target - above);
+                total_mass = mass_a + (double)keep * w;
+                return {tau, keep, nin};
             }
         }
+    }
+
+    // How many of n elements of mass w reach `rest`.
+    __device__ __forceinline__ static int ties_for(double rest, double w, int n) {
+        const double t = w > 0.0 ? ceil(rest / w) : (double)n;
+        return t < 1.0 ? 1 : t > (double)n ? n : (int)t;
+    }
+
+    // How often each bf16 value occurs, and the row's maximum.  Whether the counts say all
+    // that a cut needs (values outside the bins' range, unless they have no mass, make the row
+    // one for the search above); a NaN or a +inf sets `bad`.
+    __device__ __forceinline__ bool count_values(bool& bad) {
+        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        for (int i = tid; i < kValueBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.count)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        i16x2 pos = {0, 0};
+        u16x2 neg = {0, 0};
+        sweep_raw([&](const typename W::raw& t, int) {
+            if constexpr (VEC == 8) {
+                const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    pos = __builtin_elementwise_max(pos, __builtin_bit_cast(i16x2, w[q]));
+                    neg = __builtin_elementwise_max(neg, __builtin_bit_cast(u16x2, w[q]));
+                    const u16x2 at = bin_bytes(w[q]);
+                    char* base = reinterpret_cast<char*>(sm.count);
+                    __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(base + at.x), 1u, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_WORKGROUP);
+                    __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(base + at.y), 1u, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
+            }
+        }, [](int) {});
+        // positive words from 0x7f80 are +inf and NaN, negative ones past 0xff80 NaN
+        const bool mine = pos.x >= 0x7f80 || pos.y >= 0x7f80 || neg.x > 0xff80 || neg.y > 0xff80;
+        bad = __syncthreads_or(mine);
+        // the highest value: the first bin that is not empty
+        int first = kValueBins;
+        for (int q = 0; q < PER / 4; ++q) {
+            const uint4 n = reinterpret_cast<const uint4*>(sm.count)[tid * (PER / 4) + q];
+            const int b = tid * PER + 4 * q;
+            first = min(first, n.x ? b : n.y ? b + 1 : n.z ? b + 2 : n.w ? b + 3 : kValueBins);
+        }
+        for (int o = 32; o; o >>= 1) first = min(first, __shfl_xor(first, o));
+        if (lane == 0) sm.redi[0][wid] = first;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) first = min(first, sm.redi[0][w]);
+        m = bin_value(first);
+        md = (double)m;
+        top = first;
+        if (!(first > kTopBin && first < kLastBin && (md + 1020.0) * c > 150.0)) return false;
+        if (sm.count[kZeroBin] == 0) return true;
+        bool small = false;   // nonzero values in the bin around zero
+        sweep([&](const float(&v)[VEC], int) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) small |= v[e] != 0.0f && fabsf(v[e]) <= 0x1p-38f;
+        }, [](int) {});
+        return !__syncthreads_or(small);
+    }
+    int top = 0;   // the bin of the row's highest value
+
+    // The bin in which the counts (BY_MASS: the masses) of the row's values reach `target`,
+    // from every thread's sums before and in its PER bins; into sm.cut_*.
+    template <bool BY_MASS>
+    __device__ __forceinline__ void locate(double target, double before_n, double before_m, double own_n, double own_m,
+                                           bool want_mass) const {
+        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const double own = BY_MASS ? own_m : own_n;
+        const uint64_t some = __ballot(own > 0.0);
+        const uint64_t hit = __ballot(own > 0.0 && (BY_MASS ? before_m : before_n) + own >= target);
+        __syncthreads();
+        if (lane == 0) {
+            sm.redi[0][wid] = hit ? wid * 64 + __ffsll((unsigned long long)hit) - 1 : BLOCK;
+            sm.redi[1][wid] = some ? wid * 64 + 63 - __clzll((long long)some) : 0;
+        }
+        __syncthreads();
+        int at = BLOCK, last = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            at = min(at, sm.redi[0][w]);
+            last = max(last, sm.redi[1][w]);
+        }
+        if (at == BLOCK) at = last;
+        if (tid == at) {
+            sm.cut_above = before_n;
+            sm.cut_mass = before_m;
+        }
+        __syncthreads();
+        if (wid == 0) {   // a lane for each of that thread's bins
+            const double base_n = sm.cut_above, base_m = sm.cut_mass;
+            const int b = at * PER + lane;
+            const int n = lane < PER && b < kLastBin ? (int)sm.count[b] : 0;
+            const double w = n && (BY_MASS || want_mass) ? mass(bin_value(b)) : 0.0;
+            const double in_n = base_n + wave_incl_scan((double)n, lane);
+            const double in_m = base_m + wave_incl_scan((double)n * w, lane);
+            const bool real = n > 0 && (!BY_MASS || w > 0.0);
+            const uint64_t over = __ballot(real && (BY_MASS ? in_m : in_n) >= target);
+            const uint64_t any = __ballot(real);
+            const int L = over ? __ffsll((unsigned long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
+            if (lane == L) {
+                const double above_n = in_n - (double)n, above_m = in_m - (double)n * w;
+                const int keep = BY_MASS ? ties_for(target - above_m, w, n) : (int)(target - above_n);
+                sm.cut_bin = b;
+                sm.cut_keep = keep;
+                sm.cut_all = n;
+                sm.cut_above = BY_MASS ? above_m : above_n;
+                sm.cut_mass = above_m + (double)keep * w;
+            }
+        }
+        __syncthreads();
+    }
+
+    // The cut of top_k and top_p from the counts of a row's values.  Where it falls among the
+    // values below all bins, the search ends it.
+    __device__ __forceinline__ Ties cut_values(int top_k, double top_p) const {
+        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const bool want_mass = top_p < 1.0;
+        double own_n = 0.0, own_m = 0.0;
+        for (int q = 0; q < PER / 4; ++q) {
+            const uint4 n4 = reinterpret_cast<const uint4*>(sm.count)[tid * (PER / 4) + q];
+            const uint32_t n[4] = {n4.x, n4.y, n4.z, n4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int b = tid * PER + 4 * q + e;
+                if (n[e] && b < kLastBin) {
+                    own_n += (double)n[e];
+                    if (want_mass) own_m += (double)n[e] * mass(bin_value(b));
+                }
+            }
+        }
+        const double in_n = wave_incl_scan(own_n, lane), in_m = wave_incl_scan(own_m, lane);
+        __syncthreads();
+        if (lane == 63) {
+            sm.red[0][wid] = in_n;
+            sm.red[1][wid] = in_m;
+        }
+        __syncthreads();
+        double before_n = in_n - own_n, before_m = in_m - own_m, all_n = 0.0, all_m = 0.0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wid) {
+                before_n += sm.red[0][w];
+                before_m += sm.red[1][w];
+            }
+            all_n += sm.red[0][w];
+            all_m += sm.red[1][w];
+        }
+        Ties cut{-INFINITY, 0, 0};
+        double mass_k = all_m;
+        bool cut_k = top_k > 0;
+        if (cut_k && (double)top_k > all_n) {
+            // into the last bin, which holds -inf too
+            int below = 0, none = 0;
+            double x = 0.0, y = 0.0;
+            sweep([&](const float(&v)[VEC], int) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) below += v[e] > -INFINITY && v[e] <= bin_value(kLastBin);
+            }, [](int) {});
+            sum2(x, y, below, none);
+            cut_k = all_n + (double)below > (double)top_k;
+            if (cut_k && !want_mass)   // top_p cuts above that bin, which has no mass
+                cut = select<false>((double)top_k, key_of(-INFINITY) + 1, key_of(bin_value(kLastBin)), all_n, want_mass,
+                                    mass_k);
+        } else if (cut_k) {
+            locate<false>((double)top_k, before_n, before_m, own_n, own_m, want_mass);
+            cut = {bin_value(sm.cut_bin), sm.cut_keep, sm.cut_all};
+            mass_k = sm.cut_mass;
+        }
+        if (top_p == 1.0) return cut;
+        locate<true>(top_p * mass_k, before_n, before_m, own_n, own_m, true);
+        return {bin_value(sm.cut_bin), sm.cut_keep, sm.cut_all};
+    }
+
+    // Number of the row's elements in the bins up to `bin`.
+    __device__ __forceinline__ int count_to(int bin) const {
+        int n = 0, none = 0;
+        double x = 0.0, y = 0.0;
+        for (int b = threadIdx.x; b <= bin; b += BLOCK) n += (int)sm.count[b];
+        sum2(x, y, n, none);
+        return n;
     }
 
     // The index of the keep-th element equal to tau.
@@ -351,31 +565,52 @@ struct Row {
             if (lane == 0) sm.ties[s] = n;
             cnt = 0;
         });
+        return tie_place(tau, keep);
+    }
+
+    // The same from the slots' numbers of such elements (sm.ties, which then holds how many of
+    // them are kept).
+    __device__ __forceinline__ int tie_place(float tau, int keep) const {
+        const int lane = threadIdx.x & 63;
+        constexpr int SPL = kRowSlots / 64;
         __syncthreads();
         if (threadIdx.x < 64) {
-            int left = keep, s = 0;
-            for (; s < nslots - 1 && sm.ties[s] < left; ++s) left -= sm.ties[s];
+            int n[SPL], own = 0;
+#pragma unroll
+            for (int q = 0; q < SPL; ++q) {
+                n[q] = SPL * lane + q < nslots ? sm.ties[SPL * lane + q] : 0;
+                own += n[q];
+            }
+            int before = incl_scan(own) - own, slot = -1, left = 0;
+#pragma unroll
+            for (int q = 0; q < SPL; ++q) {
+                const int kept = max(0, min(n[q], keep - before));
+                if (before < keep && before + n[q] >= keep) {
+                    slot = SPL * lane + q;
+                    left = keep - before;
+                }
+                if (SPL * lane + q < nslots) sm.ties[SPL * lane + q] = kept;
+                before += n[q];
+            }
+            const int L = __ffsll((unsigned long long)__ballot(slot >= 0)) - 1;
+            slot = __builtin_amdgcn_readlane(slot, L);
+            left = __builtin_amdgcn_readlane(left, L);
             int limit = -1;
-            for (int q = s * G * UNR; q < (s + 1) * G * UNR && limit < 0; ++q) {
+            for (int q = slot * G * UNR; q < (slot + 1) * G * UNR && limit < 0; ++q) {
                 const int j = q * 64 * VEC + lane * VEC;
                 float v[VEC];
                 load_vec<In, VEC>(row, j, V, v);
-                int own = 0;
+                int eq = 0;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) own += v[e] == tau;
-                int incl = own;
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int x = __shfl_up(incl, o);
-                    if (lane >= o) incl += x;
-                }
+                for (int e = 0; e < VEC; ++e) eq += v[e] == tau;
+                const int incl = incl_scan(eq);
                 const uint64_t hit = __ballot(incl >= left);
                 if (hit) {
-                    const int L = __ffsll((unsigned long long)hit) - 1;
-                    int at = -1, c2 = incl - own;
+                    int at = -1, c2 = incl - eq;
 #pragma unroll
                     for (int e = 0; e < VEC; ++e)
                         if (v[e] == tau && ++c2 == left) at = j + e;
-                    limit = __builtin_amdgcn_readlane(at, L);
+                    limit = __builtin_amdgcn_readlane(at, __ffsll((unsigned long long)hit) - 1);
                 }
                 left -= __builtin_amdgcn_readlane(incl, 63);
             }
@@ -383,6 +618,135 @@ struct Row {
         }
         __syncthreads();
         return sm.limit;
+    }
+    __device__ __forceinline__ static int incl_scan(int v) {
+        const int lane = threadIdx.x & 63;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(v, o);
+            if (lane >= o) v += x;
+        }
+        return v;
+    }
+
+    // The slots' sums of all masses, against the highest of the waves' first elements; or, where
+    // the row's maximum is far above it, against that.  False where the row has no
+    // distribution.
+    __device__ __forceinline__ bool slot_masses() {
+        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        float v[VEC], mx = -INFINITY;
+        load_vec<In, VEC>(row, wid * G * CHUNK + lane * VEC, V, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v[e]);
+        for (int attempt = 0;; ++attempt) {
+            mx = wave_max(mx);
+            __syncthreads();
+            if (lane == 0) sm.redf[wid] = mx;
+            __syncthreads();
+            for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sm.redf[w]);
+            // a NaN or a +inf here shows in the pass too
+            md = mx > -INFINITY && mx < INFINITY ? (double)mx : 0.0;
+            double a = 0.0;
+            int n = 0, bad = 0, none = 0;
+            sweep([&](const float(&t)[VEC], int) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    mx = fmaxf(mx, t[e]);
+                    n += t[e] > -INFINITY;
+                    bad |= !(t[e] < INFINITY);
+                    a += mass(t[e]);
+                }
+            }, [&](int s) {
+                const double t = wave_sum(a);
+                if (lane == 0) sm.slot[s] = t;
+                a = 0.0;
+            });
+            double x = 0.0, y = 0.0;
+            sum2(x, y, n, none);
+            finite = n;
+            m = wave_max(mx);
+            __syncthreads();
+            if (lane == 0) sm.redf[wid] = m;
+            const bool any_bad = __syncthreads_or(bad);
+            for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sm.redf[w]);
+            if (any_bad || n == 0) return false;
+            if (attempt == 1 || fabs((double)m - md) * c < 500.0) return true;
+            mx = m;
+        }
+    }
+    int finite = 0;
+
+    // The slots' sums of what a cut keeps, from a table of the masses of the values above it,
+    // and how many elements that is.  `partial`: the elements equal to the cut's value are
+    // counted by slot instead.  False where the table has no room for all values.
+    __device__ __forceinline__ bool table_masses(const Ties& cut, bool partial, int& n) const {
+        const int tid = threadIdx.x, lane = tid & 63;
+        if constexpr (VEC == 8) {
+            if (!(cut.tau > -INFINITY)) return false;
+            int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
+            if (end == kZeroBin && cut.tau > 0.0f) --end;   // the bin holds zeros, below the cut
+            if (end == kLastBin || end - top + 2 > kValueBins / 2) return false;
+            n = count_to(end) - (partial ? cut.all - cut.keep : 0);
+            __syncthreads();
+            for (int i = tid; i <= end - top + 1; i += BLOCK)
+                sm.table[i] = i > end - top || (partial && i == end - top) ? 0.0 : mass(bin_value(top + i));
+            __syncthreads();
+            const char* base = reinterpret_cast<const char*>(sm.table) - top * 8;
+            const uint16_t last = (uint16_t)(end * 4 + 4), at_cut = (uint16_t)(end * 4);
+            const u16x2 lasts = {last, last};
+            double a = 0.0;
+            int ties = 0;
+            sweep_raw([&](const typename W::raw& t, int) {
+                const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+                u16x2 at[4];
+                u16x2 lowest = lasts;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    at[q] = __builtin_elementwise_min(bin_bytes(w[q]), lasts);
+                    lowest = __builtin_elementwise_min(lowest, at[q]);
+                }
+                if (__ballot(lowest.x < last || lowest.y < last) == 0) return;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    a += *reinterpret_cast<const double*>(base + 2 * at[q].x);
+                    a += *reinterpret_cast<const double*>(base + 2 * at[q].y);
+                    if (partial) ties += (at[q].x == at_cut) + (at[q].y == at_cut);
+                }
+            }, [&](int s) {
+                const double t = wave_sum(a);
+                const int nt = partial ? __reduce_add_sync(~0ull, ties) : 0;
+                if (lane == 0) {
+                    sm.slot[s] = t;
+                    sm.ties[s] = nt;
+                }
+                a = 0.0;
+                ties = 0;
+            });
+            __syncthreads();
+            return true;
+        }
+        return false;
+    }
+
+    // Of the listed elements of a filtered row, all equal, the first `keep` stay; the others
+    // become -inf.
+    __device__ __forceinline__ void drop_ties(int keep, uint16_t* out) const {
+        const int tid = threadIdx.x;
+        __syncthreads();
+        const int n = sm.nlist;
+        for (int s = tid; s < kRowSlots; s += BLOCK) sm.ties[s] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += BLOCK) atomicAdd(&sm.ties[sm.list[i] / (G * CHUNK)], 1);
+        __syncthreads();
+        for (int i = tid; i < n; i += BLOCK) {
+            const int j = sm.list[i], s = j / (G * CHUNK);
+            int before = 0;
+            for (int q = 0; q < s; ++q) before += sm.ties[q];
+            if (before + sm.ties[s] > keep) {
+                if (before < keep)
+                    for (int q = 0; q < n; ++q) before += sm.list[q] < j && sm.list[q] / (G * CHUNK) == s;
+                if (before >= keep) out[j] = 0xff80;
+            }
+        }
     }
 
     // The token of uniform u: the first index at which the kept masses' running sum exceeds
@@ -497,11 +861,12 @@ __device__ __forceinline__ void store_vec(In* out, int j, int V, const float (&v
     }
 }
 
-// One workgroup a row: statistics, the cut, then the draws or the filtered row.
+// One workgroup a row: the cut, then the draws or the filtered row.
 template <typename In, int VEC, int UNR, int BLOCK, bool FILTER>
 __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
     __shared__ RowSmem sm;
     constexpr int kWaves = BLOCK / 64;
+    constexpr bool kCounts = VEC == 8;   // bf16 rows: counts of values
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int64_t r = blockIdx.x;
     const int64_t entry = r / P.rows_per_entry;
@@ -512,21 +877,72 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
     Row<In, VEC, UNR, BLOCK> row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
                                  1.4426950408889634 / (double)T, sm};
     In* out = FILTER ? reinterpret_cast<In*>(P.out) + r * P.out_stride : nullptr;
-    int status = RS_SEQ_OK, n = 0;
+    int status = RS_SEQ_OK;
     if (!(T > 0.0f && T < INFINITY && top_k >= 0 && top_p > 0.0f && top_p <= 1.0f && min_p >= 0.0f && min_p <= 1.0f))
         status = RS_SEQ_BAD_PARAM;
     if (!FILTER && status == RS_SEQ_OK) {
         const float u = tid < P.k ? P.u[r * P.k + tid] : 0.0f;
         if (__syncthreads_or(!(u >= 0.0f && u < 1.0f))) status = RS_SEQ_BAD_UNIFORM;
     }
-    if (status == RS_SEQ_OK && !row.statistics(n)) status = RS_SEQ_UNDERFLOW;
+    // ---- the cut, and whether the counts of the row's values are at hand
+    const bool filters = top_k > 0 || top_p < 1.0f || min_p > 0.0f;
+    Ties ties{-INFINITY, 0, 0};
+    bool counts = false;
+    int kept = -1;
+    if (status == RS_SEQ_OK && (filters || FILTER)) {
+        bool bad = false;
+        if constexpr (kCounts) {
+            counts = row.count_values(bad);
+            if (counts && filters) ties = row.cut_values(top_k, (double)top_p);
+        }
+        if (!counts) {
+            int n = 0;
+            if (bad || !row.statistics(n)) {
+                status = RS_SEQ_UNDERFLOW;
+            } else {
+                const uint32_t lo = key_of(-INFINITY) + 1, hi = key_of(row.m);
+                double mass = 0.0;
+                const bool cuts_k = top_k > 0 && top_k < n;
+                if (cuts_k) ties = row.template select<false>((double)top_k, lo, hi, 0.0, top_p < 1.0f, mass);
+                if (top_p < 1.0f) {
+                    if (!cuts_k) {
+                        double a = 0.0, b = 0.0;
+                        int x = 0, y = 0;
+                        row.sweep([&](const float(&v)[VEC], int) {
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) a += row.mass(v[e]);
+                        }, [](int) {});
+                        row.sum2(a, b, x, y);
+                        mass = a;
+                    }
+                    ties = row.template select<true>((double)top_p * mass, lo, hi, 0.0, false, mass);
+                }
+            }
+        } else if (bad) {
+            status = RS_SEQ_UNDERFLOW;
+        }
+        if (status == RS_SEQ_OK && min_p > 0.0f) {
+            // w >= min_p where l >= m + T ln(min_p): the lowest value of the row's type that is
+            const double t = row.md + (double)T * log((double)min_p);
+            float f = (float)t;
+            if ((double)f < t) f = value_of(key_of(f) + 1);
+            if (kCounts) {
+                const uint32_t b = __float_as_uint(f);
+                f = __uint_as_float((b & 0xffff0000u) + ((b & 0xffffu) && !(b >> 31) ? 0x10000u : 0u));
+            }
+            if (f > ties.tau) ties = Ties{f, 0, 0};
+        }
+    }
+    // ---- no filter: the slots' sums against a reference near the maximum
+    double total = 0.0;
+    if (status == RS_SEQ_OK && !FILTER && !filters)
+        if (!row.slot_masses()) status = RS_SEQ_UNDERFLOW;
     if (status != RS_SEQ_OK) {
         if (FILTER) {
-            const float none[VEC] = {};
             float inf[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) inf[e] = none[e] - INFINITY;
-            for (int64_t j = (int64_t)tid * VEC; j < P.V; j += BLOCK * VEC) store_vec<In, VEC>(out, (int)j, P.V, inf);
+            for (int e = 0; e < VEC; ++e) inf[e] = -INFINITY;
+            for (int j = tid * VEC; j < P.V; j += BLOCK * VEC) store_vec<In, VEC>(out, j, P.V, inf);
         } else if (tid < P.k) {
             P.token[r * P.k + tid] = -1;
             if (P.logprob) P.logprob[r * P.k + tid] = NAN;
@@ -537,66 +953,81 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
         }
         return;
     }
-    Cut cut{-INFINITY, -1};
-    double mass = 0.0;
-    const bool cuts_k = top_k > 0 && top_k < n;
-    if (cuts_k) cut = row.template select<false>((double)top_k, top_p < 1.0f, mass);
-    if (top_p < 1.0f) {
-        if (!cuts_k) {
-            double a = 0.0, b = 0.0;
-            int x = 0, y = 0;
-            row.sweep([&](const float(&v)[VEC], int) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) a += row.mass(v[e]);
-            }, [](int) {});
-            row.sum2(a, b, x, y);
-            mass = a;
-        }
-        cut = row.template select<true>((double)top_p * mass, true, mass);
-    }
-    if (min_p > 0.0f) {
-        // w >= min_p where l >= m + T ln(min_p): the lowest 32-bit value that is
-        const double t = row.md + (double)T * log((double)min_p);
-        float f = (float)t;
-        if ((double)f < t) f = value_of(key_of(f) + 1);
-        if (f > cut.tau) cut = Cut{f, INT_MAX};
-    }
-    int kept = 0, none = 0;
+    // ---- which of the elements equal to the cut's value are kept
+    const bool partial = ties.keep < ties.all;
+    Cut cut{ties.tau, ties.tau > -INFINITY ? INT_MAX : -1};
     if (FILTER) {
+        // many ties: their last index is found first; few: all are written as kept, and the
+        // rest taken back
+        constexpr int kListed = 4096;
+        const bool listed = counts && partial && ties.all <= kListed;
+        if (partial && !listed) cut.limit = row.tie_limit(ties.tau, ties.keep);
+        __syncthreads();
+        if (tid == 0) sm.nlist = 0;
+        __syncthreads();
+        int n = 0, none = 0;
         row.sweep([&](const float(&v)[VEC], int j) {
             float w[VEC];
+            bool tie = false;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const bool k = cut.keeps(v[e], j + e);
                 w[e] = k ? v[e] : -INFINITY;
-                kept += k;
+                n += k;
+                tie |= v[e] == ties.tau;
             }
             store_vec<In, VEC>(out, j, P.V, w);
-        }, [](int) {});
-    } else {
-        double a = 0.0;
-        row.sweep([&](const float(&v)[VEC], int j) {
+            if (listed && tie) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                if (cut.keeps(v[e], j + e)) {
-                    a += row.mass(v[e]);
-                    ++kept;
-                }
+                for (int e = 0; e < VEC; ++e)
+                    if (v[e] == ties.tau) sm.list[atomicAdd(&sm.nlist, 1)] = j + e;
             }
-        }, [&](int s) {
-            const double t = wave_sum(a);
-            if (lane == 0) sm.slot[s] = t;
-            a = 0.0;
-        });
+        }, [](int) {});
+        double x = 0.0, y = 0.0;
+        row.sum2(x, y, n, none);
+        if (listed) {
+            row.drop_ties(ties.keep, reinterpret_cast<uint16_t*>(out));
+            n -= ties.all - ties.keep;
+        }
+        kept = n;
+    } else if (filters) {
+        int n = 0, none = 0;
+        if (counts && row.table_masses(ties, partial, n)) {
+            if (partial) cut.limit = row.tie_place(ties.tau, ties.keep);
+            const double w = row.mass(ties.tau);
+            __syncthreads();
+            if (partial && tid < P.nslots) sm.slot[tid] += (double)sm.ties[tid] * w;
+            __syncthreads();
+            kept = n;
+        } else {
+            if (partial) cut.limit = row.tie_limit(ties.tau, ties.keep);
+            double a = 0.0;
+            row.sweep([&](const float(&v)[VEC], int j) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    if (cut.keeps(v[e], j + e)) {
+                        a += row.mass(v[e]);
+                        ++n;
+                    }
+                }
+            }, [&](int s) {
+                const double t = wave_sum(a);
+                if (lane == 0) sm.slot[s] = t;
+                a = 0.0;
+            });
+            double x = 0.0, y = 0.0;
+            row.sum2(x, y, n, none);
+            kept = n;
+        }
+    } else {
+        kept = row.finite;
     }
-    double x = 0.0, y = 0.0;
-    row.sum2(x, y, kept, none);
     if (tid == 0) {
         if (P.kept) P.kept[r] = kept;
         if (P.status) P.status[r] = RS_SEQ_OK;
     }
     if (FILTER) return;
-    double total = 0.0;
+    // ---- the draws
     for (int s = lane; s < P.nslots; s += 64) total += sm.slot[s];
     total = wave_sum(total);
     for (int i = wid; i < P.k; i += kWaves) {
