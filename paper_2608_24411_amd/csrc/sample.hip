@@ -18,14 +18,26 @@ namespace {
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
-constexpr int kUnrRow = 4;          // 16-byte loads a lane and chunk
+// 16-byte loads a lane and chunk: bf16 rows, others (fewer: four would cost registers that the
+// exponentials need)
+constexpr int kUnrRow16 = 4, kUnrRow32 = 2;
 
 // Bins of bf16 values, from the highest to the lowest: one for every value with 2^-38 < |l| <
-// 1020, one for those between (where both zeros are), one at each end for those outside
-// (-inf in the last).  Unused: bin 0.
+// 1020, one for both zeros, one on each side of it for the values nearer to zero, one at each
+// end for those outside (-inf in the last).  Unused: bin 0.
 constexpr int kHalf = 6144, kValueBins = 2 * kHalf;
 constexpr uint16_t kLoMag = (127 - 38) << 7, kTopMag = kHalf - 1;
 constexpr int kTopBin = 1, kZeroBin = kHalf, kLastBin = kValueBins - 1;
+constexpr int kGroups = kValueBins / 64, kLaneGroups = kGroups / 64;
+
+// Other rows: bins of 1/128 of a logit, from 8 above a reference near the maximum to 24 below
+// it (the first and last take what lies outside).
+constexpr int kLinearBins = 4096;
+constexpr float kBinsPerUnit = 128.0f, kRefBin = 1024.0f;
+constexpr double kMassUnit = 0x1p-40;           // of the masses in them
+// Elements that a search may leave to be sorted, and how many of them are sorted by counting.
+constexpr int kSorted = 2048, kRanked = 512;
+constexpr float kSampleBins = 64.0f;            // of a row's sample: bins a unit of logits
 
 struct SParams {
     const void* logits;
@@ -45,23 +57,58 @@ struct SParams {
     int32_t G, nslots;
 };
 
-struct RowSmem {
-    union {
-        float hist[kBins];            // search within a range of keys
-        uint32_t count[kValueBins];   // how often each bf16 value occurs
-        double table[kValueBins / 2]; // their masses, from the highest value of the row
-        int32_t list[kValueBins];     // indices of equal elements
-    };
-    double slot[kRowSlots];
-    int32_t ties[kRowSlots];
-    double cut_above, cut_mass;       // what lies above the crossing bin, and the prefix's mass
-    int32_t cut_bin, cut_keep, cut_all, nlist;
+struct ReduceSmem {
     double red[2][kMaxWaves];
     int32_t redi[2][kMaxWaves];
     uint32_t redk[2][kMaxWaves];
     float redf[kMaxWaves];
+};
+
+struct RowSmem : ReduceSmem {
+    union {
+        float hist[kBins];            // search within a range of keys
+        uint32_t count[kValueBins];   // how often each bf16 value occurs
+        double table[kValueBins / 2]; // their masses, from the highest value of the row
+        int32_t equal[kValueBins];    // indices of equal elements
+        uint32_t sample[kBins];       // of the row's first elements
+        uint64_t bins[kLinearBins];   // number or mass of the elements in a bin
+        struct {
+            uint64_t list[kSorted];   // elements: inverted key, index
+            uint64_t sorted[kSorted];
+            double running[kSorted];  // running sums of their masses
+        };
+    };
+    // sums over groups of 64 bins while the cut is looked for, over slots after that
+    union {
+        double slot[kRowSlots];
+        double group_sum[kGroups];
+    };
+    union {
+        int32_t ties[kRowSlots];
+        int32_t group_count[kGroups];
+    };
+    int32_t nlist;
     int32_t bin, limit;
 };
+
+// A value that all lanes hold, in scalar registers.
+__device__ __forceinline__ float uniform(float v) {
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+__device__ __forceinline__ double uniform(double v) {
+    return __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(v)),
+                            __builtin_amdgcn_readfirstlane(__double2loint(v)));
+}
+
+// The sum of an integer over a wave, to every lane.
+__device__ __forceinline__ int wave_sum_i(int v) {
+    v += dpp_i<kDppXor1>(v);
+    v += dpp_i<kDppXor2>(v);
+    v += dpp_i<kDppHalfMirror>(v);
+    v += dpp_i<kDppMirror>(v);
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) +
+           (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
 
 // Ordered keys: a > b as floats exactly where key(a) > key(b); -0 and +0 share one.
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -111,7 +158,8 @@ __device__ __forceinline__ u16x2 bin_bytes(uint32_t word) {
     const u16x2 lo = {kLoMag, kLoMag}, top = {kTopMag, kTopMag};
     const u16x2 one = {(uint16_t)(kHalf + 1), (uint16_t)(kHalf + 1)};
     const u16x2 mag = __builtin_bit_cast(u16x2, word & 0x7fff7fffu);
-    const u16x2 t = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, lo), top);
+    const u16x2 far = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, lo), top);
+    const u16x2 t = __builtin_elementwise_max(far, __builtin_elementwise_min(mag, u16x2{1, 1}));
     const u16x2 neg = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, word) >> 15);
     // kHalf - t for positive values, kHalf + t for negative ones
     return (~(t ^ neg) + neg + one) << 2;
@@ -122,17 +170,17 @@ __device__ __forceinline__ float bin_value(int bin) {
     return __uint_as_float((uint32_t)(t + kLoMag) << 16 | (bin > kHalf ? 0x80000000u : 0u));
 }
 
-template <typename In, int VEC, int UNR, int BLOCK>
+template <typename In, int VEC, int UNR, int BLOCK, typename Smem = RowSmem>
 struct Row {
     using W = Vec<In, VEC>;
     static constexpr int CHUNK = 64 * VEC * UNR;
     static constexpr int kWaves = BLOCK / 64;
-    static constexpr int PER = kValueBins / BLOCK;   // bins a thread
     const In* row;
     int V, G, nslots;
     float m;       // the row's maximum
-    double md, c;  // the same, and log2(e) / T
-    RowSmem& sm;
+    double md, c;  // the reference of the masses, the maximum or near it; log2(e) / T
+    double T;
+    Smem& sm;
 
     __device__ __forceinline__ double mass(float l) const { return exp2_64(((double)l - md) * c); }
 
@@ -181,11 +229,23 @@ struct Row {
         }, flush);
     }
 
+    // body(l, j), one element a load: for the rare passes, which would cost the others their
+    // registers.
+    template <typename Body>
+    __device__ __forceinline__ void each(Body&& body) const {
+        using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
+        for (int j = threadIdx.x; j < V; j += BLOCK) {
+            float v[1];
+            load_vec<E, 1>(reinterpret_cast<const E*>(row), j, V, v);
+            body(v[0], j);
+        }
+    }
+
     // Sums over the workgroup in a fixed order, to every thread.
     __device__ __forceinline__ void sum2(double& a, double& b, int& p, int& q) const {
         const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
         const double wa = wave_sum(a), wb = wave_sum(b);
-        const int wp = __reduce_add_sync(~0ull, p), wq = __reduce_add_sync(~0ull, q);
+        const int wp = wave_sum_i(p), wq = wave_sum_i(q);
         __syncthreads();
         if (lane == 0) {
             sm.red[0][wid] = wa;
@@ -202,6 +262,18 @@ struct Row {
             p += sm.redi[0][w];
             q += sm.redi[1][w];
         }
+        a = uniform(a);
+        b = uniform(b);
+        p = __builtin_amdgcn_readfirstlane(p);
+        q = __builtin_amdgcn_readfirstlane(q);
+    }
+    __device__ __forceinline__ float block_max(float v) const {
+        v = wave_max(v);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sm.redf[threadIdx.x >> 6] = v;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) v = fmaxf(v, sm.redf[w]);
+        return uniform(v);
     }
     __device__ __forceinline__ void range(uint32_t& lo, uint32_t& hi) const {
         const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
@@ -224,7 +296,6 @@ struct Row {
     // Maximum and number of the row's finite elements; false where the row has a NaN, a
     // +inf or no finite element.
     __device__ __forceinline__ bool statistics(int& n) {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
         float mx = -INFINITY;
         int cnt = 0, bad = 0;
         sweep([&](const float(&v)[VEC], int) {
@@ -235,17 +306,14 @@ struct Row {
                 bad |= !(v[e] < INFINITY);
             }
         }, [](int) {});
-        mx = wave_max(mx);
-        __syncthreads();
-        if (lane == 0) sm.redf[wid] = mx;
+        mx = block_max(mx);
         const bool any_bad = __syncthreads_or(bad);
-        for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sm.redf[w]);
         double x = 0.0, y = 0.0;
         int z = 0;
         sum2(x, y, cnt, z);
         n = cnt;
         m = mx;
-        md = (double)mx;
+        md = uniform((double)mx);
         return !any_bad && n > 0;
     }
 
@@ -294,16 +362,11 @@ struct Row {
             __syncthreads();
             for (int i = tid; i < kBins; i += BLOCK) sm.hist[i] = 0.0f;
             __syncthreads();
-            sweep([&](const float(&v)[VEC], int) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const uint32_t k = key_of(v[e]);
-                    if (v[e] > -INFINITY && k >= lo && k <= hi) {
-                        const float w = MASS ? exp2_fast((v[e] - m) * (float)fmin(c, (double)FLT_MAX)) : 1.0f;
-                        unsafeAtomicAdd(&sm.hist[(hi - k) >> shift], w);
-                    }
-                }
-            }, [](int) {});
+            each([&](float l, int) {
+                const uint32_t k = key_of(l);
+                if (l > -INFINITY && k >= lo && k <= hi)
+                    unsafeAtomicAdd(&sm.hist[(hi - k) >> shift], MASS ? (float)mass(l) : 1.0f);
+            });
             int bin = crossing(above, target);
             double a, in, mass_a, mass_in;
             int na, nin;
@@ -315,26 +378,22 @@ struct Row {
                 na = nin = 0;
                 kmin = ~0u;
                 kmax = 0u;
-                sweep([&](const float(&v)[VEC], int) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        if (!(v[e] > -INFINITY)) continue;
-                        const uint32_t k = key_of(v[e]);
-                        if (k < lo) continue;
-                        const int b = k > hi ? -1 : (int)((hi - k) >> shift);
-                        if (b > bin) continue;
-                        const double w = MASS || want_mass ? mass(v[e]) : 0.0;
-                        if (b < bin) {
-                            ++na;
-                            mass_a += w;
-                        } else {
-                            ++nin;
-                            mass_in += w;
-                            kmin = min(kmin, k);
-                            kmax = max(kmax, k);
-                        }
+                each([&](float l, int) {
+                    const uint32_t k = key_of(l);
+                    if (!(l > -INFINITY) || k < lo) return;
+                    const int b = k > hi ? -1 : (int)((hi - k) >> shift);
+                    if (b > bin) return;
+                    const double w = MASS || want_mass ? mass(l) : 0.0;
+                    if (b < bin) {
+                        ++na;
+                        mass_a += w;
+                    } else {
+                        ++nin;
+                        mass_in += w;
+                        kmin = min(kmin, k);
+                        kmax = max(kmax, k);
                     }
-                }, [](int) {});
+                });
                 sum2(mass_a, mass_in, na, nin);
                 range(kmin, kmax);
                 a = MASS ? mass_a : (double)na;
@@ -392,164 +451,175 @@ struct Row {
         sweep_raw([&](const typename W::raw& t, int) {
             if constexpr (VEC == 8) {
                 const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+                u16x2 at[4], most = {0, 0};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     pos = __builtin_elementwise_max(pos, __builtin_bit_cast(i16x2, w[q]));
                     neg = __builtin_elementwise_max(neg, __builtin_bit_cast(u16x2, w[q]));
-                    const u16x2 at = bin_bytes(w[q]);
-                    char* base = reinterpret_cast<char*>(sm.count);
-                    __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(base + at.x), 1u, __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_WORKGROUP);
-                    __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(base + at.y), 1u, __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_WORKGROUP);
+                    at[q] = bin_bytes(w[q]);
+                    most = __builtin_elementwise_max(most, at[q]);
+                }
+                char* base = reinterpret_cast<char*>(sm.count);
+                auto add = [&](int byte) {
+                    uint32_t* at = reinterpret_cast<uint32_t*>(base + byte);
+                    __hip_atomic_fetch_add(at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                };
+                // the last bin's count is not used, and masked rows would crowd it
+                if (__ballot(most.x == 4 * kLastBin || most.y == 4 * kLastBin) == 0) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        add(at[q].x);
+                        add(at[q].y);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (at[q].x < 4 * kLastBin) add(at[q].x);
+                        if (at[q].y < 4 * kLastBin) add(at[q].y);
+                    }
                 }
             }
         }, [](int) {});
         // positive words from 0x7f80 are +inf and NaN, negative ones past 0xff80 NaN
         const bool mine = pos.x >= 0x7f80 || pos.y >= 0x7f80 || neg.x > 0xff80 || neg.y > 0xff80;
         bad = __syncthreads_or(mine);
+        for (int g = wid; g < kGroups; g += kWaves) {
+            const int b = g * 64 + lane;
+            const int n = wave_sum_i(b < kLastBin ? (int)sm.count[b] : 0);
+            if (lane == 0) sm.group_count[g] = n;
+        }
+        __syncthreads();
         // the highest value: the first bin that is not empty
         int first = kValueBins;
-        for (int q = 0; q < PER / 4; ++q) {
-            const uint4 n = reinterpret_cast<const uint4*>(sm.count)[tid * (PER / 4) + q];
-            const int b = tid * PER + 4 * q;
-            first = min(first, n.x ? b : n.y ? b + 1 : n.z ? b + 2 : n.w ? b + 3 : kValueBins);
-        }
-        for (int o = 32; o; o >>= 1) first = min(first, __shfl_xor(first, o));
-        if (lane == 0) sm.redi[0][wid] = first;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) first = min(first, sm.redi[0][w]);
-        m = bin_value(first);
-        md = (double)m;
-        top = first;
-        if (!(first > kTopBin && first < kLastBin && (md + 1020.0) * c > 150.0)) return false;
-        if (sm.count[kZeroBin] == 0) return true;
-        bool small = false;   // nonzero values in the bin around zero
-        sweep([&](const float(&v)[VEC], int) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) small |= v[e] != 0.0f && fabsf(v[e]) <= 0x1p-38f;
-        }, [](int) {});
-        return !__syncthreads_or(small);
+        for (int q = kLaneGroups - 1; q >= 0; --q)
+            if (sm.group_count[lane * kLaneGroups + q]) first = lane * kLaneGroups + q;
+        const uint64_t some = __ballot(first < kValueBins);
+        if (some) {
+            const int g = __builtin_amdgcn_readlane(first, __ffsll((unsigned long long)some) - 1);
+            const uint64_t in = __ballot(g * 64 + lane < kLastBin && sm.count[g * 64 + lane]);
+            first = g * 64 + __ffsll((unsigned long long)in) - 1;
+        }
+        first = __builtin_amdgcn_readfirstlane(first);
+        m = uniform(bin_value(first));
+        md = uniform((double)m);
+        top = first;
+        return first > kTopBin && first < kLastBin && (md + 1020.0) * c > 150.0 &&
+               (sm.count[kZeroBin - 1] | sm.count[kZeroBin + 1]) == 0;
     }
     int top = 0;   // the bin of the row's highest value
 
-    // The bin in which the counts (BY_MASS: the masses) of the row's values reach `target`,
-    // from every thread's sums before and in its PER bins; into sm.cut_*.
-    template <bool BY_MASS>
-    __device__ __forceinline__ void locate(double target, double before_n, double before_m, double own_n, double own_m,
-                                           bool want_mass) const {
-        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-        const double own = BY_MASS ? own_m : own_n;
-        const uint64_t some = __ballot(own > 0.0);
-        const uint64_t hit = __ballot(own > 0.0 && (BY_MASS ? before_m : before_n) + own >= target);
-        __syncthreads();
-        if (lane == 0) {
-            sm.redi[0][wid] = hit ? wid * 64 + __ffsll((unsigned long long)hit) - 1 : BLOCK;
-            sm.redi[1][wid] = some ? wid * 64 + 63 - __clzll((long long)some) : 0;
+    // The group of 64 bins in which a running sum over the groups reaches `target`, or the last
+    // with anything in it; `base` is the sum before it, `base2` that of another array.
+    // Every wave finds the same.
+    template <typename A, typename B>
+    __device__ __forceinline__ static int reach_group(const A* sums, const B* others, double target, double& base,
+                                                      double& base2) {
+        const int lane = threadIdx.x & 63;
+        double a[kLaneGroups], b[kLaneGroups], own = 0.0, own2 = 0.0;
+#pragma unroll
+        for (int q = 0; q < kLaneGroups; ++q) {
+            a[q] = (double)sums[lane * kLaneGroups + q];
+            b[q] = (double)others[lane * kLaneGroups + q];
+            own += a[q];
+            own2 += b[q];
         }
-        __syncthreads();
-        int at = BLOCK, last = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            at = min(at, sm.redi[0][w]);
-            last = max(last, sm.redi[1][w]);
-        }
-        if (at == BLOCK) at = last;
-        if (tid == at) {
-            sm.cut_above = before_n;
-            sm.cut_mass = before_m;
-        }
-        __syncthreads();
-        if (wid == 0) {   // a lane for each of that thread's bins
-            const double base_n = sm.cut_above, base_m = sm.cut_mass;
-            const int b = at * PER + lane;
-            const int n = lane < PER && b < kLastBin ? (int)sm.count[b] : 0;
-            const double w = n && (BY_MASS || want_mass) ? mass(bin_value(b)) : 0.0;
-            const double in_n = base_n + wave_incl_scan((double)n, lane);
-            const double in_m = base_m + wave_incl_scan((double)n * w, lane);
-            const bool real = n > 0 && (!BY_MASS || w > 0.0);
-            const uint64_t over = __ballot(real && (BY_MASS ? in_m : in_n) >= target);
-            const uint64_t any = __ballot(real);
-            const int L = over ? __ffsll((unsigned long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
-            if (lane == L) {
-                const double above_n = in_n - (double)n, above_m = in_m - (double)n * w;
-                const int keep = BY_MASS ? ties_for(target - above_m, w, n) : (int)(target - above_n);
-                sm.cut_bin = b;
-                sm.cut_keep = keep;
-                sm.cut_all = n;
-                sm.cut_above = BY_MASS ? above_m : above_n;
-                sm.cut_mass = above_m + (double)keep * w;
+        const double incl = base + wave_incl_scan(own, lane), incl2 = base2 + wave_incl_scan(own2, lane);
+        const uint64_t hit = __ballot(own > 0.0 && incl >= target), some = __ballot(own > 0.0);
+        const int L = hit ? __ffsll((unsigned long long)hit) - 1 : some ? 63 - __clzll((long long)some) : 0;
+        double c = incl - own, c2 = incl2 - own2, at = c, at2 = c2;
+        int g = lane * kLaneGroups;
+        bool found = false;
+#pragma unroll
+        for (int q = 0; q < kLaneGroups; ++q) {
+            if (a[q] > 0.0 && !found) {
+                g = lane * kLaneGroups + q;
+                at = c;
+                at2 = c2;
+                found = c + a[q] >= target;
             }
+            c += a[q];
+            c2 += b[q];
         }
-        __syncthreads();
+        base = readlane_d(at, L);
+        base2 = readlane_d(at2, L);
+        return __builtin_amdgcn_readlane(g, L);
+    }
+
+    // The value at which the counts (BY_MASS: the masses) of the row's values reach `target`,
+    // how many of the elements equal to it are kept, and the prefix's mass.
+    template <bool BY_MASS>
+    __device__ __forceinline__ Ties locate(double target, bool want_mass, double& prefix) const {
+        const int lane = threadIdx.x & 63;
+        double base = 0.0, base2 = 0.0;
+        const int g = BY_MASS ? reach_group(sm.group_sum, sm.group_sum, target, base, base2)
+                              : reach_group(sm.group_count, sm.group_sum, target, base, base2);
+        const int b = g * 64 + lane;
+        const int n = b < kLastBin ? (int)sm.count[b] : 0;
+        const double w = n && (BY_MASS || want_mass) ? mass(bin_value(b)) : 0.0;
+        const double in_m = (BY_MASS ? base : base2) + wave_incl_scan((double)n * w, lane);
+        const double in = BY_MASS ? in_m : base + wave_incl_scan((double)n, lane);
+        const bool real = n > 0 && (!BY_MASS || w > 0.0);
+        const uint64_t over = __ballot(real && in >= target), any = __ballot(real);
+        const int L = over ? __ffsll((unsigned long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
+        const double above_m = in_m - (double)n * w;
+        const int keep = BY_MASS ? ties_for(target - above_m, w, n) : (int)(target - (in - (double)n));
+        prefix = readlane_d(above_m + (double)keep * w, L);
+        return {readlane_f(bin_value(b), L), __builtin_amdgcn_readlane(keep, L), __builtin_amdgcn_readlane(n, L)};
     }
 
     // The cut of top_k and top_p from the counts of a row's values.  Where it falls among the
     // values below all bins, the search ends it.
     __device__ __forceinline__ Ties cut_values(int top_k, double top_p) const {
-        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
         const bool want_mass = top_p < 1.0;
-        double own_n = 0.0, own_m = 0.0;
-        for (int q = 0; q < PER / 4; ++q) {
-            const uint4 n4 = reinterpret_cast<const uint4*>(sm.count)[tid * (PER / 4) + q];
-            const uint32_t n[4] = {n4.x, n4.y, n4.z, n4.w};
+        for (int g = wid; g < kGroups; g += kWaves) {
+            double t = 0.0;
+            if (want_mass && sm.group_count[g]) {
+                const int b = g * 64 + lane;
+                const int n = b < kLastBin ? (int)sm.count[b] : 0;
+                t = wave_sum(n ? (double)n * mass(bin_value(b)) : 0.0);
+            }
+            if (lane == 0) sm.group_sum[g] = t;
+        }
+        __syncthreads();
+        int all = 0;
+        double all_m = 0.0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int b = tid * PER + 4 * q + e;
-                if (n[e] && b < kLastBin) {
-                    own_n += (double)n[e];
-                    if (want_mass) own_m += (double)n[e] * mass(bin_value(b));
-                }
-            }
+        for (int q = 0; q < kLaneGroups; ++q) {
+            all += sm.group_count[lane * kLaneGroups + q];
+            all_m += sm.group_sum[lane * kLaneGroups + q];
         }
-        const double in_n = wave_incl_scan(own_n, lane), in_m = wave_incl_scan(own_m, lane);
-        __syncthreads();
-        if (lane == 63) {
-            sm.red[0][wid] = in_n;
-            sm.red[1][wid] = in_m;
-        }
-        __syncthreads();
-        double before_n = in_n - own_n, before_m = in_m - own_m, all_n = 0.0, all_m = 0.0;
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wid) {
-                before_n += sm.red[0][w];
-                before_m += sm.red[1][w];
-            }
-            all_n += sm.red[0][w];
-            all_m += sm.red[1][w];
-        }
+        all = wave_sum_i(all);
+        all_m = wave_sum(all_m);
         Ties cut{-INFINITY, 0, 0};
-        double mass_k = all_m;
-        bool cut_k = top_k > 0;
-        if (cut_k && (double)top_k > all_n) {
-            // into the last bin, which holds -inf too
+        if (top_k > all) {
+            // into the last bin, which holds -inf too; it has no mass, so top_p cuts above it
             int below = 0, none = 0;
             double x = 0.0, y = 0.0;
-            sweep([&](const float(&v)[VEC], int) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) below += v[e] > -INFINITY && v[e] <= bin_value(kLastBin);
-            }, [](int) {});
-            sum2(x, y, below, none);
-            cut_k = all_n + (double)below > (double)top_k;
-            if (cut_k && !want_mass)   // top_p cuts above that bin, which has no mass
-                cut = select<false>((double)top_k, key_of(-INFINITY) + 1, key_of(bin_value(kLastBin)), all_n, want_mass,
-                                    mass_k);
-        } else if (cut_k) {
-            locate<false>((double)top_k, before_n, before_m, own_n, own_m, want_mass);
-            cut = {bin_value(sm.cut_bin), sm.cut_keep, sm.cut_all};
-            mass_k = sm.cut_mass;
+            if (!want_mass) {
+                each([&](float l, int) { below += l > -INFINITY && l <= bin_value(kLastBin); });
+                sum2(x, y, below, none);
+                if (all + below > top_k)
+                    cut = select<false>((double)top_k, key_of(-INFINITY) + 1, key_of(bin_value(kLastBin)), (double)all,
+                                        false, x);
+            }
+        } else if (top_k > 0) {
+            cut = locate<false>((double)top_k, want_mass, all_m);
         }
-        if (top_p == 1.0) return cut;
-        locate<true>(top_p * mass_k, before_n, before_m, own_n, own_m, true);
-        return {bin_value(sm.cut_bin), sm.cut_keep, sm.cut_all};
+        if (!want_mass) return cut;
+        double prefix;
+        return locate<true>(top_p * all_m, true, prefix);
     }
 
     // Number of the row's elements in the bins up to `bin`.
     __device__ __forceinline__ int count_to(int bin) const {
-        int n = 0, none = 0;
-        double x = 0.0, y = 0.0;
-        for (int b = threadIdx.x; b <= bin; b += BLOCK) n += (int)sm.count[b];
-        sum2(x, y, n, none);
-        return n;
+        const int lane = threadIdx.x & 63, g = bin / 64;
+        int n = lane <= bin % 64 ? (int)sm.count[g * 64 + lane] : 0;
+#pragma unroll
+        for (int q = 0; q < kLaneGroups; ++q)
+            if (lane * kLaneGroups + q < g) n += sm.group_count[lane * kLaneGroups + q];
+        return wave_sum_i(n);
     }
 
     // The index of the keep-th element equal to tau.
@@ -561,7 +631,7 @@ struct Row {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) cnt += v[e] == tau;
         }, [&](int s) {
-            const int n = __reduce_add_sync(~0ull, cnt);
+            const int n = wave_sum_i(cnt);
             if (lane == 0) sm.ties[s] = n;
             cnt = 0;
         });
@@ -628,28 +698,25 @@ struct Row {
         return v;
     }
 
-    // The slots' sums of all masses, against the highest of the waves' first elements; or, where
+    // The slots' sums of all masses, against the highest element of the row's sample; or, where
     // the row's maximum is far above it, against that.  False where the row has no
     // distribution.
     __device__ __forceinline__ bool slot_masses() {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63;
         float v[VEC], mx = -INFINITY;
-        load_vec<In, VEC>(row, wid * G * CHUNK + lane * VEC, V, v);
+        load_sample(v);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v[e]);
         for (int attempt = 0;; ++attempt) {
-            mx = wave_max(mx);
-            __syncthreads();
-            if (lane == 0) sm.redf[wid] = mx;
-            __syncthreads();
-            for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sm.redf[w]);
+            mx = block_max(mx);
             // a NaN or a +inf here shows in the pass too
-            md = mx > -INFINITY && mx < INFINITY ? (double)mx : 0.0;
+            md = uniform(mx > -INFINITY && mx < INFINITY ? (double)mx : 0.0);
             double a = 0.0;
             int n = 0, bad = 0, none = 0;
             sweep([&](const float(&t)[VEC], int) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
+                    if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                     mx = fmaxf(mx, t[e]);
                     n += t[e] > -INFINITY;
                     bad |= !(t[e] < INFINITY);
@@ -663,17 +730,429 @@ struct Row {
             double x = 0.0, y = 0.0;
             sum2(x, y, n, none);
             finite = n;
-            m = wave_max(mx);
-            __syncthreads();
-            if (lane == 0) sm.redf[wid] = m;
+            m = block_max(mx);
             const bool any_bad = __syncthreads_or(bad);
-            for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sm.redf[w]);
             if (any_bad || n == 0) return false;
             if (attempt == 1 || fabs((double)m - md) * c < 500.0) return true;
             mx = m;
         }
     }
     int finite = 0;
+
+    // ---- rows whose kept elements are few, or whose values are many
+
+    // The row's sample: the first elements of eight slots spread over it, whatever the
+    // workgroup's size, so that what is relative to it does not depend on that; a vector for
+    // each lane of the first eight waves.
+    static constexpr int kSampleSlots = 8, kSample = kSampleSlots * 64 * VEC;
+    __device__ __forceinline__ void load_sample(float (&v)[VEC]) const {
+        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = -INFINITY;
+        if (wid < kSampleSlots)
+            load_vec<In, VEC>(row, (int)((uint32_t)wid * (uint32_t)nslots / kSampleSlots) * G * CHUNK + lane * VEC, V, v);
+    }
+
+    // The sample, the highest of its elements (finite, or the answer is false) and their
+    // histogram below it.
+    __device__ __forceinline__ bool take_sample(float (&v)[VEC], float& ref) const {
+        const int tid = threadIdx.x;
+        load_sample(v);
+        __syncthreads();
+        for (int i = tid; i < kBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.sample)[i] = make_uint4(0, 0, 0, 0);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v[e]);
+        ref = block_max(mx);
+        if (!(ref > -INFINITY && ref < INFINITY)) return false;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float b = (ref - v[e]) * kSampleBins;
+            if (b < (float)(kBins - 1)) atomicAdd(&sm.sample[(int)b], 1u);
+        }
+        __syncthreads();
+        return true;
+    }
+
+    // A threshold above which lie, going by the sample, `rank` of its elements (BY_MASS: all
+    // but `rest` of its mass, in which the highest element stands for itself alone and every
+    // other one for `scale` elements); -inf where there is none.  Every wave finds the same.
+    template <bool BY_MASS>
+    __device__ __forceinline__ float threshold(float ref, float rank, float rest, float scale) const {
+        const int lane = threadIdx.x & 63;
+        constexpr int PER = kBins / 64;
+        const float step = -(float)fmin(c, 1e30) / kSampleBins;
+        float own = 0.0f;
+        for (int q = 0; q < PER / 4; ++q) {
+            const uint4 n = reinterpret_cast<const uint4*>(sm.sample)[lane * (PER / 4) + q];
+            const float b = (float)(lane * PER + 4 * q) + 0.5f;
+            own += BY_MASS ? ((float)n.x * exp2_fast(b * step) + (float)n.y * exp2_fast((b + 1.0f) * step)) +
+                                 ((float)n.z * exp2_fast((b + 2.0f) * step) + (float)n.w * exp2_fast((b + 3.0f) * step))
+                           : (float)(n.x + n.y + n.z + n.w);
+        }
+        const double incl = wave_incl_scan((double)own, lane);
+        double goal = (double)rank;
+        if (BY_MASS) {
+            const double total = readlane_d(incl, 63), first = (double)exp2_fast(0.5f * step);
+            goal = total - (double)rest * (fmax(total - first, 0.0) + first / (double)scale);
+        }
+        const uint64_t hit = __ballot(incl >= goal);
+        if (!hit) return -INFINITY;
+        const int L = __ffsll((unsigned long long)hit) - 1;
+        const int b = L * PER + lane;
+        const float n = lane < PER ? (float)sm.sample[b] : 0.0f;
+        const double in = readlane_d(incl - (double)own, L) +
+                          wave_incl_scan((double)(BY_MASS ? n * exp2_fast(((float)b + 0.5f) * step) : n), lane);
+        const uint64_t over = __ballot(lane < PER && in >= goal * (1.0 - 1e-6));
+        const int at = over ? L * PER + __ffsll((unsigned long long)over) - 1 : kBins;
+        return at < kBins - 1 ? ref - (float)(at + 1) / kSampleBins : -INFINITY;
+    }
+
+    // Adds a vector's elements that are at least tau, if any, to the list.
+    __device__ __forceinline__ void gather(const float (&v)[VEC], int j, float tau) const {
+        uint64_t in[VEC], any = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            in[e] = __ballot(v[e] >= tau);
+            any |= in[e];
+        }
+        if (any == 0) return;
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) n += __popcll(in[e]);
+        int at = 0;
+        if ((threadIdx.x & 63) == 0) at = atomicAdd(&sm.nlist, n);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            if (in[e] == 0) continue;
+            const int i = at + __popcll(in[e] & __lanemask_lt());
+            if (v[e] >= tau && i < kSorted) sm.list[i] = (uint64_t)~key_of(v[e]) << 32 | (uint32_t)(j + e);
+            at += __popcll(in[e]);
+        }
+    }
+
+    // sm.list[0 .. n) into sm.sorted in ascending order, n <= kSorted; no two are equal.
+    __device__ __forceinline__ void sort(int n) const {
+        const int tid = threadIdx.x;
+        __syncthreads();
+        if (n <= kRanked) {
+            // an element's place is the number of those below it
+            if (tid == 0 && (n & 1)) sm.list[n] = ~0ull;
+            __syncthreads();
+            for (int i = tid; i < n; i += BLOCK) {
+                const uint64_t x = sm.list[i];
+                int before = 0;
+                for (int q = 0; q < n; q += 2) {
+                    const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&sm.list[q]);
+                    before += (y.x < x) + (y.y < x);
+                }
+                sm.sorted[before] = x;
+            }
+            __syncthreads();
+            return;
+        }
+        const int size = n <= 1024 ? 1024 : 2048;
+        for (int i = tid; i < size; i += BLOCK) sm.sorted[i] = i < n ? sm.list[i] : ~0ull;
+        for (int k = 2; k <= size; k <<= 1)
+            for (int j = k >> 1; j; j >>= 1) {
+                __syncthreads();
+                for (int p = tid; p < size / 2; p += BLOCK) {
+                    const int a = 2 * p - (p & (j - 1)), b = a + j;
+                    const uint64_t x = sm.sorted[a], y = sm.sorted[b];
+                    if ((x > y) == ((a & k) == 0)) {
+                        sm.sorted[a] = y;
+                        sm.sorted[b] = x;
+                    }
+                }
+            }
+        __syncthreads();
+    }
+    __device__ __forceinline__ float sorted_value(int i) const { return value_of(~(uint32_t)(sm.sorted[i] >> 32)); }
+
+    // Running sums of the masses of sm.sorted[0 .. n) into sm.running.
+    __device__ __forceinline__ void prefix(int n) const {
+        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const int per = (n + BLOCK - 1) / BLOCK;
+        double own = 0.0;
+        for (int q = 0; q < per; ++q)
+            if (tid * per + q < n) own += mass(sorted_value(tid * per + q));
+        const double incl = wave_incl_scan(own, lane);
+        if (lane == 63) sm.red[0][wid] = incl;
+        __syncthreads();
+        double at = incl - own;
+        for (int v = 0; v < wid; ++v) at += sm.red[0][v];
+        for (int q = 0; q < per; ++q) {
+            if (tid * per + q >= n) break;
+            at += mass(sorted_value(tid * per + q));
+            sm.running[tid * per + q] = at;
+        }
+        __syncthreads();
+    }
+    // The first i < n with sm.running[i] >= goal, n where there is none.
+    __device__ __forceinline__ int reach_running(int n, double goal) const {
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sm.running[mid] >= goal) hi = mid;
+            else lo = mid + 1;
+        }
+        return lo;
+    }
+    // How many of sm.sorted[0 .. n) are at least `floor`; one at least.
+    __device__ __forceinline__ int above_floor(int n, float floor) const {
+        int lo = 1, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sorted_value(mid) >= floor) lo = mid + 1;
+            else hi = mid;
+        }
+        return lo;
+    }
+    // Adds the masses of sm.sorted[0 .. n) to the slots' sums (CLEAR: which were none), as
+    // whole numbers of 2^-52 of the first's power of two, so that their order does not count.
+    template <bool CLEAR>
+    __device__ __forceinline__ void add_to_slots(int n) const {
+        const int tid = threadIdx.x;
+        unsigned long long* sums = reinterpret_cast<unsigned long long*>(sm.running);
+        __syncthreads();
+        for (int i = tid; i < kRowSlots; i += BLOCK) sums[i] = 0;
+        __syncthreads();
+        const int power = ilogb(mass(sorted_value(0))) + 1 - 52;   // far below zero where it has no mass
+        for (int i = tid; i < n && power > -1200; i += BLOCK)
+            atomicAdd(&sums[(uint32_t)sm.sorted[i] / (uint32_t)(G * CHUNK)],
+                      (unsigned long long)(__builtin_ldexp(mass(sorted_value(i)), -power) + 0.5));
+        __syncthreads();
+        for (int i = tid; i < nslots; i += BLOCK)
+            sm.slot[i] = (CLEAR ? 0.0 : sm.slot[i]) + __builtin_ldexp((double)sums[i], power);
+        __syncthreads();
+    }
+
+    enum Search { kFound, kNone, kUnsettled };
+
+    // The cut of top_k, with top_p and min_p or without, or of min_p alone, where it keeps few
+    // elements, in one pass: a sample of the row gives a threshold with some more elements
+    // above it, the pass lists those, and the sorted list is cut.  Left unsettled where they
+    // are too many or too few.  slots: sm.slot holds what is kept.
+    __device__ __forceinline__ Search few(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
+                                          bool& slots, int& kept) {
+        constexpr float kRoom = 0.5f * (float)kSorted;
+        const float scale = (float)V / (float)kSample;
+        if (VEC == 1 || scale < 2.0f || (float)top_k > kRoom) return kUnsettled;
+        float v0[VEC], ref;
+        if (!take_sample(v0, ref)) return kUnsettled;
+        // min_p's cut lies at or above its threshold below the sample's maximum (less what its
+        // rounding may be); top_p after top_k needs all that top_k keeps
+        float tau = -INFINITY;
+        bool floored = false;
+        if (min_p > 0.0 && (top_k == 0 || top_p == 1.0)) {
+            tau = (float)((double)ref + T * log(min_p));
+            tau -= 1e-6f * (fabsf(ref) + fabsf(tau));
+            floored = true;
+        }
+        if (top_k > 0) {
+            const float mean = (float)top_k / scale;
+            const float t = threshold<false>(ref, mean + 4.0f * sqrtf(mean) + 3.0f, 0.0f, scale);
+            floored = floored && tau >= t;
+            tau = fmaxf(tau, t);
+        }
+        tau = uniform(tau);
+        if (!(tau > -INFINITY)) return kUnsettled;
+        int up = 0;   // elements above it, going by the sample
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) up += v0[e] >= tau;
+        double x = 0.0, y = 0.0;
+        int bad = 0;
+        if (threadIdx.x == 0) sm.nlist = 0;
+        sum2(x, y, up, bad);
+        if ((float)up * scale > kRoom) return kUnsettled;
+        sweep([&](const float(&v)[VEC], int j) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) bad |= !(v[e] < INFINITY);
+            gather(v, j, tau);
+        }, [](int) {});
+        if (__syncthreads_or(bad)) return kNone;
+        const int n = sm.nlist;
+        if (n > kSorted || n < 1 || (n < top_k && !floored)) return kUnsettled;
+        sort(n);
+        m = uniform(sorted_value(0));
+        md = uniform((double)m);
+        int keep = top_k > 0 ? min(n, top_k) : n;
+        if (top_k > 0 && top_p < 1.0) {
+            prefix(keep);
+            keep = min(keep, reach_running(keep, top_p * sm.running[keep - 1]) + 1);
+        }
+        if (min_p > 0.0) keep = above_floor(keep, min_floor(min_p));
+        cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
+        kept = keep;
+        slots = want_slots;
+        if (want_slots) add_to_slots<true>(keep);
+        return kFound;
+    }
+
+    // The cut of top_p alone, or of a top_k that keeps many elements: a histogram over linear
+    // bins below the maximum, of what a sample of the row cannot rule out, says which bin the
+    // cut falls into, and a second pass sums what lies above the bin and lists what is in it.
+    // Left unsettled where that is too much to be sorted, or the histogram's masses (in units
+    // of 2^-40) named a neighbour of the bin.  slots: sm.slot holds what is kept.
+    __device__ __forceinline__ Search search(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
+                                             bool& slots, int& kept) {
+        const int tid = threadIdx.x, lane = tid & 63;
+        const bool by_mass = top_k == 0;
+        if (!by_mass && top_p < 1.0) return kUnsettled;
+        float v0[VEC], ref, tau = -INFINITY;
+        if (!take_sample(v0, ref)) return kUnsettled;
+        if (by_mass) tau = threshold<true>(ref, 0.0f, 0.5f * (float)(1.0 - top_p), fmaxf(1.0f, (float)V / (float)kSample));
+        int bin = 0;
+        double before = 0.0, target = 0.0, sum = 0.0;
+        for (;;) {
+            md = uniform((double)ref);
+            __syncthreads();
+            for (int i = tid; i < kLinearBins / 2; i += BLOCK) reinterpret_cast<ulonglong2*>(sm.bins)[i] = make_ulonglong2(0, 0);
+            __syncthreads();
+            float mx = -INFINITY;
+            double a = 0.0, y = 0.0;
+            int n = 0, bad = 0;
+            auto add = [&](float l, uint64_t q) {
+                atomicAdd(reinterpret_cast<unsigned long long*>(&sm.bins[linear_bin(l, ref)]), (unsigned long long)q);
+            };
+            if (by_mass) {
+                sweep([&](const float(&v)[VEC], int) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        mx = fmaxf(mx, v[e]);
+                        bad |= !(v[e] < INFINITY);
+                        const double w = mass(v[e]);
+                        a += w;
+                        // the low bits of 2^52 + w 2^40 are the mass in its units
+                        if (v[e] >= tau && w > 0.0)
+                            add(v[e], __double_as_longlong(fma(w, 1.0 / kMassUnit, 0x1p52)) & 0xfffffffffffffull);
+                    }
+                }, [](int) {});
+            } else {
+                sweep([&](const float(&v)[VEC], int) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        mx = fmaxf(mx, v[e]);
+                        bad |= !(v[e] < INFINITY);
+                        n += v[e] > -INFINITY;
+                        if (linear_bin(v[e], ref) < kLinearBins - 1) add(v[e], 1);
+                    }
+                }, [](int) {});
+            }
+            int none = 0;
+            sum2(a, y, n, none);
+            m = block_max(mx);
+            if (__syncthreads_or(bad)) return kNone;
+            if (!by_mass && top_k >= n) {
+                cut = Cut{-INFINITY, -1};
+                slots = false;
+                return kFound;
+            }
+            // the units' 52 bits hold masses below 2^12
+            if (by_mass && ((double)m - md) * c > 10.0) {
+                ref = m;
+                continue;
+            }
+            sum = a;
+            target = by_mass ? top_p * sum : (double)top_k;
+            bin = reach(target, by_mass ? kMassUnit : 1.0, before);
+            if (bin >= 0) break;
+            if (!by_mass || !(tau > -INFINITY)) return kUnsettled;
+            tau = -INFINITY;   // the sample ruled out too much
+        }
+        __syncthreads();
+        if (tid == 0) sm.nlist = 0;
+        __syncthreads();
+        double a = 0.0, y = 0.0;
+        int above = 0, none = 0;
+        sweep([&](const float(&v)[VEC], int j) {
+            float in[VEC];
+            bool some = false;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const int b = linear_bin(v[e], ref);
+                in[e] = b == bin && v[e] > -INFINITY ? v[e] : -INFINITY;
+                some |= b < bin;
+            }
+            if (by_mass && __ballot(some)) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (linear_bin(v[e], ref) < bin) {
+                        ++above;
+                        a += mass(v[e]);
+                    }
+                }
+            }
+            gather(in, j, -FLT_MAX);
+        }, [&](int s) {
+            if (by_mass) {
+                const double t = wave_sum(a);
+                if (lane == 0) sm.slot[s] = t;
+                a = 0.0;
+            }
+        });
+        sum2(a, y, above, none);
+        const int n = sm.nlist;
+        if (n > kSorted || n < 1) return kUnsettled;
+        sort(n);
+        int keep;
+        if (by_mass) {
+            double total = 0.0;
+            for (int s = lane; s < nslots; s += 64) total += sm.slot[s];
+            total = wave_sum(total);
+            if (total >= target) return kUnsettled;
+            prefix(n);
+            keep = reach_running(n, target - total) + 1;
+        } else {
+            keep = top_k - (int)before;
+        }
+        if (keep < 1 || keep > n) return kUnsettled;
+        cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
+        kept = keep + above;
+        slots = want_slots && by_mass && !(min_p > 0.0 && min_floor(min_p) > cut.tau);
+        if (slots) add_to_slots<false>(keep);
+        return kFound;
+    }
+    __device__ __forceinline__ static int linear_bin(float l, float ref) {
+        return (int)fminf(fmaxf(fmaf(ref - l, kBinsPerUnit, kRefBin), 0.0f), (float)(kLinearBins - 1));
+    }
+
+    // The bin of sm.bins in which their running sum, in `unit`s, reaches `target` and what lies
+    // above it; -1 where it does not.
+    __device__ __forceinline__ int reach(double target, double unit, double& before) const {
+        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        constexpr int kLinearGroups = kLinearBins / 64;
+        static_assert(kLinearGroups == 64, "a lane a group");
+        for (int g = wid; g < kLinearGroups; g += kWaves) {
+            const double t = wave_sum((double)sm.bins[g * 64 + lane]);
+            if (lane == 0) sm.group_sum[g] = t * unit;
+        }
+        __syncthreads();
+        const double own = sm.group_sum[lane], incl = wave_incl_scan(own, lane);
+        const uint64_t hit = __ballot(own > 0.0 && incl >= target);
+        if (!hit) return -1;
+        const int g = __ffsll((unsigned long long)hit) - 1;
+        const double h = (double)sm.bins[g * 64 + lane] * unit;
+        const double inc = readlane_d(incl - own, g) + wave_incl_scan(h, lane);
+        const uint64_t over = __ballot(h > 0.0 && inc >= target), any = __ballot(h > 0.0);
+        const int L = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)any);
+        before = readlane_d(inc - h, L);
+        return g * 64 + L;
+    }
+
+    // The lowest value of the row's type with mass at least min_p: l >= m + T ln(min_p).
+    __device__ __forceinline__ float min_floor(double min_p) const {
+        const double t = (double)m + T * log(min_p);
+        float f = (float)t;
+        if ((double)f < t) f = value_of(key_of(f) + 1);
+        if (sizeof(In) == 2) {
+            const uint32_t b = __float_as_uint(f);
+            f = __uint_as_float((b & 0xffff0000u) + ((b & 0xffffu) && !(b >> 31) ? 0x10000u : 0u));
+        }
+        return f;
+    }
 
     // The slots' sums of what a cut keeps, from a table of the masses of the values above it,
     // and how many elements that is.  `partial`: the elements equal to the cut's value are
@@ -682,8 +1161,7 @@ struct Row {
         const int tid = threadIdx.x, lane = tid & 63;
         if constexpr (VEC == 8) {
             if (!(cut.tau > -INFINITY)) return false;
-            int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
-            if (end == kZeroBin && cut.tau > 0.0f) --end;   // the bin holds zeros, below the cut
+            const int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
             if (end == kLastBin || end - top + 2 > kValueBins / 2) return false;
             n = count_to(end) - (partial ? cut.all - cut.keep : 0);
             __syncthreads();
@@ -713,7 +1191,7 @@ struct Row {
                 }
             }, [&](int s) {
                 const double t = wave_sum(a);
-                const int nt = partial ? __reduce_add_sync(~0ull, ties) : 0;
+                const int nt = partial ? wave_sum_i(ties) : 0;
                 if (lane == 0) {
                     sm.slot[s] = t;
                     sm.ties[s] = nt;
@@ -735,15 +1213,15 @@ struct Row {
         const int n = sm.nlist;
         for (int s = tid; s < kRowSlots; s += BLOCK) sm.ties[s] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += BLOCK) atomicAdd(&sm.ties[sm.list[i] / (G * CHUNK)], 1);
+        for (int i = tid; i < n; i += BLOCK) atomicAdd(&sm.ties[sm.equal[i] / (G * CHUNK)], 1);
         __syncthreads();
         for (int i = tid; i < n; i += BLOCK) {
-            const int j = sm.list[i], s = j / (G * CHUNK);
+            const int j = sm.equal[i], s = j / (G * CHUNK);
             int before = 0;
             for (int q = 0; q < s; ++q) before += sm.ties[q];
             if (before + sm.ties[s] > keep) {
                 if (before < keep)
-                    for (int q = 0; q < n; ++q) before += sm.list[q] < j && sm.list[q] / (G * CHUNK) == s;
+                    for (int q = 0; q < n; ++q) before += sm.equal[q] < j && sm.equal[q] / (G * CHUNK) == s;
                 if (before >= keep) out[j] = 0xff80;
             }
         }
@@ -863,7 +1341,7 @@ __device__ __forceinline__ void store_vec(In* out, int j, int V, const float (&v
 
 // One workgroup a row: the cut, then the draws or the filtered row.
 template <typename In, int VEC, int UNR, int BLOCK, bool FILTER>
-__global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
+__global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) rs_sample_kernel(const SParams P) {
     __shared__ RowSmem sm;
     constexpr int kWaves = BLOCK / 64;
     constexpr bool kCounts = VEC == 8;   // bf16 rows: counts of values
@@ -875,7 +1353,7 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
     const float min_p = P.min_ps ? P.min_ps[entry] : P.min_p;
     const int top_k = P.top_ks ? P.top_ks[entry] : P.top_k;
     Row<In, VEC, UNR, BLOCK> row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
-                                 1.4426950408889634 / (double)T, sm};
+                                 uniform(1.4426950408889634 / (double)T), uniform((double)T), sm};
     In* out = FILTER ? reinterpret_cast<In*>(P.out) + r * P.out_stride : nullptr;
     int status = RS_SEQ_OK;
     if (!(T > 0.0f && T < INFINITY && top_k >= 0 && top_p > 0.0f && top_p <= 1.0f && min_p >= 0.0f && min_p <= 1.0f))
@@ -884,22 +1362,35 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
         const float u = tid < P.k ? P.u[r * P.k + tid] : 0.0f;
         if (__syncthreads_or(!(u >= 0.0f && u < 1.0f))) status = RS_SEQ_BAD_UNIFORM;
     }
-    // ---- the cut, and whether the counts of the row's values are at hand
+    // ---- the cut: from the counts of the row's values, which are at hand then; by the search
+    // over linear bins; or by the one over ranges of keys, which settles every row
     const bool filters = top_k > 0 || top_p < 1.0f || min_p > 0.0f;
     Ties ties{-INFINITY, 0, 0};
-    bool counts = false;
+    Cut cut{-INFINITY, -1};
+    bool counts = false, settled = false, slots = false;
     int kept = -1;
     if (status == RS_SEQ_OK && (filters || FILTER)) {
         bool bad = false;
+        auto found = Row<In, VEC, UNR, BLOCK>::kUnsettled;
+        if (top_k > 0 || (!FILTER && min_p > 0.0f && top_p == 1.0f))
+            found = row.few(top_k, (double)top_p, (double)min_p, !FILTER, cut, slots, kept);
         if constexpr (kCounts) {
-            counts = row.count_values(bad);
-            if (counts && filters) ties = row.cut_values(top_k, (double)top_p);
+            if (found == Row<In, VEC, UNR, BLOCK>::kUnsettled) {
+                counts = row.count_values(bad);
+                if (counts && filters) ties = row.cut_values(top_k, (double)top_p);
+            }
         }
-        if (!counts) {
+        if (bad || found == Row<In, VEC, UNR, BLOCK>::kNone) {
+            status = RS_SEQ_UNDERFLOW;
+        } else if (!counts) {
             int n = 0;
-            if (bad || !row.statistics(n)) {
-                status = RS_SEQ_UNDERFLOW;
-            } else {
+            const bool cuts = top_k > 0 || top_p < 1.0f;
+            if constexpr (!kCounts)
+                if (cuts && found == Row<In, VEC, UNR, BLOCK>::kUnsettled) found = row.search(top_k, (double)top_p, (double)min_p, !FILTER, cut, slots, kept);
+            if (found == Row<In, VEC, UNR, BLOCK>::kNone) status = RS_SEQ_UNDERFLOW;
+            settled = found == Row<In, VEC, UNR, BLOCK>::kFound;
+            if (!settled && status == RS_SEQ_OK && !row.statistics(n)) status = RS_SEQ_UNDERFLOW;
+            if (!settled && status == RS_SEQ_OK && cuts) {
                 const uint32_t lo = key_of(-INFINITY) + 1, hi = key_of(row.m);
                 double mass = 0.0;
                 const bool cuts_k = top_k > 0 && top_k < n;
@@ -908,29 +1399,22 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
                     if (!cuts_k) {
                         double a = 0.0, b = 0.0;
                         int x = 0, y = 0;
-                        row.sweep([&](const float(&v)[VEC], int) {
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) a += row.mass(v[e]);
-                        }, [](int) {});
+                        row.each([&](float l, int) { a += row.mass(l); });
                         row.sum2(a, b, x, y);
                         mass = a;
                     }
                     ties = row.template select<true>((double)top_p * mass, lo, hi, 0.0, false, mass);
                 }
             }
-        } else if (bad) {
-            status = RS_SEQ_UNDERFLOW;
         }
+        if (settled) ties = Ties{uniform(cut.tau), 0, 0};
+        else cut = Cut{ties.tau, ties.tau > -INFINITY ? INT_MAX : -1};
         if (status == RS_SEQ_OK && min_p > 0.0f) {
-            // w >= min_p where l >= m + T ln(min_p): the lowest value of the row's type that is
-            const double t = row.md + (double)T * log((double)min_p);
-            float f = (float)t;
-            if ((double)f < t) f = value_of(key_of(f) + 1);
-            if (kCounts) {
-                const uint32_t b = __float_as_uint(f);
-                f = __uint_as_float((b & 0xffff0000u) + ((b & 0xffffu) && !(b >> 31) ? 0x10000u : 0u));
+            const float f = row.min_floor((double)min_p);
+            if (f > ties.tau) {
+                ties = Ties{f, 0, 0};
+                cut = Cut{f, INT_MAX};
             }
-            if (f > ties.tau) ties = Ties{f, 0, 0};
         }
     }
     // ---- no filter: the slots' sums against a reference near the maximum
@@ -955,7 +1439,6 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
     }
     // ---- which of the elements equal to the cut's value are kept
     const bool partial = ties.keep < ties.all;
-    Cut cut{ties.tau, ties.tau > -INFINITY ? INT_MAX : -1};
     if (FILTER) {
         // many ties: their last index is found first; few: all are written as kept, and the
         // rest taken back
@@ -980,7 +1463,7 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
             if (listed && tie) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    if (v[e] == ties.tau) sm.list[atomicAdd(&sm.nlist, 1)] = j + e;
+                    if (v[e] == ties.tau) sm.equal[atomicAdd(&sm.nlist, 1)] = j + e;
             }
         }, [](int) {});
         double x = 0.0, y = 0.0;
@@ -990,7 +1473,7 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
             n -= ties.all - ties.keep;
         }
         kept = n;
-    } else if (filters) {
+    } else if (filters && !slots) {
         int n = 0, none = 0;
         if (counts && row.table_masses(ties, partial, n)) {
             if (partial) cut.limit = row.tie_place(ties.tau, ties.keep);
@@ -1005,6 +1488,7 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
             row.sweep([&](const float(&v)[VEC], int j) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
+                    if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                     if (cut.keeps(v[e], j + e)) {
                         a += row.mass(v[e]);
                         ++n;
@@ -1019,7 +1503,7 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
             row.sum2(x, y, n, none);
             kept = n;
         }
-    } else {
+    } else if (!filters) {
         kept = row.finite;
     }
     if (tid == 0) {
@@ -1040,64 +1524,111 @@ __global__ void __launch_bounds__(BLOCK) rs_sample_kernel(const SParams P) {
     }
 }
 
-// One workgroup a row: the sum of the row's masses against its maximum, and for every token
-// how many elements come before it in the order.
+// One workgroup a row, one pass: the sum of the row's masses against the highest element of its
+// sample, in 32-bit exponentials (a log-probability is no border: its error is that of the
+// sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
+// vectors with an element that is not below every token take the count, a step a token.
+// Where the sum overflows or the sample is masked, a second pass against the maximum.
 template <typename In, int VEC, int UNR, int BLOCK>
 __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
-    __shared__ RowSmem sm;
-    const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63;
-    constexpr int kWaves = BLOCK / 64;
+    __shared__ ReduceSmem sm;
+    __shared__ float token_logit[kMaxCand];
+    __shared__ int32_t token_id[kMaxCand], token_rank[kMaxCand];
+    __shared__ double slot[kRowSlots];
+    const int tid = threadIdx.x, lane = tid & 63;
+    using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
     const int64_t r = blockIdx.x;
     const float T = P.temperatures ? P.temperatures[r / P.rows_per_entry] : P.temperature;
-    Row<In, VEC, UNR, BLOCK> row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
-                                 1.4426950408889634 / (double)T, sm};
-    int status = RS_SEQ_OK, n = 0;
+    using RowT = Row<In, VEC, UNR, BLOCK, ReduceSmem>;
+    RowT row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
+                                 uniform(1.4426950408889634 / (double)T), uniform((double)T), sm};
+    int status = RS_SEQ_OK;
     if (!(T > 0.0f && T < INFINITY)) status = RS_SEQ_BAD_PARAM;
     const int x = tid < P.k ? P.tokens[r * P.k + tid] : -1;
     if (__syncthreads_or(x < -1 || x >= P.V) && status == RS_SEQ_OK) status = RS_SEQ_BAD_TOKEN;
-    if (status == RS_SEQ_OK && !row.statistics(n)) status = RS_SEQ_UNDERFLOW;
-    if (tid == 0 && P.status) P.status[r] = status;
-    if (status != RS_SEQ_OK) {
+    double total = 0.0;
+    if (status == RS_SEQ_OK) {
         if (tid < P.k) {
-            if (P.logprob) P.logprob[r * P.k + tid] = NAN;
-            if (P.rank) P.rank[r * P.k + tid] = -1;
+            float l[1] = {INFINITY};
+            if (x >= 0) load_vec<E, 1>(reinterpret_cast<const E*>(row.row), x, P.V, l);
+            token_logit[tid] = l[0];
+            token_id[tid] = x;
+            token_rank[tid] = 0;
         }
-        return;
-    }
-    double a = 0.0, b = 0.0;
-    int p = 0, q = 0;
-    row.sweep([&](const float(&v)[VEC], int) {
+        __syncthreads();
+        float lowest = INFINITY;
+        for (int i = 0; i < P.k; ++i) lowest = fminf(lowest, token_logit[i]);
+        lowest = uniform(P.rank ? lowest : INFINITY);
+        float v0[VEC], mx = -INFINITY;
+        row.load_sample(v0);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) a += row.mass(v[e]);
-    }, [](int) {});
-    row.sum2(a, b, p, q);
-    for (int i = 0; i < P.k; ++i) {
-        const int t = P.tokens[r * P.k + i];
-        float l = 0.0f;
-        int before = 0;
-        if (t >= 0) {
-            float v[1];
-            load_vec<std::conditional_t<sizeof(In) == 2, uint16_t, float>, 1>(
-                reinterpret_cast<const std::conditional_t<sizeof(In) == 2, uint16_t, float>*>(row.row), t, P.V, v);
-            l = v[0];
-            if (P.rank) {
-                row.sweep([&](const float(&w)[VEC], int j) {
+        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v0[e]);
+        float ref = row.block_max(mx);
+        if (!(ref > -INFINITY && ref < INFINITY)) ref = 0.0f;
+        // c in two parts, both above zero: a -inf element's exponent is -inf, not a NaN
+        float ch = (float)fmin(row.c, (double)FLT_MAX);
+        if ((double)ch >= row.c) ch = __uint_as_float(__float_as_uint(ch) - 1);
+        const float cl = (float)fmin(row.c - (double)ch, (double)FLT_MAX);
+        int before = 0;   // lane i: token i's, of the wave's elements
+        for (int attempt = 0;; ++attempt) {
+            double a = 0.0;
+            row.sweep([&](const float(&v)[VEC], int j) {
+                float w[VEC];
+                bool some = false;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) before += w[e] > l || (w[e] == l && j + e < t);
-                }, [](int) {});
-                double z = 0.0, z2 = 0.0;
-                int none = 0;
-                row.sum2(z, z2, before, none);
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = v[e] - ref;
+                    w[e] = exp2_fast(fmaf(d, cl, d * ch));
+                    some |= v[e] >= lowest;
+                }
+#pragma unroll
+                for (int h = VEC / 2; h; h >>= 1)
+#pragma unroll
+                    for (int e = 0; e < h; ++e) w[e] += w[e + h];
+                a += (double)w[0];
+                if (attempt == 0 && __ballot(some)) {
+                    for (int i = 0; i < P.k; ++i) {
+                        const float l = token_logit[i];
+                        const int id = token_id[i];
+                        int n = 0;
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            n += __popcll(__ballot(v[e] > l || (v[e] == l && j + e < id)));
+                        if (lane == i) before += n;
+                    }
+                }
+            }, [&](int s) {
+                const double t = wave_sum(a);
+                if (lane == 0) slot[s] = t;
+                a = 0.0;
+            });
+            __syncthreads();
+            total = 0.0;
+            for (int s = lane; s < P.nslots; s += 64) total += slot[s];
+            total = uniform(wave_sum(total));
+            row.md = (double)ref;
+            if (total >= kLowSum && total < INFINITY) break;
+            int n = 0;
+            if (attempt == 1 || !row.statistics(n)) {
+                status = RS_SEQ_UNDERFLOW;
+                break;
             }
+            ref = row.m;
         }
-        if (tid == 0) {
-            if (P.logprob) P.logprob[r * P.k + i] = t < 0 ? 0.0f : (float)(((double)l - row.md) / (double)T - log(a));
-            if (P.rank) P.rank[r * P.k + i] = t < 0 ? 0 : before + 1;
-        }
+        if (before) atomicAdd(&token_rank[lane], before);
+        __syncthreads();
     }
-    (void)wid;
-    (void)lane;
-    (void)kWaves;
+    if (tid == 0 && P.status) P.status[r] = status;
+    if (tid < P.k) {
+        float lp = NAN;
+        int rank = -1;
+        if (status == RS_SEQ_OK) {
+            lp = x < 0 ? 0.0f : (float)(((double)token_logit[tid] - row.md) / row.T - log(total));
+            rank = x < 0 ? 0 : token_rank[tid] + 1;
+        }
+        P.logprob[r * P.k + tid] = lp;
+        if (P.rank) P.rank[r * P.k + tid] = rank;
+    }
 }
 
 // ------------------------------------------------------------------- host ----
@@ -1138,21 +1669,30 @@ RowLoads strided_loads(const void* p, int64_t stride, int32_t V, int dtype) {
 }
 
 // The row of V elements in slots of G chunks.
-template <int VEC>
+template <int VEC, int UNR>
 void set_slots(SParams& P) {
-    constexpr int64_t CHUNK = 64 * VEC * kUnrRow;
+    constexpr int64_t CHUNK = 64 * VEC * UNR;
     const int64_t nch = ((int64_t)P.V + CHUNK - 1) / CHUNK;
     P.G = (int32_t)((nch + kRowSlots - 1) / kRowSlots);
     P.nslots = (int32_t)((nch + P.G - 1) / P.G);
 }
 
-// f(element type, elements a load) for the kernels' instance.
+// f(element type, elements a load, loads a chunk) for the kernels' instance.
 template <typename F>
 auto with_rows(int dtype, RowLoads loads, F&& f) {
-    return with_layout(dtype, loads, [&](auto in, auto vec, auto) { return f(in, vec); });
+    return with_layout(dtype, loads, [&](auto in, auto vec, auto) {
+        return f(in, vec, std::integral_constant<int, vec() == 4 ? kUnrRow32 : kUnrRow16>());
+    });
 }
 
-constexpr int kRowBlock = 512;
+// Threads a row: 16 waves where every row has a CU to itself, two rows of 8 waves a CU where
+// there are more.
+constexpr int kCus = 256;
+template <typename F>
+auto with_block(int32_t R, F&& f) {
+    using std::integral_constant;
+    return R <= kCus ? f(integral_constant<int, 1024>()) : f(integral_constant<int, 512>());
+}
 
 }  // namespace
 
@@ -1175,11 +1715,13 @@ rs_status resispec_sample(const void* logits, int64_t row_stride, const float* u
     P.kept = out_kept;
     P.status = out_status;
     const hipError_t e = with_rows(
-        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec) {
-            set_slots<vec()>(P);
-            hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), kUnrRow, kRowBlock, false>), dim3((unsigned)R),
-                               dim3(kRowBlock), 0, (hipStream_t)stream, P);
-            return hipGetLastError();
+        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec, auto unr) {
+            set_slots<vec(), unr()>(P);
+            return with_block(R, [&](auto block) {
+                hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), unr(), block(), false>), dim3((unsigned)R), dim3(block()),
+                                   0, (hipStream_t)stream, P);
+                return hipGetLastError();
+            });
         });
     return e == hipSuccess ? RS_OK : RS_ERR_HIP;
 }
@@ -1200,11 +1742,13 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
     P.status = out_status;
     const RowLoads in = strided_loads(logits, row_stride, V, filter->logits_dtype);
     const RowLoads to = strided_loads(out, out_row_stride, V, filter->logits_dtype);
-    const hipError_t e = with_rows(filter->logits_dtype, in > to ? in : to, [&](auto in, auto vec) {
-        set_slots<vec()>(P);
-        hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), kUnrRow, kRowBlock, true>), dim3((unsigned)R),
-                           dim3(kRowBlock), 0, (hipStream_t)stream, P);
-        return hipGetLastError();
+    const hipError_t e = with_rows(filter->logits_dtype, in > to ? in : to, [&](auto in, auto vec, auto unr) {
+        set_slots<vec(), unr()>(P);
+        return with_block(R, [&](auto block) {
+            hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), unr(), block(), true>), dim3((unsigned)R),
+                               dim3(block()), 0, (hipStream_t)stream, P);
+            return hipGetLastError();
+        });
     });
     return e == hipSuccess ? RS_OK : RS_ERR_HIP;
 }
@@ -1228,11 +1772,13 @@ rs_status resispec_token_logprobs(const void* logits, int64_t row_stride, const 
     P.rank = out_rank;
     P.status = out_status;
     const hipError_t e = with_rows(
-        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec) {
-            set_slots<vec()>(P);
-            hipLaunchKernelGGL((rs_logprob_kernel<decltype(in), vec(), kUnrRow, kRowBlock>), dim3((unsigned)R),
-                               dim3(kRowBlock), 0, (hipStream_t)stream, P);
-            return hipGetLastError();
+        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec, auto unr) {
+            set_slots<vec(), unr()>(P);
+            return with_block(R, [&](auto block) {
+                hipLaunchKernelGGL((rs_logprob_kernel<decltype(in), vec(), unr(), block()>), dim3((unsigned)R), dim3(block()),
+                                   0, (hipStream_t)stream, P);
+                return hipGetLastError();
+            });
         });
     return e == hipSuccess ? RS_OK : RS_ERR_HIP;
 }
