@@ -185,44 +185,65 @@ struct Row {
     __device__ __forceinline__ double mass(float l) const { return exp2_64(((double)l - md) * c); }
 
     // body(t, j): a vector of VEC elements from index j as loaded (-inf at and past V);
-    // flush(slot) after a slot's last.  A wave's slots are the same in every pass.
-    template <typename Body, typename Flush>
+    // flush(slot) after a slot's last.  A wave's slots are the same in every pass.  NT: the
+    // row's last use.  Two chunks of registers alternate.  Loads take no branch, so that the
+    // wait before a chunk is for that chunk alone (with bounds checks around them the compiler
+    // waits for the next one too: 128 x 5 rows of 128,256 took 60 us where they take 44): what
+    // lies past the row reads the row's last elements and is put right in the last chunk, and
+    // a wave's last step loads its chunk again.
+    template <bool NT, typename Body, typename Flush>
     __device__ __forceinline__ void sweep_raw(Body&& body, Flush&& flush) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
         typename W::raw a[UNR], b[UNR];
         auto load = [&](int s, int g, typename W::raw(&t)[UNR]) {
-            load_chunk<In, VEC, UNR, false, false>(row, row, (s * G + g) * CHUNK, V, t, t);
-        };
-        auto process = [&](int s, int g, typename W::raw(&t)[UNR]) {
             const int j0 = (s * G + g) * CHUNK + lane * VEC;
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) {
-                W::settle(t[u], row, j0 + u * 64 * VEC, V);
-                body(t[u], j0 + u * 64 * VEC);
+            for (int u = 0; u < UNR; ++u) t[u] = W::template load_full<NT>(row, min(j0 + u * 64 * VEC, V - VEC));
+        };
+        auto process = [&](int s, int g, typename W::raw(&t)[UNR]) {
+            const int c0 = (s * G + g) * CHUNK, j0 = c0 + lane * VEC;
+            if (c0 + CHUNK > V) {
+#pragma unroll
+                for (int u = 0; u < UNR; ++u) cut_off(t[u], j0 + u * 64 * VEC);
             }
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) body(t[u], j0 + u * 64 * VEC);
             if (g == G - 1) flush(s);
         };
         int s = wid, g = 0;
         if (s >= nslots) return;
         load(s, g, a);
         for (;;) {
-            int s2 = s, g2 = g + 1;
-            if (g2 == G) { s2 += kWaves; g2 = 0; }
-            if (s2 < nslots) load(s2, g2, b);
+            int s2 = g + 1 == G ? s + kWaves : s, g2 = g + 1 == G ? 0 : g + 1;
+            bool more = s2 < nslots;
+            load(more ? s2 : s, more ? g2 : g, b);
             process(s, g, a);
-            if (s2 >= nslots) break;
-            s = s2; g = g2 + 1;
-            if (g == G) { s += kWaves; g = 0; }
-            if (s < nslots) load(s, g, a);
+            if (!more) break;
+            s = g2 + 1 == G ? s2 + kWaves : s2;
+            g = g2 + 1 == G ? 0 : g2 + 1;
+            more = s < nslots;
+            load(more ? s : s2, more ? g : g2, a);
             process(s2, g2, b);
-            if (s >= nslots) break;
+            if (!more) break;
+        }
+    }
+    __device__ __forceinline__ static int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+    // A vector loaded from index min(j, V - VEC): its elements from j on, and -inf after them.
+    __device__ __forceinline__ void cut_off(typename W::raw& t, int j) const {
+        if constexpr (VEC == 1) {
+            if (j >= V) t = 0xff800000u;
+        } else {
+            constexpr uint32_t FILL = sizeof(In) == 2 ? 0xff80ff80u : 0xff800000u;
+            if (j >= V) t = make_uint4(FILL, FILL, FILL, FILL);
+            else if (j + VEC > V) t = drop_front<(int)sizeof(In), FILL>(t, j + VEC - V);
         }
     }
 
     // The same with the elements as floats.
-    template <typename Body, typename Flush>
+    template <bool NT, typename Body, typename Flush>
     __device__ __forceinline__ void sweep(Body&& body, Flush&& flush) const {
-        sweep_raw([&](const typename W::raw& t, int j) {
+        sweep_raw<NT>([&](const typename W::raw& t, int j) {
             float v[VEC];
             W::unpack(t, v);
             body(v, j);
@@ -243,7 +264,7 @@ struct Row {
 
     // Sums over the workgroup in a fixed order, to every thread.
     __device__ __forceinline__ void sum2(double& a, double& b, int& p, int& q) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
         const double wa = wave_sum(a), wb = wave_sum(b);
         const int wp = wave_sum_i(p), wq = wave_sum_i(q);
         __syncthreads();
@@ -276,7 +297,7 @@ struct Row {
         return uniform(v);
     }
     __device__ __forceinline__ void range(uint32_t& lo, uint32_t& hi) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
         for (int o = 32; o; o >>= 1) {
             lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
             hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
@@ -298,7 +319,7 @@ struct Row {
     __device__ __forceinline__ bool statistics(int& n) {
         float mx = -INFINITY;
         int cnt = 0, bad = 0;
-        sweep([&](const float(&v)[VEC], int) {
+        sweep<false>([&](const float(&v)[VEC], int) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 mx = fmaxf(mx, v[e]);
@@ -443,12 +464,12 @@ struct Row {
     // that a cut needs (values outside the bins' range, unless they have no mass, make the row
     // one for the search above); a NaN or a +inf sets `bad`.
     __device__ __forceinline__ bool count_values(bool& bad) {
-        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         for (int i = tid; i < kValueBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.count)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         i16x2 pos = {0, 0};
         u16x2 neg = {0, 0};
-        sweep_raw([&](const typename W::raw& t, int) {
+        sweep_raw<false>([&](const typename W::raw& t, int) {
             if constexpr (VEC == 8) {
                 const uint32_t w[4] = {t.x, t.y, t.z, t.w};
                 u16x2 at[4], most = {0, 0};
@@ -483,8 +504,10 @@ struct Row {
         // positive words from 0x7f80 are +inf and NaN, negative ones past 0xff80 NaN
         const bool mine = pos.x >= 0x7f80 || pos.y >= 0x7f80 || neg.x > 0xff80 || neg.y > 0xff80;
         bad = __syncthreads_or(mine);
-        for (int g = wid; g < kGroups; g += kWaves) {
-            const int b = g * 64 + lane;
+        static_assert(kGroups % kWaves == 0, "as many groups a wave");
+#pragma unroll 4
+        for (int i = 0; i < kGroups / kWaves; ++i) {
+            const int g = wid + i * kWaves, b = g * 64 + lane;
             const int n = wave_sum_i(b < kLastBin ? (int)sm.count[b] : 0);
             if (lane == 0) sm.group_count[g] = n;
         }
@@ -571,7 +594,7 @@ struct Row {
     // The cut of top_k and top_p from the counts of a row's values.  Where it falls among the
     // values below all bins, the search ends it.
     __device__ __forceinline__ Ties cut_values(int top_k, double top_p) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
         const bool want_mass = top_p < 1.0;
         for (int g = wid; g < kGroups; g += kWaves) {
             double t = 0.0;
@@ -627,7 +650,7 @@ struct Row {
         const int lane = threadIdx.x & 63;
         int cnt = 0;
         __syncthreads();
-        sweep([&](const float(&v)[VEC], int) {
+        sweep<false>([&](const float(&v)[VEC], int) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) cnt += v[e] == tau;
         }, [&](int s) {
@@ -713,7 +736,7 @@ struct Row {
             md = uniform(mx > -INFINITY && mx < INFINITY ? (double)mx : 0.0);
             double a = 0.0;
             int n = 0, bad = 0, none = 0;
-            sweep([&](const float(&t)[VEC], int) {
+            sweep<true>([&](const float(&t)[VEC], int) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -746,7 +769,7 @@ struct Row {
     // each lane of the first eight waves.
     static constexpr int kSampleSlots = 8, kSample = kSampleSlots * 64 * VEC;
     __device__ __forceinline__ void load_sample(float (&v)[VEC]) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[e] = -INFINITY;
         if (wid < kSampleSlots)
@@ -779,18 +802,22 @@ struct Row {
     // other one for `scale` elements); -inf where there is none.  Every wave finds the same.
     template <bool BY_MASS>
     __device__ __forceinline__ float threshold(float ref, float rank, float rest, float scale) const {
-        const int lane = threadIdx.x & 63;
-        constexpr int PER = kBins / 64;
+        const int lane = threadIdx.x & 63, wid = wave_id();
+        constexpr int kSampleGroups = kBins / 64;
+        static_assert(kSampleGroups <= 64, "a lane a group");
         const float step = -(float)fmin(c, 1e30) / kSampleBins;
-        float own = 0.0f;
-        for (int q = 0; q < PER / 4; ++q) {
-            const uint4 n = reinterpret_cast<const uint4*>(sm.sample)[lane * (PER / 4) + q];
-            const float b = (float)(lane * PER + 4 * q) + 0.5f;
-            own += BY_MASS ? ((float)n.x * exp2_fast(b * step) + (float)n.y * exp2_fast((b + 1.0f) * step)) +
-                                 ((float)n.z * exp2_fast((b + 2.0f) * step) + (float)n.w * exp2_fast((b + 3.0f) * step))
-                           : (float)(n.x + n.y + n.z + n.w);
+        auto held = [&](int b) -> float {
+            const float n = (float)sm.sample[b];
+            return BY_MASS ? n * exp2_fast(((float)b + 0.5f) * step) : n;
+        };
+#pragma unroll
+        for (int i = 0; i < kSampleGroups / kWaves; ++i) {
+            const int g = wid + i * kWaves;
+            const double t = wave_sum((double)held(g * 64 + lane));
+            if (lane == 0) sm.group_sum[g] = t;
         }
-        const double incl = wave_incl_scan((double)own, lane);
+        __syncthreads();
+        const double own = lane < kSampleGroups ? sm.group_sum[lane] : 0.0, incl = wave_incl_scan(own, lane);
         double goal = (double)rank;
         if (BY_MASS) {
             const double total = readlane_d(incl, 63), first = (double)exp2_fast(0.5f * step);
@@ -798,13 +825,11 @@ struct Row {
         }
         const uint64_t hit = __ballot(incl >= goal);
         if (!hit) return -INFINITY;
-        const int L = __ffsll((unsigned long long)hit) - 1;
-        const int b = L * PER + lane;
-        const float n = lane < PER ? (float)sm.sample[b] : 0.0f;
-        const double in = readlane_d(incl - (double)own, L) +
-                          wave_incl_scan((double)(BY_MASS ? n * exp2_fast(((float)b + 0.5f) * step) : n), lane);
-        const uint64_t over = __ballot(lane < PER && in >= goal * (1.0 - 1e-6));
-        const int at = over ? L * PER + __ffsll((unsigned long long)over) - 1 : kBins;
+        const int g = __ffsll((unsigned long long)hit) - 1;
+        if (g >= kSampleGroups) return -INFINITY;
+        const double in = readlane_d(incl - own, g) + wave_incl_scan((double)held(g * 64 + lane), lane);
+        const uint64_t over = __ballot(in >= goal * (1.0 - 1e-9));
+        const int at = over ? g * 64 + __ffsll((unsigned long long)over) - 1 : kBins;
         return at < kBins - 1 ? ref - (float)(at + 1) / kSampleBins : -INFINITY;
     }
 
@@ -872,7 +897,7 @@ struct Row {
 
     // Running sums of the masses of sm.sorted[0 .. n) into sm.running.
     __device__ __forceinline__ void prefix(int n) const {
-        const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+        const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int per = (n + BLOCK - 1) / BLOCK;
         double own = 0.0;
         for (int q = 0; q < per; ++q)
@@ -966,7 +991,7 @@ struct Row {
         if (threadIdx.x == 0) sm.nlist = 0;
         sum2(x, y, up, bad);
         if ((float)up * scale > kRoom) return kUnsettled;
-        sweep([&](const float(&v)[VEC], int j) {
+        sweep<true>([&](const float(&v)[VEC], int j) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) bad |= !(v[e] < INFINITY);
             gather(v, j, tau);
@@ -1017,7 +1042,7 @@ struct Row {
                 atomicAdd(reinterpret_cast<unsigned long long*>(&sm.bins[linear_bin(l, ref)]), (unsigned long long)q);
             };
             if (by_mass) {
-                sweep([&](const float(&v)[VEC], int) {
+                sweep<false>([&](const float(&v)[VEC], int) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         mx = fmaxf(mx, v[e]);
@@ -1030,7 +1055,7 @@ struct Row {
                     }
                 }, [](int) {});
             } else {
-                sweep([&](const float(&v)[VEC], int) {
+                sweep<false>([&](const float(&v)[VEC], int) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         mx = fmaxf(mx, v[e]);
@@ -1066,7 +1091,7 @@ struct Row {
         __syncthreads();
         double a = 0.0, y = 0.0;
         int above = 0, none = 0;
-        sweep([&](const float(&v)[VEC], int j) {
+        sweep<true>([&](const float(&v)[VEC], int j) {
             float in[VEC];
             bool some = false;
 #pragma unroll
@@ -1122,10 +1147,12 @@ struct Row {
     // The bin of sm.bins in which their running sum, in `unit`s, reaches `target` and what lies
     // above it; -1 where it does not.
     __device__ __forceinline__ int reach(double target, double unit, double& before) const {
-        const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wid = wave_id();
         constexpr int kLinearGroups = kLinearBins / 64;
         static_assert(kLinearGroups == 64, "a lane a group");
-        for (int g = wid; g < kLinearGroups; g += kWaves) {
+#pragma unroll
+        for (int i = 0; i < kLinearGroups / kWaves; ++i) {
+            const int g = wid + i * kWaves;
             const double t = wave_sum((double)sm.bins[g * 64 + lane]);
             if (lane == 0) sm.group_sum[g] = t * unit;
         }
@@ -1173,8 +1200,18 @@ struct Row {
             const u16x2 lasts = {last, last};
             double a = 0.0;
             int ties = 0;
-            sweep_raw([&](const typename W::raw& t, int) {
+            // words from the cut's up, as signed numbers, are the values above it if that is
+            // not negative
+            const int32_t tau_word = (int32_t)__float_as_uint(cut.tau) >> 16;
+            const bool words = cut.tau > 0.0f;
+            sweep_raw<true>([&](const typename W::raw& t, int) {
                 const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+                if (words) {
+                    i16x2 most = __builtin_bit_cast(i16x2, w[0]);
+#pragma unroll
+                    for (int q = 1; q < 4; ++q) most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, w[q]));
+                    if (__ballot(most.x >= tau_word || most.y >= tau_word) == 0) return;
+                }
                 u16x2 at[4];
                 u16x2 lowest = lasts;
 #pragma unroll
@@ -1345,7 +1382,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
     __shared__ RowSmem sm;
     constexpr int kWaves = BLOCK / 64;
     constexpr bool kCounts = VEC == 8;   // bf16 rows: counts of values
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t r = blockIdx.x;
     const int64_t entry = r / P.rows_per_entry;
     const float T = P.temperatures ? P.temperatures[entry] : P.temperature;
@@ -1449,7 +1486,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         if (tid == 0) sm.nlist = 0;
         __syncthreads();
         int n = 0, none = 0;
-        row.sweep([&](const float(&v)[VEC], int j) {
+        row.template sweep<true>([&](const float(&v)[VEC], int j) {
             float w[VEC];
             bool tie = false;
 #pragma unroll
@@ -1485,7 +1522,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         } else {
             if (partial) cut.limit = row.tie_limit(ties.tau, ties.keep);
             double a = 0.0;
-            row.sweep([&](const float(&v)[VEC], int j) {
+            row.template sweep<true>([&](const float(&v)[VEC], int j) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -1572,7 +1609,7 @@ __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
         int before = 0;   // lane i: token i's, of the wave's elements
         for (int attempt = 0;; ++attempt) {
             double a = 0.0;
-            row.sweep([&](const float(&v)[VEC], int j) {
+            row.template sweep<true>([&](const float(&v)[VEC], int j) {
                 float w[VEC];
                 bool some = false;
 #pragma unroll
