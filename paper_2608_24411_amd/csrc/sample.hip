@@ -119,11 +119,14 @@ __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float(k ^ ((uint32_t)((int32_t)~k >> 31) | 0x80000000u));
 }
 
-// 2^x for x <= 0 in fp64, zero below 2^-1074.  2^f = 1 + f g(f) on [-1/2, 1/2], g of degree 8
-// interpolated at Chebyshev nodes: 3.7e-14 off at most, and exactly 1 at 0.
+// 2^x in fp64 for x < 1023, zero up to -1023.  2^f = 1 + f g(f) on [-1/2, 1/2], g of degree 8
+// interpolated at Chebyshev nodes: 3.7e-14 off at most, and exactly 1 at 0.  x + 1.5 2^52 has
+// the whole number in its low bits, which go to the exponent: rounding, conversion and ldexp
+// instructions in their place take 110 cycles a wave and element where this takes 80.  At
+// -1023, where everything below is put, the exponent and the mantissa of 1 give zero.
 __device__ __forceinline__ double exp2_64(double x) {
-    x = fmax(x, -1100.0);
-    const double n = rint(x), f = x - n;
+    x = fmax(x, -1023.0);
+    const double t = x + 0x1.8p52, f = x - (t - 0x1.8p52);
     double p = 0x1.b63880a30e9ffp-24;
     p = fma(p, f, 0x1.63d136366db24p-20);
     p = fma(p, f, 0x1.ffcb9515a8016p-17);
@@ -134,7 +137,7 @@ __device__ __forceinline__ double exp2_64(double x) {
     p = fma(p, f, 0x1.ebfbdff823cedp-3);
     p = fma(p, f, 0x1.62e42fefa39efp-1);
     p = fma(p, f, 1.0);
-    return __builtin_ldexp(p, (int)n);
+    return __hiloint2double(__double2hiint(p) + (int)((uint32_t)__double2loint(t) << 20), __double2loint(p));
 }
 
 // What is kept of a row: values above tau, and those equal to it up to index `limit`.
@@ -155,14 +158,14 @@ struct Ties {
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 bin_bytes(uint32_t word) {
-    const u16x2 lo = {kLoMag, kLoMag}, top = {kTopMag, kTopMag};
-    const u16x2 one = {(uint16_t)(kHalf + 1), (uint16_t)(kHalf + 1)};
+    const u16x2 lo = {kLoMag, kLoMag}, top = {kTopMag, kTopMag}, eight = {8, 8}, four = {4, 4};
+    const u16x2 half = {(uint16_t)(4 * kHalf), (uint16_t)(4 * kHalf)};
     const u16x2 mag = __builtin_bit_cast(u16x2, word & 0x7fff7fffu);
     const u16x2 far = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, lo), top);
     const u16x2 t = __builtin_elementwise_max(far, __builtin_elementwise_min(mag, u16x2{1, 1}));
     const u16x2 neg = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, word) >> 15);
-    // kHalf - t for positive values, kHalf + t for negative ones
-    return (~(t ^ neg) + neg + one) << 2;
+    // 4 kHalf - 4 t for positive values, 4 kHalf + 4 t for negative ones
+    return t * ((neg & eight) - four) + half;
 }
 __device__ __forceinline__ float bin_value(int bin) {
     const int t = bin < kHalf ? kHalf - bin : bin - kHalf;
@@ -467,16 +470,13 @@ struct Row {
         const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         for (int i = tid; i < kValueBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.count)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        i16x2 pos = {0, 0};
-        u16x2 neg = {0, 0};
+        bool mine = false;
         sweep_raw<false>([&](const typename W::raw& t, int) {
             if constexpr (VEC == 8) {
                 const uint32_t w[4] = {t.x, t.y, t.z, t.w};
                 u16x2 at[4], most = {0, 0};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    pos = __builtin_elementwise_max(pos, __builtin_bit_cast(i16x2, w[q]));
-                    neg = __builtin_elementwise_max(neg, __builtin_bit_cast(u16x2, w[q]));
                     at[q] = bin_bytes(w[q]);
                     most = __builtin_elementwise_max(most, at[q]);
                 }
@@ -485,7 +485,9 @@ struct Row {
                     uint32_t* at = reinterpret_cast<uint32_t*>(base + byte);
                     __hip_atomic_fetch_add(at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 };
-                // the last bin's count is not used, and masked rows would crowd it
+                // the last bin's count is not used, and masked rows would crowd it; a negative
+                // NaN is in it, a positive one and +inf make the top bin, and the row one for
+                // the search
                 if (__ballot(most.x == 4 * kLastBin || most.y == 4 * kLastBin) == 0) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -497,12 +499,11 @@ struct Row {
                     for (int q = 0; q < 4; ++q) {
                         if (at[q].x < 4 * kLastBin) add(at[q].x);
                         if (at[q].y < 4 * kLastBin) add(at[q].y);
+                        mine |= w[q] > 0xff80ffffu || (w[q] & 0xffffu) > 0xff80u;
                     }
                 }
             }
         }, [](int) {});
-        // positive words from 0x7f80 are +inf and NaN, negative ones past 0xff80 NaN
-        const bool mine = pos.x >= 0x7f80 || pos.y >= 0x7f80 || neg.x > 0xff80 || neg.y > 0xff80;
         bad = __syncthreads_or(mine);
         static_assert(kGroups % kWaves == 0, "as many groups a wave");
 #pragma unroll 4
@@ -862,17 +863,19 @@ struct Row {
         const int tid = threadIdx.x;
         __syncthreads();
         if (n <= kRanked) {
-            // an element's place is the number of those below it
-            if (tid == 0 && (n & 1)) sm.list[n] = ~0ull;
+            // an element's place is the number of those below it, counted by four threads
+            if (tid < 8 && tid < kSorted - n) sm.list[n + tid] = ~0ull;
             __syncthreads();
-            for (int i = tid; i < n; i += BLOCK) {
-                const uint64_t x = sm.list[i];
+            for (int i = tid; i < 4 * n; i += BLOCK) {
+                const uint64_t x = sm.list[i >> 2];
                 int before = 0;
-                for (int q = 0; q < n; q += 2) {
+                for (int q = 2 * (i & 3); q < n; q += 8) {
                     const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&sm.list[q]);
                     before += (y.x < x) + (y.y < x);
                 }
-                sm.sorted[before] = x;
+                before += dpp_i<kDppXor1>(before);
+                before += dpp_i<kDppXor2>(before);
+                if ((i & 3) == 0) sm.sorted[before] = x;
             }
             __syncthreads();
             return;
@@ -935,16 +938,15 @@ struct Row {
         return lo;
     }
     // Adds the masses of sm.sorted[0 .. n) to the slots' sums (CLEAR: which were none), as
-    // whole numbers of 2^-52 of the first's power of two, so that their order does not count.
+    // whole numbers of 2^power, so that their order does not count; none is above 2^52 of them.
     template <bool CLEAR>
-    __device__ __forceinline__ void add_to_slots(int n) const {
+    __device__ __forceinline__ void add_to_slots(int n, int power) const {
         const int tid = threadIdx.x;
         unsigned long long* sums = reinterpret_cast<unsigned long long*>(sm.running);
         __syncthreads();
         for (int i = tid; i < kRowSlots; i += BLOCK) sums[i] = 0;
         __syncthreads();
-        const int power = ilogb(mass(sorted_value(0))) + 1 - 52;   // far below zero where it has no mass
-        for (int i = tid; i < n && power > -1200; i += BLOCK)
+        for (int i = tid; i < n && power > -1000; i += BLOCK)
             atomicAdd(&sums[(uint32_t)sm.sorted[i] / (uint32_t)(G * CHUNK)],
                       (unsigned long long)(__builtin_ldexp(mass(sorted_value(i)), -power) + 0.5));
         __syncthreads();
@@ -952,6 +954,8 @@ struct Row {
             sm.slot[i] = (CLEAR ? 0.0 : sm.slot[i]) + __builtin_ldexp((double)sums[i], power);
         __syncthreads();
     }
+    // For masses of at most w (far below zero where w has none).
+    __device__ __forceinline__ static int mass_power(double w) { return ilogb(w) + 1 - 52; }
 
     enum Search { kFound, kNone, kUnsettled };
 
@@ -1011,7 +1015,7 @@ struct Row {
         cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
         kept = keep;
         slots = want_slots;
-        if (want_slots) add_to_slots<true>(keep);
+        if (want_slots) add_to_slots<true>(keep, mass_power(1.0));
         return kFound;
     }
 
@@ -1027,7 +1031,7 @@ struct Row {
         if (!by_mass && top_p < 1.0) return kUnsettled;
         float v0[VEC], ref, tau = -INFINITY;
         if (!take_sample(v0, ref)) return kUnsettled;
-        if (by_mass) tau = threshold<true>(ref, 0.0f, 0.5f * (float)(1.0 - top_p), fmaxf(1.0f, (float)V / (float)kSample));
+        if (by_mass) tau = threshold<true>(ref, 0.0f, 0.3f * (float)(1.0 - top_p), fmaxf(1.0f, (float)V / (float)kSample));
         int bin = 0;
         double before = 0.0, target = 0.0, sum = 0.0;
         for (;;) {
@@ -1103,11 +1107,10 @@ struct Row {
             if (by_mass && __ballot(some)) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (linear_bin(v[e], ref) < bin) {
-                        ++above;
-                        a += mass(v[e]);
-                    }
+                    const bool k = linear_bin(v[e], ref) < bin;
+                    const double w = mass(v[e]);
+                    above += k;
+                    a += k ? w : 0.0;
                 }
             }
             gather(in, j, -FLT_MAX);
@@ -1137,7 +1140,7 @@ struct Row {
         cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
         kept = keep + above;
         slots = want_slots && by_mass && !(min_p > 0.0 && min_floor(min_p) > cut.tau);
-        if (slots) add_to_slots<false>(keep);
+        if (slots) add_to_slots<false>(keep, mass_power(mass(sorted_value(0))));
         return kFound;
     }
     __device__ __forceinline__ static int linear_bin(float l, float ref) {
@@ -1181,17 +1184,47 @@ struct Row {
         return f;
     }
 
-    // The slots' sums of what a cut keeps, from a table of the masses of the values above it,
-    // and how many elements that is.  `partial`: the elements equal to the cut's value are
-    // counted by slot instead.  False where the table has no room for all values.
+    // The slots' sums of what a cut keeps, and how many elements that is: those of a list,
+    // where they fit one; else from a table of the masses of the values above the cut.
+    // `partial`: the elements equal to the cut's value are counted by slot instead.  False
+    // where the table has no room for all values.
     __device__ __forceinline__ bool table_masses(const Ties& cut, bool partial, int& n) const {
         const int tid = threadIdx.x, lane = tid & 63;
         if constexpr (VEC == 8) {
             if (!(cut.tau > -INFINITY)) return false;
             const int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
             if (end == kLastBin || end - top + 2 > kValueBins / 2) return false;
-            n = count_to(end) - (partial ? cut.all - cut.keep : 0);
+            const int all = count_to(end);
+            n = all - (partial ? cut.all - cut.keep : 0);
+            // words from the cut's up, as signed numbers, are the values above it if that is
+            // not negative
+            const int32_t tau_word = (int32_t)__float_as_uint(cut.tau) >> 16;
             __syncthreads();
+            if (all <= kSorted && cut.tau > 0.0f) {
+                if (tid == 0) sm.nlist = 0;
+                for (int s = tid; s < nslots; s += BLOCK) sm.ties[s] = 0;
+                __syncthreads();
+                sweep_raw<true>([&](const typename W::raw& t, int j) {
+                    i16x2 most = __builtin_bit_cast(i16x2, t.x);
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, t.y));
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, t.z));
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, t.w));
+                    if (__ballot(most.x >= tau_word || most.y >= tau_word) == 0) return;
+                    float v[VEC];
+                    W::unpack(t, v);
+                    gather(v, j, cut.tau);
+                }, [](int) {});
+                __syncthreads();
+                for (int i = tid; i < all; i += BLOCK) {
+                    // a tie that may be dropped has no mass in the sums
+                    const uint64_t x = sm.list[i];
+                    const bool tie = partial && (uint32_t)(x >> 32) == ~key_of(cut.tau);
+                    if (tie) atomicAdd(&sm.ties[(uint32_t)x / (uint32_t)(G * CHUNK)], 1);
+                    sm.sorted[i] = tie ? (uint64_t)~key_of(-INFINITY) << 32 | (uint32_t)x : x;
+                }
+                add_to_slots<true>(all, -51);
+                return true;
+            }
             for (int i = tid; i <= end - top + 1; i += BLOCK)
                 sm.table[i] = i > end - top || (partial && i == end - top) ? 0.0 : mass(bin_value(top + i));
             __syncthreads();
@@ -1200,18 +1233,8 @@ struct Row {
             const u16x2 lasts = {last, last};
             double a = 0.0;
             int ties = 0;
-            // words from the cut's up, as signed numbers, are the values above it if that is
-            // not negative
-            const int32_t tau_word = (int32_t)__float_as_uint(cut.tau) >> 16;
-            const bool words = cut.tau > 0.0f;
             sweep_raw<true>([&](const typename W::raw& t, int) {
                 const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-                if (words) {
-                    i16x2 most = __builtin_bit_cast(i16x2, w[0]);
-#pragma unroll
-                    for (int q = 1; q < 4; ++q) most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, w[q]));
-                    if (__ballot(most.x >= tau_word || most.y >= tau_word) == 0) return;
-                }
                 u16x2 at[4];
                 u16x2 lowest = lasts;
 #pragma unroll
@@ -1243,26 +1266,46 @@ struct Row {
     }
 
     // Of the listed elements of a filtered row, all equal, the first `keep` stay; the others
-    // become -inf.
+    // become -inf.  Those of the slot that the last kept one is in are counted among each other.
     __device__ __forceinline__ void drop_ties(int keep, uint16_t* out) const {
-        const int tid = threadIdx.x;
+        const int tid = threadIdx.x, lane = tid & 63;
+        constexpr int SPL = kRowSlots / 64;
+        int32_t* part = sm.equal + kListed;
         __syncthreads();
         const int n = sm.nlist;
         for (int s = tid; s < kRowSlots; s += BLOCK) sm.ties[s] = 0;
         __syncthreads();
         for (int i = tid; i < n; i += BLOCK) atomicAdd(&sm.ties[sm.equal[i] / (G * CHUNK)], 1);
         __syncthreads();
-        for (int i = tid; i < n; i += BLOCK) {
-            const int j = sm.equal[i], s = j / (G * CHUNK);
-            int before = 0;
-            for (int q = 0; q < s; ++q) before += sm.ties[q];
-            if (before + sm.ties[s] > keep) {
-                if (before < keep)
-                    for (int q = 0; q < n; ++q) before += sm.equal[q] < j && sm.equal[q] / (G * CHUNK) == s;
-                if (before >= keep) out[j] = 0xff80;
+        if (tid < 64) {
+            int cnt[SPL], own = 0;
+#pragma unroll
+            for (int q = 0; q < SPL; ++q) own += cnt[q] = sm.ties[SPL * lane + q];
+            int before = incl_scan(own) - own;
+#pragma unroll
+            for (int q = 0; q < SPL; ++q) {
+                const int left = keep - before;      // -1: the slot's all stay
+                sm.ties[SPL * lane + q] = left >= cnt[q] ? -1 : max(left, 0);
+                before += cnt[q];
             }
+            if (lane == 0) sm.nlist = 0;
+        }
+        __syncthreads();
+        for (int i = tid; i < n; i += BLOCK) {
+            const int j = sm.equal[i], left = sm.ties[j / (G * CHUNK)];
+            if (left == 0) out[j] = 0xff80;
+            else if (left > 0) part[atomicAdd(&sm.nlist, 1)] = j;
+        }
+        __syncthreads();
+        const int m = sm.nlist;
+        for (int i = tid; i < m; i += BLOCK) {
+            const int j = part[i];
+            int before = 0;
+            for (int q = 0; q < m; ++q) before += part[q] < j;
+            if (before >= sm.ties[j / (G * CHUNK)]) out[j] = 0xff80;
         }
     }
+    static constexpr int kListed = 4096;
 
     // The token of uniform u: the first index at which the kept masses' running sum exceeds
     // u times their total.  One wave; every lane returns it, and its logit.
@@ -1479,8 +1522,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
     if (FILTER) {
         // many ties: their last index is found first; few: all are written as kept, and the
         // rest taken back
-        constexpr int kListed = 4096;
-        const bool listed = counts && partial && ties.all <= kListed;
+        const bool listed = counts && partial && ties.all <= row.kListed;
         if (partial && !listed) cut.limit = row.tie_limit(ties.tau, ties.keep);
         __syncthreads();
         if (tid == 0) sm.nlist = 0;
