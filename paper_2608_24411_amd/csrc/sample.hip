@@ -36,7 +36,7 @@ constexpr int kLinearBins = 4096;
 constexpr float kBinsPerUnit = 128.0f, kRefBin = 1024.0f;
 constexpr double kMassUnit = 0x1p-40;           // of the masses in them
 // Elements that a search may leave to be sorted, and how many of them are sorted by counting.
-constexpr int kSorted = 2048, kRanked = 512;
+constexpr int kSorted = 2048, kRanked = 384;
 constexpr float kSampleBins = 64.0f;            // of a row's sample: bins a unit of logits
 
 struct SParams {
@@ -75,7 +75,10 @@ struct RowSmem : ReduceSmem {
         struct {
             uint64_t list[kSorted];   // elements: inverted key, index
             uint64_t sorted[kSorted];
-            double running[kSorted];  // running sums of their masses
+            union {
+                double running[kSorted];           // running sums of their masses
+                float packed[kMaxWaves][128];      // elements whose masses are to be summed
+            };
         };
     };
     // sums over groups of 64 bins while the cut is looked for, over slots after that
@@ -727,12 +730,10 @@ struct Row {
     // distribution.
     __device__ __forceinline__ bool slot_masses() {
         const int lane = threadIdx.x & 63;
-        float v[VEC], mx = -INFINITY;
+        float v[kSampleLane];
         load_sample(v);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v[e]);
+        float mx = sample_max(v);
         for (int attempt = 0;; ++attempt) {
-            mx = block_max(mx);
             // a NaN or a +inf here shows in the pass too
             md = uniform(mx > -INFINITY && mx < INFINITY ? (double)mx : 0.0);
             double a = 0.0;
@@ -758,7 +759,7 @@ struct Row {
             const bool any_bad = __syncthreads_or(bad);
             if (any_bad || n == 0) return false;
             if (attempt == 1 || fabs((double)m - md) * c < 500.0) return true;
-            mx = m;
+            mx = m;   // the next pass's reference
         }
     }
     int finite = 0;
@@ -766,71 +767,70 @@ struct Row {
     // ---- rows whose kept elements are few, or whose values are many
 
     // The row's sample: the first elements of eight slots spread over it, whatever the
-    // workgroup's size, so that what is relative to it does not depend on that; a vector for
-    // each lane of the first eight waves.
-    static constexpr int kSampleSlots = 8, kSample = kSampleSlots * 64 * VEC;
-    __device__ __forceinline__ void load_sample(float (&v)[VEC]) const {
+    // workgroup's size, so that what is relative to it does not depend on that; two vectors
+    // for each lane of the first eight waves.
+    static constexpr int kSampleSlots = 8, kSampleLane = 2 * VEC, kSample = kSampleSlots * 64 * kSampleLane;
+    __device__ __forceinline__ void load_sample(float (&v)[kSampleLane]) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = -INFINITY;
-        if (wid < kSampleSlots)
-            load_vec<In, VEC>(row, (int)((uint32_t)wid * (uint32_t)nslots / kSampleSlots) * G * CHUNK + lane * VEC, V, v);
+        for (int e = 0; e < kSampleLane; ++e) v[e] = -INFINITY;
+        if (wid < kSampleSlots) {
+            const int j = (int)((uint32_t)wid * (uint32_t)nslots / kSampleSlots) * G * CHUNK + lane * VEC;
+            typename W::raw t[2] = {W::template load_full<false>(row, min(j, V - VEC)),
+                                    W::template load_full<false>(row, min(j + 64 * VEC, V - VEC))};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float x[VEC];
+                cut_off(t[u], j + u * 64 * VEC);
+                W::unpack(t[u], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[u * VEC + e] = x[e];
+            }
+        }
     }
 
     // The sample, the highest of its elements (finite, or the answer is false) and their
     // histogram below it.
-    __device__ __forceinline__ bool take_sample(float (&v)[VEC], float& ref) const {
+    __device__ __forceinline__ bool take_sample(float (&v)[kSampleLane], float& ref) const {
         const int tid = threadIdx.x;
         load_sample(v);
         __syncthreads();
         for (int i = tid; i < kBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.sample)[i] = make_uint4(0, 0, 0, 0);
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v[e]);
-        ref = block_max(mx);
+        ref = sample_max(v);
         if (!(ref > -INFINITY && ref < INFINITY)) return false;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
+        for (int e = 0; e < kSampleLane; ++e) {
             const float b = (ref - v[e]) * kSampleBins;
             if (b < (float)(kBins - 1)) atomicAdd(&sm.sample[(int)b], 1u);
         }
         __syncthreads();
         return true;
     }
+    __device__ __forceinline__ float sample_max(const float (&v)[kSampleLane]) const {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kSampleLane; ++e) mx = fmaxf(mx, v[e]);
+        return block_max(mx);
+    }
 
-    // A threshold above which lie, going by the sample, `rank` of its elements (BY_MASS: all
-    // but `rest` of its mass, in which the highest element stands for itself alone and every
-    // other one for `scale` elements); -inf where there is none.  Every wave finds the same.
-    template <bool BY_MASS>
-    __device__ __forceinline__ float threshold(float ref, float rank, float rest, float scale) const {
+    // A threshold above which lie, going by the sample, `rank` of its elements; -inf where
+    // there is none.  Every wave finds the same.
+    __device__ __forceinline__ float threshold(float ref, float rank) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
         constexpr int kSampleGroups = kBins / 64;
-        static_assert(kSampleGroups <= 64, "a lane a group");
-        const float step = -(float)fmin(c, 1e30) / kSampleBins;
-        auto held = [&](int b) -> float {
-            const float n = (float)sm.sample[b];
-            return BY_MASS ? n * exp2_fast(((float)b + 0.5f) * step) : n;
-        };
+        static_assert(kSampleGroups <= 64 && kSampleGroups % kWaves == 0, "a lane a group");
 #pragma unroll
         for (int i = 0; i < kSampleGroups / kWaves; ++i) {
-            const int g = wid + i * kWaves;
-            const double t = wave_sum((double)held(g * 64 + lane));
-            if (lane == 0) sm.group_sum[g] = t;
+            const int g = wid + i * kWaves, n = wave_sum_i((int)sm.sample[g * 64 + lane]);
+            if (lane == 0) sm.group_sum[g] = (double)n;
         }
         __syncthreads();
         const double own = lane < kSampleGroups ? sm.group_sum[lane] : 0.0, incl = wave_incl_scan(own, lane);
-        double goal = (double)rank;
-        if (BY_MASS) {
-            const double total = readlane_d(incl, 63), first = (double)exp2_fast(0.5f * step);
-            goal = total - (double)rest * (fmax(total - first, 0.0) + first / (double)scale);
-        }
-        const uint64_t hit = __ballot(incl >= goal);
+        const uint64_t hit = __ballot(incl >= (double)rank);
         if (!hit) return -INFINITY;
         const int g = __ffsll((unsigned long long)hit) - 1;
-        if (g >= kSampleGroups) return -INFINITY;
-        const double in = readlane_d(incl - own, g) + wave_incl_scan((double)held(g * 64 + lane), lane);
-        const uint64_t over = __ballot(in >= goal * (1.0 - 1e-9));
-        const int at = over ? g * 64 + __ffsll((unsigned long long)over) - 1 : kBins;
+        const double in = readlane_d(incl - own, g) + wave_incl_scan((double)sm.sample[g * 64 + lane], lane);
+        const int at = g * 64 + __ffsll((unsigned long long)__ballot(in >= (double)rank)) - 1;
         return at < kBins - 1 ? ref - (float)(at + 1) / kSampleBins : -INFINITY;
     }
 
@@ -856,6 +856,37 @@ struct Row {
             if (v[e] >= tau && i < kSorted) sm.list[i] = (uint64_t)~key_of(v[e]) << 32 | (uint32_t)(j + e);
             at += __popcll(in[e]);
         }
+    }
+
+    // Sums the masses of the elements marked, 64 at a time: they wait in the wave's part of
+    // sm.packed until there are as many.  Where a few of a vector's lanes hold one, the
+    // exponentials of the others would be computed for nothing (20 instructions each; packing
+    // takes 6).  rest() sums what is left.
+    struct Packed {
+        float* held;
+        int head = 0, tail = 0;
+    };
+    __device__ __forceinline__ Packed packed() const { return {sm.packed[wave_id()]}; }
+    __device__ __forceinline__ void pack(const float (&v)[VEC], const bool (&in)[VEC], Packed& p, double& a) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const uint64_t some = __ballot(in[e]);
+            if (some == 0) continue;
+            if (in[e]) p.held[(p.tail + __popcll(some & __lanemask_lt())) & 127] = v[e];
+            p.tail += __popcll(some);
+            if (p.tail - p.head >= 64) {
+                __builtin_amdgcn_wave_barrier();
+                a += mass(p.held[(p.head + lane) & 127]);
+                p.head += 64;
+            }
+        }
+    }
+    __device__ __forceinline__ void rest(Packed& p, double& a) const {
+        const int lane = threadIdx.x & 63;
+        __builtin_amdgcn_wave_barrier();
+        if (lane < p.tail - p.head) a += mass(p.held[(p.head + lane) & 127]);
+        p.head = p.tail;
     }
 
     // sm.list[0 .. n) into sm.sorted in ascending order, n <= kSorted; no two are equal.
@@ -968,7 +999,7 @@ struct Row {
         constexpr float kRoom = 0.5f * (float)kSorted;
         const float scale = (float)V / (float)kSample;
         if (VEC == 1 || scale < 2.0f || (float)top_k > kRoom) return kUnsettled;
-        float v0[VEC], ref;
+        float v0[kSampleLane], ref;
         if (!take_sample(v0, ref)) return kUnsettled;
         // min_p's cut lies at or above its threshold below the sample's maximum (less what its
         // rounding may be); top_p after top_k needs all that top_k keeps
@@ -981,7 +1012,7 @@ struct Row {
         }
         if (top_k > 0) {
             const float mean = (float)top_k / scale;
-            const float t = threshold<false>(ref, mean + 4.0f * sqrtf(mean) + 3.0f, 0.0f, scale);
+            const float t = threshold(ref, mean + 4.0f * sqrtf(mean) + 3.0f);
             floored = floored && tau >= t;
             tau = fmaxf(tau, t);
         }
@@ -989,7 +1020,7 @@ struct Row {
         if (!(tau > -INFINITY)) return kUnsettled;
         int up = 0;   // elements above it, going by the sample
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) up += v0[e] >= tau;
+        for (int e = 0; e < kSampleLane; ++e) up += v0[e] >= tau;
         double x = 0.0, y = 0.0;
         int bad = 0;
         if (threadIdx.x == 0) sm.nlist = 0;
@@ -1020,20 +1051,21 @@ struct Row {
     }
 
     // The cut of top_p alone, or of a top_k that keeps many elements: a histogram over linear
-    // bins below the maximum, of what a sample of the row cannot rule out, says which bin the
-    // cut falls into, and a second pass sums what lies above the bin and lists what is in it.
-    // Left unsettled where that is too much to be sorted, or the histogram's masses (in units
-    // of 2^-40) named a neighbour of the bin.  slots: sm.slot holds what is kept.
+    // bins below the maximum says which bin the cut falls into, and a second pass sums what
+    // lies above the bin and lists what is in it.  Left unsettled where that is too much to be
+    // sorted, or the histogram's masses (whole numbers of 2^-40; sums of floats take ten times
+    // as long in LDS) named a neighbour of the bin.  slots: sm.slot holds what is kept.
     __device__ __forceinline__ Search search(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
                                              bool& slots, int& kept) {
         const int tid = threadIdx.x, lane = tid & 63;
         const bool by_mass = top_k == 0;
         if (!by_mass && top_p < 1.0) return kUnsettled;
-        float v0[VEC], ref, tau = -INFINITY;
-        if (!take_sample(v0, ref)) return kUnsettled;
-        if (by_mass) tau = threshold<true>(ref, 0.0f, 0.3f * (float)(1.0 - top_p), fmaxf(1.0f, (float)V / (float)kSample));
+        float v0[kSampleLane];
+        load_sample(v0);
+        float ref = sample_max(v0);
+        if (!(ref > -INFINITY && ref < INFINITY)) return kUnsettled;
         int bin = 0;
-        double before = 0.0, target = 0.0, sum = 0.0;
+        double before = 0.0, target = 0.0;
         for (;;) {
             md = uniform((double)ref);
             __syncthreads();
@@ -1054,8 +1086,7 @@ struct Row {
                         const double w = mass(v[e]);
                         a += w;
                         // the low bits of 2^52 + w 2^40 are the mass in its units
-                        if (v[e] >= tau && w > 0.0)
-                            add(v[e], __double_as_longlong(fma(w, 1.0 / kMassUnit, 0x1p52)) & 0xfffffffffffffull);
+                        add(v[e], __double_as_longlong(fma(w, 1.0 / kMassUnit, 0x1p52)) & 0xfffffffffffffull);
                     }
                 }, [](int) {});
             } else {
@@ -1083,39 +1114,32 @@ struct Row {
                 ref = m;
                 continue;
             }
-            sum = a;
-            target = by_mass ? top_p * sum : (double)top_k;
+            target = by_mass ? top_p * a : (double)top_k;
             bin = reach(target, by_mass ? kMassUnit : 1.0, before);
-            if (bin >= 0) break;
-            if (!by_mass || !(tau > -INFINITY)) return kUnsettled;
-            tau = -INFINITY;   // the sample ruled out too much
+            if (bin < 0) return kUnsettled;
+            break;
         }
         __syncthreads();
         if (tid == 0) sm.nlist = 0;
         __syncthreads();
         double a = 0.0, y = 0.0;
         int above = 0, none = 0;
+        Packed held = packed();
         sweep<true>([&](const float(&v)[VEC], int j) {
             float in[VEC];
-            bool some = false;
+            bool up[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int b = linear_bin(v[e], ref);
                 in[e] = b == bin && v[e] > -INFINITY ? v[e] : -INFINITY;
-                some |= b < bin;
+                up[e] = by_mass && b < bin;
+                above += up[e];
             }
-            if (by_mass && __ballot(some)) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const bool k = linear_bin(v[e], ref) < bin;
-                    const double w = mass(v[e]);
-                    above += k;
-                    a += k ? w : 0.0;
-                }
-            }
+            pack(v, up, held, a);
             gather(in, j, -FLT_MAX);
         }, [&](int s) {
             if (by_mass) {
+                rest(held, a);
                 const double t = wave_sum(a);
                 if (lane == 0) sm.slot[s] = t;
                 a = 0.0;
@@ -1144,7 +1168,9 @@ struct Row {
         return kFound;
     }
     __device__ __forceinline__ static int linear_bin(float l, float ref) {
-        return (int)fminf(fmaxf(fmaf(ref - l, kBinsPerUnit, kRefBin), 0.0f), (float)(kLinearBins - 1));
+        // 2^23 and a whole number: the number is in the low bits
+        const float b = fmaf(ref - l, kBinsPerUnit, 0x1p23f + kRefBin);
+        return (int)(__float_as_uint(fminf(fmaxf(b, 0x1p23f), 0x1p23f + (float)(kLinearBins - 1))) & (kLinearBins - 1));
     }
 
     // The bin of sm.bins in which their running sum, in `unit`s, reaches `target` and what lies
@@ -1343,10 +1369,20 @@ struct Row {
         base = readlane_d(base, L);
         int last = 0;
         float last_l = 0.0f;
-        for (int q = slot * G * UNR; q < (slot + 1) * G * UNR; ++q) {
-            const int j = q * 64 * VEC + lane * VEC;
+        typename W::raw held[UNR];
+        for (int q = 0; q < G * UNR; ++q) {
+            if (q % UNR == 0) {
+#pragma unroll
+                for (int u = 0; u < UNR; ++u)
+                    held[u] = W::template load_full<false>(row, min((slot * G * UNR + q + u) * 64 * VEC + lane * VEC, V - VEC));
+            }
+            const int j = (slot * G * UNR + q) * 64 * VEC + lane * VEC;
+            typename W::raw x = held[0];
+#pragma unroll
+            for (int u = 0; u + 1 < UNR; ++u) held[u] = held[u + 1];
+            cut_off(x, j);
             float v[VEC];
-            load_vec<In, VEC>(row, j, V, v);
+            W::unpack(x, v);
             double w[VEC], sum = 0.0;
             int at = -1;
             float l = 0.0f;
@@ -1564,16 +1600,15 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         } else {
             if (partial) cut.limit = row.tie_limit(ties.tau, ties.keep);
             double a = 0.0;
+            auto held = row.packed();
+            __syncthreads();
             row.template sweep<true>([&](const float(&v)[VEC], int j) {
+                bool in[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                    if (cut.keeps(v[e], j + e)) {
-                        a += row.mass(v[e]);
-                        ++n;
-                    }
-                }
+                for (int e = 0; e < VEC; ++e) n += in[e] = cut.keeps(v[e], j + e);
+                row.pack(v, in, held, a);
             }, [&](int s) {
+                row.rest(held, a);
                 const double t = wave_sum(a);
                 if (lane == 0) sm.slot[s] = t;
                 a = 0.0;
@@ -1638,11 +1673,9 @@ __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
         float lowest = INFINITY;
         for (int i = 0; i < P.k; ++i) lowest = fminf(lowest, token_logit[i]);
         lowest = uniform(P.rank ? lowest : INFINITY);
-        float v0[VEC], mx = -INFINITY;
+        float v0[RowT::kSampleLane];
         row.load_sample(v0);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, v0[e]);
-        float ref = row.block_max(mx);
+        float ref = row.sample_max(v0);
         if (!(ref > -INFINITY && ref < INFINITY)) ref = 0.0f;
         // c in two parts, both above zero: a -inf element's exponent is -inf, not a NaN
         float ch = (float)fmin(row.c, (double)FLT_MAX);
