@@ -718,20 +718,20 @@ def _rows(t, name):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    if t.dtype != torch.float32 and t.dtype != torch.bfloat16:
+    if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
         raise TypeError("%s must be float32 or bfloat16" % name)
     shape, stride = t.shape, t.stride()
-    if not 2 <= len(shape) <= 3:
-        raise ValueError("%s must be [R, V] or [B, N, V]" % name)
-    V = shape[-1]
-    if V > 1 and stride[-1] != 1:
-        raise ValueError("%s: the elements of a row must be adjacent" % name)
     if len(shape) == 2:
         R, step = shape[0], stride[0]
-    else:
+    elif len(shape) == 3:
         R, step = shape[0] * shape[1], stride[1] if shape[1] > 1 else stride[0]
         if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
             raise ValueError("%s: all rows must lie one stride apart" % name)
+    else:
+        raise ValueError("%s must be [R, V] or [B, N, V]" % name)
+    V = shape[-1]
+    if stride[-1] != 1 and V > 1:
+        raise ValueError("%s: the elements of a row must be adjacent" % name)
     if R < 2:
         step = V
     elif step < V:
@@ -743,12 +743,10 @@ def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
     """rs_filter of settings that are numbers, or device tensors with an entry a row ([R] or
     [B, N]) or a sequence ([B])."""
     import torch
-    f = RsFilter(RS_BF16 if logits.dtype == torch.bfloat16 else RS_F32, 1, 1.0, 0, 1.0, 0.0)
+    f = RsFilter(RS_BF16 if logits.dtype is torch.bfloat16 else RS_F32, 1, 1.0, 0, 1.0, 0.0)
     shape = None
-    for v, number, array, dtype in ((temperature, "temperature", "temperatures", torch.float32),
-                                    (top_k, "top_k", "top_ks", torch.int32),
-                                    (top_p, "top_p", "top_ps", torch.float32),
-                                    (min_p, "min_p", "min_ps", torch.float32)):
+    for v, number, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                             (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
         if not isinstance(v, torch.Tensor):
             setattr(f, number, v)
             continue
@@ -758,47 +756,39 @@ def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
                 raise ValueError("%s has shape %s, expected %s or %s" % (number, tuple(shape), tuple(lead),
                                                                         tuple(lead[:1])))
             f.rows_per_entry = max(1, R // max(1, v.numel()))
-        elif v.shape != shape:
-            raise ValueError("settings given as tensors must have one shape")
-        if v.device != logits.device:
-            raise ValueError("all tensors must be on one device, got %s" % {v.device, logits.device})
-        setattr(f, array, _dev(v, dtype, number))
+        setattr(f, number + "s", _given(v, shape, dtype, logits, number))
     return f
 
 
-class _On:
-    """The device of the rows made current, and `stream` (or its current stream) the one that
-    temporary and returned tensors belong to."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.guards = []
-        if stream is not None:
-            if stream.device != device:
-                raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, device))
-            self.guards.append(torch.cuda.stream(stream))
-        elif torch.cuda.current_device() != device.index:
-            self.guards.append(torch.cuda.device(device))
-
-    def __enter__(self):
-        for g in self.guards:
-            g.__enter__()
-
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
-
-
-def _out(t, shape, dtype, device, name):
-    """An output of the caller's, checked, or a new one."""
+def _given(t, shape, dtype, logits, name):
+    """The address of a contiguous tensor on the rows' device."""
     import torch
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _shape(t, shape, name)
-    _dev(t, dtype, name)
-    if t.device != device:
-        raise ValueError("all tensors must be on one device, got %s" % {t.device, device})
-    return t
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if t.get_device() != logits.get_device():
+        raise ValueError("all tensors must be on one device, got %s" % {t.device, logits.device})
+    return t.data_ptr()
+
+
+def _row_call(logits, stream, call):
+    """call(stream handle) with the rows' device current, and `stream`, if given, the one that
+    the tensors allocated in it belong to."""
+    import torch
+    if stream is None and torch.cuda.current_device() == logits.get_device():
+        return call(_stream(None))
+    if stream is None:
+        with torch.cuda.device(logits.device):
+            return call(_stream(None))
+    if stream.device != logits.device:
+        raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, logits.device))
+    with torch.cuda.stream(stream):
+        return call(_stream(stream))
 
 
 def resispec_sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out_token=None,
@@ -815,18 +805,22 @@ def resispec_sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
     ptr, step, lead, R, V = _rows(logits, "logits")
     if u.dim() != len(lead) + 1 or u.shape[:-1] != lead:
         raise ValueError("u has shape %s, expected %s and the number of draws" % (tuple(u.shape), tuple(lead)))
-    dev, k = logits.device, u.shape[-1]
+    shape, dev = u.shape, logits.device
     f = _settings(logits, lead, R, temperature, top_k, top_p, min_p)
-    _same_device(logits, u)
-    with _On(dev, stream):
-        out_token = _out(out_token, u.shape, torch.int32, dev, "out_token")
-        out_logprob = _out(out_logprob, u.shape, torch.float32, dev, "out_logprob")
-        out_kept = _out(out_kept, lead, torch.int32, dev, "out_kept")
-        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
-        _check(lib.resispec_sample(ptr, step, _dev(u, torch.float32, "u"), R, V, k, ctypes.byref(f),
-                                   out_token.data_ptr(), out_logprob.data_ptr(), out_kept.data_ptr(),
-                                   out_status.data_ptr(), _stream(stream)))
-    return out_token, out_logprob, out_kept, out_status
+    up = _given(u, shape, torch.float32, logits, "u")
+
+    def call(handle):
+        tok = torch.empty(shape, dtype=torch.int32, device=dev) if out_token is None else out_token
+        lp = torch.empty(shape, dtype=torch.float32, device=dev) if out_logprob is None else out_logprob
+        kept = torch.empty(lead, dtype=torch.int32, device=dev) if out_kept is None else out_kept
+        st = torch.empty(lead, dtype=torch.int32, device=dev) if out_status is None else out_status
+        _check(lib.resispec_sample(ptr, step, up, R, V, shape[-1], ctypes.byref(f),
+                                   _given(tok, shape, torch.int32, logits, "out_token"),
+                                   _given(lp, shape, torch.float32, logits, "out_logprob"),
+                                   _given(kept, lead, torch.int32, logits, "out_kept"),
+                                   _given(st, lead, torch.int32, logits, "out_status"), handle))
+        return tok, lp, kept, st
+    return _row_call(logits, stream, call)
 
 
 def resispec_filter_logits(logits, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None,
@@ -838,23 +832,26 @@ def resispec_filter_logits(logits, *, temperature=1.0, top_k=0, top_p=1.0, min_p
     ptr, step, lead, R, V = _rows(logits, "logits")
     dev = logits.device
     f = _settings(logits, lead, R, temperature, top_k, top_p, min_p)
-    with _On(dev, stream):
-        if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-        to, to_step, _, _, _ = _rows(out, "out")
-        _shape(out, logits.shape, "out")
-        _same_device(logits, out)
-        if out.dtype != logits.dtype:
+
+    def call(handle):
+        y = torch.empty(logits.shape, dtype=logits.dtype, device=dev) if out is None else out
+        to, to_step, _, _, _ = _rows(y, "out")
+        _shape(y, logits.shape, "out")
+        if y.dtype is not logits.dtype:
             raise TypeError("out must be %s" % logits.dtype)
+        if y.get_device() != logits.get_device():
+            raise ValueError("all tensors must be on one device, got %s" % {y.device, dev})
         if R and not (to == ptr and to_step == step):
             size = logits.element_size()
             if to < ptr + ((R - 1) * step + V) * size and ptr < to + ((R - 1) * to_step + V) * size:
                 raise ValueError("out must not overlap logits, unless it is the same rows")
-        out_kept = _out(out_kept, lead, torch.int32, dev, "out_kept")
-        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
-        _check(lib.resispec_filter_logits(ptr, step, R, V, ctypes.byref(f), to, to_step, out_kept.data_ptr(),
-                                          out_status.data_ptr(), _stream(stream)))
-    return out, out_kept, out_status
+        kept = torch.empty(lead, dtype=torch.int32, device=dev) if out_kept is None else out_kept
+        st = torch.empty(lead, dtype=torch.int32, device=dev) if out_status is None else out_status
+        _check(lib.resispec_filter_logits(ptr, step, R, V, ctypes.byref(f), to, to_step,
+                                          _given(kept, lead, torch.int32, logits, "out_kept"),
+                                          _given(st, lead, torch.int32, logits, "out_status"), handle))
+        return y, kept, st
+    return _row_call(logits, stream, call)
 
 
 def resispec_token_logprobs(logits, tokens, *, temperature=1.0, out_logprob=None, out_rank=None,
@@ -867,14 +864,17 @@ def resispec_token_logprobs(logits, tokens, *, temperature=1.0, out_logprob=None
     if tokens.dim() != len(lead) + 1 or tokens.shape[:-1] != lead:
         raise ValueError("tokens has shape %s, expected %s and the number of tokens" %
                          (tuple(tokens.shape), tuple(lead)))
-    dev, k = logits.device, tokens.shape[-1]
+    shape, dev = tokens.shape, logits.device
     f = _settings(logits, lead, R, temperature, 0, 1.0, 0.0)
-    _same_device(logits, tokens)
-    with _On(dev, stream):
-        out_logprob = _out(out_logprob, tokens.shape, torch.float32, dev, "out_logprob")
-        out_rank = _out(out_rank, tokens.shape, torch.int32, dev, "out_rank")
-        out_status = _out(out_status, lead, torch.int32, dev, "out_status")
-        _check(lib.resispec_token_logprobs(ptr, step, _dev(tokens, torch.int32, "tokens"), R, V, k,
-                                           ctypes.byref(f), out_logprob.data_ptr(), out_rank.data_ptr(),
-                                           out_status.data_ptr(), _stream(stream)))
-    return out_logprob, out_rank, out_status
+    ids = _given(tokens, shape, torch.int32, logits, "tokens")
+
+    def call(handle):
+        lp = torch.empty(shape, dtype=torch.float32, device=dev) if out_logprob is None else out_logprob
+        rank = torch.empty(shape, dtype=torch.int32, device=dev) if out_rank is None else out_rank
+        st = torch.empty(lead, dtype=torch.int32, device=dev) if out_status is None else out_status
+        _check(lib.resispec_token_logprobs(ptr, step, ids, R, V, shape[-1], ctypes.byref(f),
+                                           _given(lp, shape, torch.float32, logits, "out_logprob"),
+                                           _given(rank, shape, torch.int32, logits, "out_rank"),
+                                           _given(st, lead, torch.int32, logits, "out_status"), handle))
+        return lp, rank, st
+    return _row_call(logits, stream, call)
