@@ -600,15 +600,16 @@ struct Row {
     __device__ __forceinline__ Ties cut_values(int top_k, double top_p) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
         const bool want_mass = top_p < 1.0;
-        for (int g = wid; g < kGroups; g += kWaves) {
-            double t = 0.0;
-            if (want_mass && sm.group_count[g]) {
-                const int b = g * 64 + lane;
-                const int n = b < kLastBin ? (int)sm.count[b] : 0;
-                t = wave_sum(n ? (double)n * mass(bin_value(b)) : 0.0);
-            }
-            if (lane == 0) sm.group_sum[g] = t;
+        // lane i: the count of the wave's i-th group, and then its mass
+        double held = 0.0;
+        uint64_t some = __ballot(want_mass && lane < kGroups / kWaves && sm.group_count[wid + min(lane, kGroups / kWaves - 1) * kWaves]);
+        for (; some; some &= some - 1) {
+            const int i = __ffsll((unsigned long long)some) - 1, b = (wid + i * kWaves) * 64 + lane;
+            const int n = b < kLastBin ? (int)sm.count[b] : 0;
+            const double t = wave_sum(n ? (double)n * mass(bin_value(b)) : 0.0);
+            if (lane == i) held = t;
         }
+        if (lane < kGroups / kWaves) sm.group_sum[wid + lane * kWaves] = held;
         __syncthreads();
         int all = 0;
         double all_m = 0.0;
@@ -647,6 +648,13 @@ struct Row {
         for (int q = 0; q < kLaneGroups; ++q)
             if (lane * kLaneGroups + q < g) n += sm.group_count[lane * kLaneGroups + q];
         return wave_sum_i(n);
+    }
+
+    // How many elements a cut from the counts keeps; -1 where they do not say.
+    __device__ __forceinline__ int count_kept(const Ties& cut) const {
+        if (!(cut.tau > -INFINITY)) return -1;
+        const int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
+        return end == kLastBin ? -1 : count_to(end) - (cut.keep < cut.all ? cut.all - cut.keep : 0);
     }
 
     // The index of the keep-th element equal to tau.
@@ -1162,7 +1170,7 @@ struct Row {
         }
         if (keep < 1 || keep > n) return kUnsettled;
         cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
-        kept = keep + above;
+        kept = by_mass ? keep + above : top_k;
         slots = want_slots && by_mass && !(min_p > 0.0 && min_floor(min_p) > cut.tau);
         if (slots) add_to_slots<false>(keep, mass_power(mass(sorted_value(0))));
         return kFound;
@@ -1217,11 +1225,11 @@ struct Row {
     __device__ __forceinline__ bool table_masses(const Ties& cut, bool partial, int& n) const {
         const int tid = threadIdx.x, lane = tid & 63;
         if constexpr (VEC == 8) {
-            if (!(cut.tau > -INFINITY)) return false;
+            const int kept = count_kept(cut);
             const int end = bin_bytes(__float_as_uint(cut.tau) >> 16).x / 4;
-            if (end == kLastBin || end - top + 2 > kValueBins / 2) return false;
-            const int all = count_to(end);
-            n = all - (partial ? cut.all - cut.keep : 0);
+            if (kept < 0 || end - top + 2 > kValueBins / 2) return false;
+            const int all = kept + (partial ? cut.all - cut.keep : 0);
+            n = kept;
             // words from the cut's up, as signed numbers, are the values above it if that is
             // not negative
             const int32_t tau_word = (int32_t)__float_as_uint(cut.tau) >> 16;
@@ -1455,6 +1463,46 @@ __device__ __forceinline__ void store_vec(In* out, int j, int V, const float (&v
     }
 }
 
+// A vector's elements below tau (not zero) become -inf; whether one equals it.
+__device__ __forceinline__ bool keep_from(uint4& t, float tau, uint16_t) {
+    // bf16 words as signed numbers in the values' order: negative ones have their low bits
+    // turned over
+    const uint32_t b = __float_as_uint(tau) >> 16;
+    const int16_t key = (int16_t)(b ^ (b & 0x8000u ? 0x7fffu : 0u));
+    const i16x2 keys = {key, key}, below = {(int16_t)(key - 1), (int16_t)(key - 1)}, fifteen = {0x7fff, 0x7fff};
+    u16x2 nearest = {0xffff, 0xffff};
+    uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const i16x2 x = __builtin_bit_cast(i16x2, w[q]), k = x ^ ((x >> 15) & fifteen);
+        const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(below, k) >> 15);
+        nearest = __builtin_elementwise_min(nearest, __builtin_bit_cast(u16x2, k ^ keys));
+        w[q] = (w[q] & m) | (0xff80ff80u & ~m);
+    }
+    t = make_uint4(w[0], w[1], w[2], w[3]);
+    return nearest.x == 0 || nearest.y == 0;
+}
+__device__ __forceinline__ bool keep_from(uint4& t, float tau, float) {
+    bool tie = false;
+    uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float v = __uint_as_float(w[q]);
+        tie |= v == tau;
+        w[q] = v >= tau ? w[q] : 0xff800000u;
+    }
+    t = make_uint4(w[0], w[1], w[2], w[3]);
+    return tie;
+}
+__device__ __forceinline__ void store_raw(odd16* out, const uint4& t) {
+    *reinterpret_cast<u32x4_at2*>(out) = u32x4{t.x, t.y, t.z, t.w};
+}
+__device__ __forceinline__ void store_raw(uint16_t* out, const uint4& t) { *reinterpret_cast<uint4*>(out) = t; }
+__device__ __forceinline__ void store_raw(odd32* out, const uint4& t) {
+    *reinterpret_cast<u32x4_at4*>(out) = u32x4{t.x, t.y, t.z, t.w};
+}
+__device__ __forceinline__ void store_raw(float* out, const uint4& t) { *reinterpret_cast<uint4*>(out) = t; }
+
 // One workgroup a row: the cut, then the draws or the filtered row.
 template <typename In, int VEC, int UNR, int BLOCK, bool FILTER>
 __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) rs_sample_kernel(const SParams P) {
@@ -1530,6 +1578,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
             if (f > ties.tau) {
                 ties = Ties{f, 0, 0};
                 cut = Cut{f, INT_MAX};
+                kept = -1;
             }
         }
     }
@@ -1559,12 +1608,14 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         // many ties: their last index is found first; few: all are written as kept, and the
         // rest taken back
         const bool listed = counts && partial && ties.all <= row.kListed;
+        if constexpr (kCounts)
+            if (counts && filters) kept = row.count_kept(ties);
         if (partial && !listed) cut.limit = row.tie_limit(ties.tau, ties.keep);
         __syncthreads();
         if (tid == 0) sm.nlist = 0;
         __syncthreads();
         int n = 0, none = 0;
-        row.template sweep<true>([&](const float(&v)[VEC], int j) {
+        auto exactly = [&](const float(&v)[VEC], int j) {
             float w[VEC];
             bool tie = false;
 #pragma unroll
@@ -1580,14 +1631,47 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
                 for (int e = 0; e < VEC; ++e)
                     if (v[e] == ties.tau) sm.equal[atomicAdd(&sm.nlist, 1)] = j + e;
             }
-        }, [](int) {});
-        double x = 0.0, y = 0.0;
-        row.sum2(x, y, n, none);
-        if (listed) {
-            row.drop_ties(ties.keep, reinterpret_cast<uint16_t*>(out));
-            n -= ties.all - ties.keep;
+        };
+        const bool known = kept >= 0;
+        if (!known || ties.tau == 0.0f) {
+            row.template sweep<true>(exactly, [](int) {});
+            double x = 0.0, y = 0.0;
+            row.sum2(x, y, n, none);
+            n -= listed ? ties.all - ties.keep : 0;
+            if (!known) kept = n;
+        } else {
+            // vectors without an element equal to the cut's value take a comparison each, of
+            // the two bf16 values of a word at once
+            const bool check = listed || cut.limit != INT_MAX;
+            row.template sweep_raw<true>([&](const typename Vec<In, VEC>::raw& t, int j) {
+                typename Vec<In, VEC>::raw w = t;
+                bool tie = false;
+                if constexpr (VEC == 1) {
+                    const float v = __uint_as_float(t);
+                    tie = v == ties.tau;
+                    w = v >= ties.tau ? t : 0xff800000u;
+                } else {
+                    tie = keep_from(w, ties.tau, std::conditional_t<sizeof(In) == 2, uint16_t, float>());
+                }
+                if (check && __ballot(tie)) {
+                    float v[VEC];
+                    Vec<In, VEC>::unpack(t, v);
+                    exactly(v, j);
+                } else {
+                    float v[VEC];
+                    if constexpr (VEC != 1) {
+                        if (j + VEC <= P.V) {
+                            store_raw(out + j, w);
+                            return;
+                        }
+                    }
+                    Vec<In, VEC>::unpack(w, v);
+                    store_vec<In, VEC>(out, j, P.V, v);
+                }
+            }, [](int) {});
+            __syncthreads();
         }
-        kept = n;
+        if (listed) row.drop_ties(ties.keep, reinterpret_cast<uint16_t*>(out));
     } else if (filters && !slots) {
         int n = 0, none = 0;
         if (counts && row.table_masses(ties, partial, n)) {
