@@ -510,7 +510,9 @@ typedef struct {
  *                 log-probabilities NaN.
  * RS_ERR_INVALID_ARG for a NULL pointer, R < 0, V <= 0, k <= 0, row_stride < V, or a number
  * in `filter` out of its range (a device array's entries are checked on the device);
- * RS_ERR_UNSUPPORTED for V > RS_MAX_VOCAB or k > RS_MAX_CANDIDATES.  R = 0 is a no-op.
+ * RS_ERR_UNSUPPORTED for V > RS_MAX_VOCAB, k > RS_MAX_CANDIDATES or R >= 2^23.  R = 0 is a
+ * no-op.  A row's outputs depend on that row, its settings and its uniforms alone, not on the
+ * batch it is in.
  */
 rs_status resispec_sample(const void* logits, int64_t row_stride, const float* u, int32_t R,
                           int32_t V, int32_t k, const rs_filter* filter, int32_t* out_token,

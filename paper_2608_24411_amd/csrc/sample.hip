@@ -18,9 +18,11 @@ namespace {
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
-// 16-byte loads a lane and chunk: bf16 rows, others (fewer: four would cost registers that the
-// exponentials need)
-constexpr int kUnrRow16 = 4, kUnrRow32 = 2;
+// 16-byte loads a lane and chunk.  Four give rows in sequence more loads under way (one row's
+// log-probability 16.0 -> 15.0 us) but cost registers, and slots of twice the length to draw
+// from: 1024 bf16 rows under top-p 134 us with two and 142 with four, six draws from each of
+// 64 rows 45 and 50.
+constexpr int kUnrRow = 2;
 
 // Bins of bf16 values, from the highest to the lowest: one for every value with 2^-38 < |l| <
 // 1020, one for both zeros, one on each side of it for the values nearer to zero, one at each
@@ -176,9 +178,10 @@ __device__ __forceinline__ float bin_value(int bin) {
     return __uint_as_float((uint32_t)(t + kLoMag) << 16 | (bin > kHalf ? 0x80000000u : 0u));
 }
 
-template <typename In, int VEC, int UNR, int BLOCK, typename Smem = RowSmem>
+template <typename In, int VEC, int BLOCK, typename Smem = RowSmem>
 struct Row {
     using W = Vec<In, VEC>;
+    static constexpr int UNR = kUnrRow;
     static constexpr int CHUNK = 64 * VEC * UNR;
     static constexpr int kWaves = BLOCK / 64;
     const In* row;
@@ -194,7 +197,7 @@ struct Row {
     // flush(slot) after a slot's last.  A wave's slots are the same in every pass.  NT: the
     // row's last use.  Two chunks of registers alternate.  Loads take no branch, so that the
     // wait before a chunk is for that chunk alone (with bounds checks around them the compiler
-    // waits for the next one too: 128 x 5 rows of 128,256 took 60 us where they take 44): what
+    // waits for the next one too: 128 x 5 rows of 128,256 took 60 us where they take 48): what
     // lies past the row reads the row's last elements and is put right in the last chunk, and
     // a wave's last step loads its chunk again.
     template <bool NT, typename Body, typename Flush>
@@ -470,7 +473,8 @@ struct Row {
     // that a cut needs (values outside the bins' range, unless they have no mass, make the row
     // one for the search above); a NaN or a +inf sets `bad`.
     __device__ __forceinline__ bool count_values(bool& bad) {
-        const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int tid = threadIdx.x, lane = tid & 63, wid = wave_id();
+        __syncthreads();   // few() may have left a wave reading the sample, which lies here
         for (int i = tid; i < kValueBins / 4; i += BLOCK) reinterpret_cast<uint4*>(sm.count)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         bool mine = false;
@@ -939,7 +943,7 @@ struct Row {
 
     // Running sums of the masses of sm.sorted[0 .. n) into sm.running.
     __device__ __forceinline__ void prefix(int n) const {
-        const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int tid = threadIdx.x, lane = tid & 63, wid = wave_id();
         const int per = (n + BLOCK - 1) / BLOCK;
         double own = 0.0;
         for (int q = 0; q < per; ++q)
@@ -996,7 +1000,8 @@ struct Row {
     // For masses of at most w (far below zero where w has none).
     __device__ __forceinline__ static int mass_power(double w) { return ilogb(w) + 1 - 52; }
 
-    enum Search { kFound, kNone, kUnsettled };
+    // kTied: the cut's value is known, and how many of the elements equal to it are kept
+    enum Search { kFound, kTied, kNone, kUnsettled };
 
     // The cut of top_k, with top_p and min_p or without, or of min_p alone, where it keeps few
     // elements, in one pass: a sample of the row gives a threshold with some more elements
@@ -1061,10 +1066,11 @@ struct Row {
     // The cut of top_p alone, or of a top_k that keeps many elements: a histogram over linear
     // bins below the maximum says which bin the cut falls into, and a second pass sums what
     // lies above the bin and lists what is in it.  Left unsettled where that is too much to be
-    // sorted, or the histogram's masses (whole numbers of 2^-40; sums of floats take ten times
-    // as long in LDS) named a neighbour of the bin.  slots: sm.slot holds what is kept.
+    // sorted and not all one value, or the histogram's masses (whole numbers of 2^-40; sums of
+    // floats take ten times as long in LDS) named a neighbour of the bin.  slots: sm.slot
+    // holds what is kept.
     __device__ __forceinline__ Search search(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
-                                             bool& slots, int& kept) {
+                                             Ties& ties, bool& slots, int& kept) {
         const int tid = threadIdx.x, lane = tid & 63;
         const bool by_mass = top_k == 0;
         if (!by_mass && top_p < 1.0) return kUnsettled;
@@ -1155,14 +1161,31 @@ struct Row {
         });
         sum2(a, y, above, none);
         const int n = sm.nlist;
-        if (n > kSorted || n < 1) return kUnsettled;
-        sort(n);
-        int keep;
+        if (n < 1) return kUnsettled;
+        double total = 0.0;
         if (by_mass) {
-            double total = 0.0;
             for (int s = lane; s < nslots; s += 64) total += sm.slot[s];
             total = wave_sum(total);
             if (total >= target) return kUnsettled;
+        }
+        if (n > kSorted) {
+            uint32_t lo = ~0u, hi = 0u;
+            each([&](float l, int) {
+                if (l > -INFINITY && linear_bin(l, ref) == bin) {
+                    lo = min(lo, key_of(l));
+                    hi = max(hi, key_of(l));
+                }
+            });
+            range(lo, hi);
+            if (lo != hi) return kUnsettled;
+            const double w = mass(value_of(lo));
+            if (by_mass && total + (double)n * w < target) return kUnsettled;
+            ties = Ties{value_of(lo), by_mass ? ties_for(target - total, w, n) : top_k - (int)before, n};
+            return kTied;
+        }
+        sort(n);
+        int keep;
+        if (by_mass) {
             prefix(n);
             keep = reach_running(n, target - total) + 1;
         } else {
@@ -1504,7 +1527,7 @@ __device__ __forceinline__ void store_raw(odd32* out, const uint4& t) {
 __device__ __forceinline__ void store_raw(float* out, const uint4& t) { *reinterpret_cast<uint4*>(out) = t; }
 
 // One workgroup a row: the cut, then the draws or the filtered row.
-template <typename In, int VEC, int UNR, int BLOCK, bool FILTER>
+template <typename In, int VEC, int BLOCK, bool FILTER>
 __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) rs_sample_kernel(const SParams P) {
     __shared__ RowSmem sm;
     constexpr int kWaves = BLOCK / 64;
@@ -1516,7 +1539,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
     const float top_p = P.top_ps ? P.top_ps[entry] : P.top_p;
     const float min_p = P.min_ps ? P.min_ps[entry] : P.min_p;
     const int top_k = P.top_ks ? P.top_ks[entry] : P.top_k;
-    Row<In, VEC, UNR, BLOCK> row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
+    Row<In, VEC, BLOCK> row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
                                  uniform(1.4426950408889634 / (double)T), uniform((double)T), sm};
     In* out = FILTER ? reinterpret_cast<In*>(P.out) + r * P.out_stride : nullptr;
     int status = RS_SEQ_OK;
@@ -1535,26 +1558,27 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
     int kept = -1;
     if (status == RS_SEQ_OK && (filters || FILTER)) {
         bool bad = false;
-        auto found = Row<In, VEC, UNR, BLOCK>::kUnsettled;
+        auto found = Row<In, VEC, BLOCK>::kUnsettled;
         if (top_k > 0 || (!FILTER && min_p > 0.0f && top_p == 1.0f))
             found = row.few(top_k, (double)top_p, (double)min_p, !FILTER, cut, slots, kept);
         if constexpr (kCounts) {
-            if (found == Row<In, VEC, UNR, BLOCK>::kUnsettled) {
+            if (found == Row<In, VEC, BLOCK>::kUnsettled) {
                 counts = row.count_values(bad);
                 if (counts && filters) ties = row.cut_values(top_k, (double)top_p);
             }
         }
-        if (bad || found == Row<In, VEC, UNR, BLOCK>::kNone) {
+        if (bad || found == Row<In, VEC, BLOCK>::kNone) {
             status = RS_SEQ_UNDERFLOW;
         } else if (!counts) {
             int n = 0;
             const bool cuts = top_k > 0 || top_p < 1.0f;
             if constexpr (!kCounts)
-                if (cuts && found == Row<In, VEC, UNR, BLOCK>::kUnsettled) found = row.search(top_k, (double)top_p, (double)min_p, !FILTER, cut, slots, kept);
-            if (found == Row<In, VEC, UNR, BLOCK>::kNone) status = RS_SEQ_UNDERFLOW;
-            settled = found == Row<In, VEC, UNR, BLOCK>::kFound;
-            if (!settled && status == RS_SEQ_OK && !row.statistics(n)) status = RS_SEQ_UNDERFLOW;
-            if (!settled && status == RS_SEQ_OK && cuts) {
+                if (cuts && found == Row<In, VEC, BLOCK>::kUnsettled) found = row.search(top_k, (double)top_p, (double)min_p, !FILTER, cut, ties, slots, kept);
+            if (found == Row<In, VEC, BLOCK>::kNone) status = RS_SEQ_UNDERFLOW;
+            settled = found == Row<In, VEC, BLOCK>::kFound;
+            const bool tied = found == Row<In, VEC, BLOCK>::kTied;
+            if (!settled && !tied && status == RS_SEQ_OK && !row.statistics(n)) status = RS_SEQ_UNDERFLOW;
+            if (!settled && !tied && status == RS_SEQ_OK && cuts) {
                 const uint32_t lo = key_of(-INFINITY) + 1, hi = key_of(row.m);
                 double mass = 0.0;
                 const bool cuts_k = top_k > 0 && top_k < n;
@@ -1727,7 +1751,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
 // sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
 // vectors with an element that is not below every token take the count, a step a token.
 // Where the sum overflows or the sample is masked, a second pass against the maximum.
-template <typename In, int VEC, int UNR, int BLOCK>
+template <typename In, int VEC, int BLOCK>
 __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
     __shared__ ReduceSmem sm;
     __shared__ float token_logit[kMaxCand];
@@ -1737,7 +1761,7 @@ __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
     using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
     const int64_t r = blockIdx.x;
     const float T = P.temperatures ? P.temperatures[r / P.rows_per_entry] : P.temperature;
-    using RowT = Row<In, VEC, UNR, BLOCK, ReduceSmem>;
+    using RowT = Row<In, VEC, BLOCK, ReduceSmem>;
     RowT row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0,
                                  uniform(1.4426950408889634 / (double)T), uniform((double)T), sm};
     int status = RS_SEQ_OK;
@@ -1764,7 +1788,7 @@ __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
         // c in two parts, both above zero: a -inf element's exponent is -inf, not a NaN
         float ch = (float)fmin(row.c, (double)FLT_MAX);
         if ((double)ch >= row.c) ch = __uint_as_float(__float_as_uint(ch) - 1);
-        const float cl = (float)fmin(row.c - (double)ch, (double)FLT_MAX);
+        const float cl = fmaxf((float)fmin(row.c - (double)ch, (double)FLT_MAX), 0x1p-149f);
         int before = 0;   // lane i: token i's, of the wave's elements
         for (int attempt = 0;; ++attempt) {
             double a = 0.0;
@@ -1864,21 +1888,22 @@ RowLoads strided_loads(const void* p, int64_t stride, int32_t V, int dtype) {
     return l == kLoadsAligned && stride * esz % 16 ? kLoadsAny : l;
 }
 
+// A workgroup a row, and less than 2^32 threads a launch.
+constexpr int32_t kMaxRows = (1 << 23) - 1;
+
 // The row of V elements in slots of G chunks.
-template <int VEC, int UNR>
+template <int VEC>
 void set_slots(SParams& P) {
-    constexpr int64_t CHUNK = 64 * VEC * UNR;
+    constexpr int64_t CHUNK = 64 * VEC * kUnrRow;
     const int64_t nch = ((int64_t)P.V + CHUNK - 1) / CHUNK;
     P.G = (int32_t)((nch + kRowSlots - 1) / kRowSlots);
     P.nslots = (int32_t)((nch + P.G - 1) / P.G);
 }
 
-// f(element type, elements a load, loads a chunk) for the kernels' instance.
+// f(element type, elements a load) for the kernels' instance.
 template <typename F>
 auto with_rows(int dtype, RowLoads loads, F&& f) {
-    return with_layout(dtype, loads, [&](auto in, auto vec, auto) {
-        return f(in, vec, std::integral_constant<int, vec() == 4 ? kUnrRow32 : kUnrRow16>());
-    });
+    return with_layout(dtype, loads, [&](auto in, auto vec, auto) { return f(in, vec); });
 }
 
 // Threads a row: 16 waves where every row has a CU to itself, two rows of 8 waves a CU where
@@ -1900,7 +1925,7 @@ rs_status resispec_sample(const void* logits, int64_t row_stride, const float* u
     const rs_status fs = check_filter(filter);
     if (fs != RS_OK) return fs;
     if (R < 0 || V <= 0 || k <= 0 || row_stride < V) return RS_ERR_INVALID_ARG;
-    if (V > RS_MAX_VOCAB || k > RS_MAX_CANDIDATES) return RS_ERR_UNSUPPORTED;
+    if (V > RS_MAX_VOCAB || k > RS_MAX_CANDIDATES || R > kMaxRows) return RS_ERR_UNSUPPORTED;
     if (R == 0) return RS_OK;
     if (!logits || !u || !out_token) return RS_ERR_INVALID_ARG;
     SParams P = row_params(logits, row_stride, R, V, filter);
@@ -1911,10 +1936,10 @@ rs_status resispec_sample(const void* logits, int64_t row_stride, const float* u
     P.kept = out_kept;
     P.status = out_status;
     const hipError_t e = with_rows(
-        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec, auto unr) {
-            set_slots<vec(), unr()>(P);
+        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec) {
+            set_slots<vec()>(P);
             return with_block(R, [&](auto block) {
-                hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), unr(), block(), false>), dim3((unsigned)R), dim3(block()),
+                hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), block(), false>), dim3((unsigned)R), dim3(block()),
                                    0, (hipStream_t)stream, P);
                 return hipGetLastError();
             });
@@ -1928,7 +1953,7 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
     const rs_status fs = check_filter(filter);
     if (fs != RS_OK) return fs;
     if (R < 0 || V <= 0 || row_stride < V || out_row_stride < V) return RS_ERR_INVALID_ARG;
-    if (V > RS_MAX_VOCAB) return RS_ERR_UNSUPPORTED;
+    if (V > RS_MAX_VOCAB || R > kMaxRows) return RS_ERR_UNSUPPORTED;
     if (R == 0) return RS_OK;
     if (!logits || !out) return RS_ERR_INVALID_ARG;
     SParams P = row_params(logits, row_stride, R, V, filter);
@@ -1938,10 +1963,10 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
     P.status = out_status;
     const RowLoads in = strided_loads(logits, row_stride, V, filter->logits_dtype);
     const RowLoads to = strided_loads(out, out_row_stride, V, filter->logits_dtype);
-    const hipError_t e = with_rows(filter->logits_dtype, in > to ? in : to, [&](auto in, auto vec, auto unr) {
-        set_slots<vec(), unr()>(P);
+    const hipError_t e = with_rows(filter->logits_dtype, in > to ? in : to, [&](auto in, auto vec) {
+        set_slots<vec()>(P);
         return with_block(R, [&](auto block) {
-            hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), unr(), block(), true>), dim3((unsigned)R),
+            hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), block(), true>), dim3((unsigned)R),
                                dim3(block()), 0, (hipStream_t)stream, P);
             return hipGetLastError();
         });
@@ -1958,7 +1983,7 @@ rs_status resispec_token_logprobs(const void* logits, int64_t row_stride, const 
     if (filter->top_ks || filter->top_ps || filter->min_ps || filter->top_k != 0 || filter->top_p != 1.0f ||
         filter->min_p != 0.0f)
         return RS_ERR_INVALID_ARG;
-    if (V > RS_MAX_VOCAB || k > RS_MAX_CANDIDATES) return RS_ERR_UNSUPPORTED;
+    if (V > RS_MAX_VOCAB || k > RS_MAX_CANDIDATES || R > kMaxRows) return RS_ERR_UNSUPPORTED;
     if (R == 0) return RS_OK;
     if (!logits || !tokens || !out_logprob) return RS_ERR_INVALID_ARG;
     SParams P = row_params(logits, row_stride, R, V, filter);
@@ -1968,10 +1993,10 @@ rs_status resispec_token_logprobs(const void* logits, int64_t row_stride, const 
     P.rank = out_rank;
     P.status = out_status;
     const hipError_t e = with_rows(
-        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec, auto unr) {
-            set_slots<vec(), unr()>(P);
+        filter->logits_dtype, strided_loads(logits, row_stride, V, filter->logits_dtype), [&](auto in, auto vec) {
+            set_slots<vec()>(P);
             return with_block(R, [&](auto block) {
-                hipLaunchKernelGGL((rs_logprob_kernel<decltype(in), vec(), unr(), block()>), dim3((unsigned)R), dim3(block()),
+                hipLaunchKernelGGL((rs_logprob_kernel<decltype(in), vec(), block()>), dim3((unsigned)R), dim3(block()),
                                    0, (hipStream_t)stream, P);
                 return hipGetLastError();
             });

@@ -1,4 +1,6 @@
-"""Sampling settings on rows of logits in plain 64-bit numpy, for the sampling tests."""
+"""Sampling settings on rows of logits in plain numpy, for the sampling tests: values and
+masses in 64 bits, sums of masses in 80 (a running sum of 33000 weights that each fall 1e-13 short of
+1 loses all of that in 64 bits, where one step is 3.6e-12, and with it the place of a cut)."""
 import numpy as np
 import torch
 
@@ -15,7 +17,7 @@ def kept(l, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
     T, top_p, min_p = (float(np.float32(x)) for x in (T, top_p, min_p))
     order = np.lexsort((np.arange(l.size), -l))
     order = order[np.isfinite(l[order])]
-    w = np.exp((l[order] - l[order[0]]) / T)
+    w = np.exp((l[order] - l[order[0]]) / T).astype(np.longdouble)
     n = order.size if top_k == 0 else min(top_k, order.size)
     if top_p < 1.0:
         total = w[:n].cumsum()
@@ -30,18 +32,18 @@ def draw(l, T, mask, u):
     """(token, log-probability) of the uniform u over the kept elements of the row l."""
     T = float(np.float32(T))
     a = (l - l[np.isfinite(l)].max()) / T
-    w = np.where(mask, np.exp(a), 0.0)
+    w = np.where(mask, np.exp(a).astype(np.longdouble), 0.0)
     c = w.cumsum()
     j = int(np.searchsorted(c, float(np.float32(u)) * c[-1], side="right"))
     j = min(j, int(np.flatnonzero(w > 0.0)[-1]))
-    return j, a[j] - np.log(c[-1])
+    return j, float(a[j] - np.log(c[-1]))
 
 
 def border(l, T, mask, u):
     """How far u times the kept mass is from the nearest border between two tokens, over
     that mass."""
     T = float(np.float32(T))
-    w = np.where(mask, np.exp((l - l[np.isfinite(l)].max()) / T), 0.0)
+    w = np.where(mask, np.exp((l - l[np.isfinite(l)].max()) / T).astype(np.longdouble), 0.0)
     c = w.cumsum()
     return np.abs(c - float(np.float32(u)) * c[-1]).min() / c[-1]
 

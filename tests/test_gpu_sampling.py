@@ -68,6 +68,58 @@ def test_sample_kinds_of_rows(gpu_lib, kind, dtype):
         check_sample(gpu_lib, rows, uniforms(3, 5, i), **s)
 
 
+KINDS = ["zipf", "flat", "peaked", "equal", "few", "masked", "lowest", "all-lowest", "large"]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", KINDS)
+def test_sample_kinds_of_long_rows(gpu_lib, kind, dtype):
+    """The same over vocabularies long enough for every way a cut is found."""
+    rows = make_rows(2, 70001, dtype, 2, kind)
+    for i, s in enumerate(SETTINGS):
+        check_sample(gpu_lib, rows, uniforms(2, 4, i), **s)
+
+
+@pytest.mark.parametrize("kind", ["zipf", "few", "lowest"])
+def test_sample_f32_rows_of_bf16_values(gpu_lib, kind):
+    """fp32 rows that hold many equal values, as logits cast from bf16 do: more of them at the
+    cut than are sorted."""
+    rows = make_rows(2, 131077, F32, 5, kind).bfloat16().float()
+    for i, s in enumerate(SETTINGS + [dict(top_p=0.99), dict(temperature=3.0, top_p=0.8), dict(top_k=30000)]):
+        check_sample(gpu_lib, rows, uniforms(2, 3, i), **s)
+    want, count = expected_filter(rows, [dict(top_p=0.99)] * 2)
+    out, n, st = gpu_lib.resispec_filter_logits(rows, top_p=0.99)
+    torch.cuda.synchronize()
+    assert same_bits(out, want) and n.tolist() == count
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_values_next_to_zero_and_far_from_it(gpu_lib, dtype):
+    """Values that share a place in the counts of a bf16 row: next to zero, and past a
+    thousand; and a maximum that the row's sample misses by far."""
+    g = np.random.default_rng(77)
+    V = 33000
+    tiny = torch.as_tensor(g.standard_normal((1, V)) * 1e-13, device="cuda")
+    mixed = torch.as_tensor(np.where(g.random((1, V)) < 0.3, 0.0, g.standard_normal((1, V)) * 1e-12), device="cuda")
+    signs = torch.as_tensor(np.where(g.random((1, V)) < 0.5, -0.0, 0.0), device="cuda")
+    far = torch.as_tensor(g.standard_normal((1, V)) * 3000.0, device="cuda")
+    low = torch.as_tensor(-2000.0 + 900.0 * g.standard_normal((1, V)), device="cuda")
+    lone = torch.as_tensor(g.standard_normal((1, V)), device="cuda")
+    lone[0, 12345] = 900.0
+    for x in (tiny, mixed, signs, far, low, lone):
+        rows = x.to(dtype)
+        for i, s in enumerate((dict(), dict(top_k=40), dict(top_p=0.9), dict(top_p=0.5, min_p=0.2), dict(top_k=9000),
+                               dict(temperature=1e-3, top_p=0.97), dict(temperature=300.0, top_p=0.6),
+                               dict(temperature=20.0, min_p=0.3))):
+            check_sample(gpu_lib, rows, uniforms(1, 3, i), **s)
+        each, t = row_settings(13)
+        many = rows.expand(13, V).contiguous()
+        want, count = expected_filter(many, each)
+        out, n, st = gpu_lib.resispec_filter_logits(many, **t)
+        torch.cuda.synchronize()
+        assert same_bits(out, want) and n.tolist() == count
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("V", [1, 2, 3, 4, 7, 8, 9, 63, 64, 65, 511, 512, 1023, 1025, 2047, 2048, 2049, 16384, 32001])
 def test_sample_sizes(gpu_lib, V, dtype):
@@ -153,10 +205,13 @@ def test_settings_of_each_sequence(gpu_lib):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-def test_rows_without_a_distribution(gpu_lib, dtype):
-    """NaN, +inf and rows of -inf are reported, and do not touch their neighbours."""
-    rows = make_rows(9, 4099, dtype, 6)
+@pytest.mark.parametrize("V", [4099, 70001])
+def test_rows_without_a_distribution(gpu_lib, V, dtype):
+    """NaN of either sign, +inf and rows of -inf are reported, and do not touch their
+    neighbours."""
+    rows = make_rows(9, V, dtype, 6)
     rows[1, 4098] = float("nan")
+    rows[3, V // 2] = -torch.tensor(float("nan"))
     rows[2, 0] = float("inf")
     rows[4] = float("-inf")
     rows[5] = float("nan")
@@ -170,11 +225,11 @@ def test_rows_without_a_distribution(gpu_lib, dtype):
     out, n, st = gpu_lib.resispec_filter_logits(rows, top_p=0.5)
     lpt, rank, st2 = gpu_lib.resispec_token_logprobs(rows, torch.zeros((9, 2), dtype=torch.int32, device="cuda"))
     torch.cuda.synchronize()
-    for r in (1, 2, 4, 5):
+    for r in (1, 2, 3, 4, 5):
         assert (out[r] == float("-inf")).all() and int(n[r]) == -1
         assert int(st[r]) == int(st2[r]) == gpu_lib.RS_SEQ_UNDERFLOW
         assert torch.isnan(lpt[r]).all() and (rank[r] == -1).all()
-    assert (st[[0, 3, 6, 7, 8]] == 0).all() and (st2[[0, 3, 6, 7, 8]] == 0).all()
+    assert (st[[0, 6, 7, 8]] == 0).all() and (st2[[0, 6, 7, 8]] == 0).all()
 
 
 def test_bad_uniforms_and_settings(gpu_lib):
@@ -221,9 +276,10 @@ def expected_filter(rows, each):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("kind", ["zipf", "equal", "few", "masked", "lowest", "all-lowest"])
-def test_filter_kinds_of_rows(gpu_lib, kind, dtype):
-    rows = make_rows(13, 5003, dtype, 11, kind)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("V", [5003, 70001])
+def test_filter_kinds_of_rows(gpu_lib, V, kind, dtype):
+    rows = make_rows(13, V, dtype, 11, kind)
     each, t = row_settings(13)
     want, count = expected_filter(rows, each)
     out, n, st = gpu_lib.resispec_filter_logits(rows, **t)
@@ -387,6 +443,40 @@ def test_empty_batches(gpu_lib):
     assert out.shape == (0, 100)
     lp, rank, st = gpu_lib.resispec_token_logprobs(x, torch.empty((0, 3), dtype=torch.int32, device="cuda"))
     assert lp.shape == (0, 3)
+
+
+def test_extreme_temperatures(gpu_lib):
+    """The smallest and largest temperatures, masked elements among the row's."""
+    for kind in ("zipf", "masked", "lowest"):
+        rows = make_rows(2, 9001, F32, 3, kind)
+        for T in (1e-45, 1e-38, 1e-6, 1e4, 1e30, 3.0e38):
+            for s in (dict(), dict(top_k=20), dict(top_p=0.7), dict(min_p=0.5)):
+                check_sample(gpu_lib, rows, uniforms(2, 2), temperature=T, **s)
+            tokens = torch.tensor([[5, 17], [9000, 0]], dtype=torch.int32, device="cuda")
+            lp, rank, st = gpu_lib.resispec_token_logprobs(rows, tokens, temperature=T)
+            torch.cuda.synchronize()
+            assert (st == 0).all()
+            for r in range(2):
+                for i in range(2):
+                    p, n = logprob(to64(rows)[r], T, int(tokens[r, i]))
+                    assert int(rank[r, i]) == n
+                    got = float(lp[r, i])
+                    assert got == -np.inf if p < -3.4e38 else abs(got - p) <= abs(p) * 2.0 ** -24 + 4.8e-6
+
+
+def test_many_short_rows(gpu_lib):
+    """A row of a few elements each, more rows than a grid has compute units by far; and the
+    first row count that is refused."""
+    R, V = 70000, 5
+    rows = make_rows(R, V, F32, 9)
+    tok, lp, n, st = gpu_lib.resispec_sample(rows, uniforms(R, 1), top_k=1)
+    out, n2, _ = gpu_lib.resispec_filter_logits(rows, top_k=2)
+    torch.cuda.synchronize()
+    assert torch.equal(tok[:, 0].long(), rows.argmax(1)) and (lp == 0).all() and (n == 1).all() and (n2 == 2).all()
+    assert (torch.isfinite(out).sum(1) == 2).all()
+    x = torch.zeros((1 << 23, 1), dtype=BF16, device="cuda")
+    with pytest.raises(gpu_lib.ResiSpecError):
+        gpu_lib.resispec_filter_logits(x)
 
 
 def test_binding_refusals(gpu_lib):
