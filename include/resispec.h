@@ -477,7 +477,8 @@ rs_status resispec_verify_tree_debug(const void* target_logits, const void* draf
  * order the finite elements by logit, equal ones by ascending index.  top_k keeps the first
  * top_k of that order; top_p, of what top_k keeps, the shortest prefix whose mass reaches
  * top_p times that of what top_k keeps; min_p those with w_j >= min_p (the maximum has w =
- * 1).  The first element is always kept.  All sums and comparisons are in 64 bits.
+ * 1).  The first element is always kept.  All sums and comparisons are in 64 bits, the
+ * exponentials to 4e-14 of their value.
  */
 typedef struct {
     int32_t logits_dtype;        /* rs_dtype */
@@ -542,7 +543,8 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
  *   tokens      : [R][k] int32; -1 = no token (the padding of resispec_verify_tree's
  *                 out_tokens): log-probability 0, rank 0
  *   filter      : the rows' type and temperature; its top_k, top_p and min_p must be off
- *   out_logprob : [R][k] fp32: (l_x - m) / T - ln sum_j exp((l_j - m) / T)
+ *   out_logprob : [R][k] fp32: (l_x - m) / T - ln sum_j exp((l_j - m) / T), its sum over
+ *                 32-bit exponentials (5e-6 off at most, 1e-7 or so on rows of logits)
  *   out_rank    : [R][k] int32, may be NULL: 1 + the number of elements before the token in
  *                 the order of rs_filter
  *   out_status  : [R] int32, may be NULL: RS_SEQ_BAD_TOKEN for an id outside [-1, V),

@@ -15,6 +15,17 @@ namespace {
 // with m the row's maximum and c = log2(e) / T, in fp64: a token or a cut is decided by the
 // side of a border that a sum over the whole row falls on, and of 1e5 borders one lies within
 // 1e-6 (what 32-bit exponentials give) of a draw now and then.
+//
+// What bounds the kernels.  A row is one workgroup's: a cut needs the row's sums before the
+// next pass begins, and a launch or a wait over compute units costs what most of these passes
+// take.  So a lone row runs at one compute unit's pace through its phases: 1 x 32,000 fp32
+// under top-p 29 us, 1 x 128,256 bf16 under top-k 50 21 us, where the bytes would take less
+// than 0.1.  Many rows are bound by memory: a filter is two reads and a write (33 x 32 rows of
+// 128,256 bf16 183 us, 836 MB, 4.6 TB/s; a copy reaches 4.7), a cut and its draws are two
+// reads (1024 x 151,936 bf16 under top-p 134 us, 583 MB fetched, 4.3 TB/s), a log-probability is
+// one (512 x 151,936 fp32, 20 tokens a row, 77-81 us, 311 MB, 3.8-4.0 TB/s; a sum reaches
+// 4.0).  fp32 rows under top-p take their two passes of fp64 exponentials instead: 256 x
+// 151,936 with a setting a row 106-117 us for 156 MB.
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
@@ -779,19 +790,21 @@ struct Row {
     // ---- rows whose kept elements are few, or whose values are many
 
     // The row's sample: the first elements of eight slots spread over it, whatever the
-    // workgroup's size, so that what is relative to it does not depend on that; two vectors
+    // workgroup's size, so that what is relative to it does not depend on that; 16 elements
     // for each lane of the first eight waves.
-    static constexpr int kSampleSlots = 8, kSampleLane = 2 * VEC, kSample = kSampleSlots * 64 * kSampleLane;
+    static constexpr int kSampleSlots = 8, kSampleVecs = VEC == 4 ? 4 : 2;
+    static constexpr int kSampleLane = kSampleVecs * VEC, kSample = kSampleSlots * 64 * kSampleLane;
     __device__ __forceinline__ void load_sample(float (&v)[kSampleLane]) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
 #pragma unroll
         for (int e = 0; e < kSampleLane; ++e) v[e] = -INFINITY;
         if (wid < kSampleSlots) {
             const int j = (int)((uint32_t)wid * (uint32_t)nslots / kSampleSlots) * G * CHUNK + lane * VEC;
-            typename W::raw t[2] = {W::template load_full<false>(row, min(j, V - VEC)),
-                                    W::template load_full<false>(row, min(j + 64 * VEC, V - VEC))};
+            typename W::raw t[kSampleVecs];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < kSampleVecs; ++u) t[u] = W::template load_full<false>(row, min(j + u * 64 * VEC, V - VEC));
+#pragma unroll
+            for (int u = 0; u < kSampleVecs; ++u) {
                 float x[VEC];
                 cut_off(t[u], j + u * 64 * VEC);
                 W::unpack(t[u], x);
@@ -812,11 +825,15 @@ struct Row {
         if (!(ref > -INFINITY && ref < INFINITY)) return false;
 #pragma unroll
         for (int e = 0; e < kSampleLane; ++e) {
-            const float b = (ref - v[e]) * kSampleBins;
-            if (b < (float)(kBins - 1)) atomicAdd(&sm.sample[(int)b], 1u);
+            const int b = sample_bin(ref, v[e]);
+            if (b < kBins - 1) atomicAdd(&sm.sample[b], 1u);
         }
         __syncthreads();
         return true;
+    }
+    // Bins below ref; what is above it is in the first, what is far below in the last.
+    __device__ __forceinline__ static int sample_bin(float ref, float l) {
+        return (int)fminf(fmaxf((ref - l) * kSampleBins, 0.0f), (float)(kBins - 1));
     }
     __device__ __forceinline__ float sample_max(const float (&v)[kSampleLane]) const {
         float mx = -INFINITY;
@@ -825,25 +842,60 @@ struct Row {
         return block_max(mx);
     }
 
-    // A threshold above which lie, going by the sample, `rank` of its elements; -inf where
-    // there is none.  Every wave finds the same.
-    __device__ __forceinline__ float threshold(float ref, float rank) const {
+    // The bin up to which a histogram below the sample's maximum counts `rank` elements; the
+    // last where it does not.  Every wave finds the same.
+    __device__ __forceinline__ int sample_rank(const uint32_t* counts, float rank) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
         constexpr int kSampleGroups = kBins / 64;
         static_assert(kSampleGroups <= 64 && kSampleGroups % kWaves == 0, "a lane a group");
 #pragma unroll
         for (int i = 0; i < kSampleGroups / kWaves; ++i) {
-            const int g = wid + i * kWaves, n = wave_sum_i((int)sm.sample[g * 64 + lane]);
+            const int g = wid + i * kWaves, n = wave_sum_i((int)counts[g * 64 + lane]);
             if (lane == 0) sm.group_sum[g] = (double)n;
         }
         __syncthreads();
         const double own = lane < kSampleGroups ? sm.group_sum[lane] : 0.0, incl = wave_incl_scan(own, lane);
         const uint64_t hit = __ballot(incl >= (double)rank);
-        if (!hit) return -INFINITY;
+        if (!hit) return kBins - 1;
         const int g = __ffsll((unsigned long long)hit) - 1;
-        const double in = readlane_d(incl - own, g) + wave_incl_scan((double)sm.sample[g * 64 + lane], lane);
-        const int at = g * 64 + __ffsll((unsigned long long)__ballot(in >= (double)rank)) - 1;
+        const double in = readlane_d(incl - own, g) + wave_incl_scan((double)counts[g * 64 + lane], lane);
+        return g * 64 + __ffsll((unsigned long long)__ballot(in >= (double)rank)) - 1;
+    }
+    // A threshold above which lie, going by the sample, `rank` of its elements; -inf where
+    // there is none.
+    __device__ __forceinline__ float threshold(float ref, float rank) const {
+        const int at = sample_rank(sm.sample, rank);
         return at < kBins - 1 ? ref - (float)(at + 1) / kSampleBins : -INFINITY;
+    }
+
+    // Takes from the list those of its n elements that are not among its first `rank` for sure:
+    // the bins' order is the elements'.  How many are left.
+    __device__ __forceinline__ int trim(int n, int rank, float ref) const {
+        const int tid = threadIdx.x;
+        constexpr int kEach = kSorted / BLOCK;
+        uint32_t* counts = reinterpret_cast<uint32_t*>(sm.sorted);
+        __syncthreads();
+        for (int i = tid; i < kBins / 4; i += BLOCK) reinterpret_cast<uint4*>(counts)[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) sm.nlist = 0;
+        __syncthreads();
+        uint64_t x[kEach];
+        int b[kEach];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const int i = tid + q * BLOCK;
+            b[q] = kBins;
+            if (i >= n) continue;
+            x[q] = sm.list[i];
+            b[q] = sample_bin(ref, value_of(~(uint32_t)(x[q] >> 32)));
+            atomicAdd(&counts[b[q]], 1u);
+        }
+        __syncthreads();
+        const int last = sample_rank(counts, (float)rank);
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (b[q] <= last) sm.list[atomicAdd(&sm.nlist, 1)] = x[q];
+        __syncthreads();
+        return sm.nlist;
     }
 
     // Adds a vector's elements that are at least tau, if any, to the list.
@@ -1005,8 +1057,11 @@ struct Row {
 
     // The cut of top_k, with top_p and min_p or without, or of min_p alone, where it keeps few
     // elements, in one pass: a sample of the row gives a threshold with some more elements
-    // above it, the pass lists those, and the sorted list is cut.  Left unsettled where they
-    // are too many or too few.  slots: sm.slot holds what is kept.
+    // above it, the pass lists those, and the sorted list is cut (min_p's needs no order).
+    // Left unsettled where they are too many or too few.  slots: sm.slot holds what is kept.
+    // 128,256 logits under top-k 50, 1 row and 512: bf16 draws 24 and 43 us (from the counts
+    // of values 31 and 55), filtered rows 27 and 72 (30 and 89), fp32 draws 25 and 57 (the
+    // search over keys takes 498 and 1360).
     __device__ __forceinline__ Search few(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
                                           bool& slots, int& kept) {
         constexpr float kRoom = 0.5f * (float)kSorted;
@@ -1045,13 +1100,34 @@ struct Row {
             gather(v, j, tau);
         }, [](int) {});
         if (__syncthreads_or(bad)) return kNone;
-        const int n = sm.nlist;
+        int n = sm.nlist;
         if (n > kSorted || n < 1 || (n < top_k && !floored)) return kUnsettled;
+        if (top_k == 0) {   // no order is needed
+            uint32_t lo = ~0u, hi = 0u;
+            for (int i = threadIdx.x; i < n; i += BLOCK) hi = max(hi, ~(uint32_t)(sm.list[i] >> 32));
+            range(lo, hi);
+            m = uniform(value_of(hi));
+            md = uniform((double)m);
+            cut = Cut{min_floor(min_p), INT_MAX};
+            const uint32_t last = ~key_of(cut.tau);
+            kept = bad = 0;
+            for (int i = threadIdx.x; i < n; i += BLOCK) {
+                const uint64_t e = sm.list[i];
+                const bool in = (uint32_t)(e >> 32) <= last;
+                kept += in;
+                sm.sorted[i] = in ? e : (uint64_t)~key_of(-INFINITY) << 32 | (uint32_t)e;
+            }
+            sum2(x, y, kept, bad);
+            slots = true;
+            add_to_slots<true>(n, mass_power(1.0));
+            return kFound;
+        }
+        if (n > kRanked) n = trim(n, top_k, ref);
         sort(n);
         m = uniform(sorted_value(0));
         md = uniform((double)m);
-        int keep = top_k > 0 ? min(n, top_k) : n;
-        if (top_k > 0 && top_p < 1.0) {
+        int keep = min(n, top_k);
+        if (top_p < 1.0) {
             prefix(keep);
             keep = min(keep, reach_running(keep, top_p * sm.running[keep - 1]) + 1);
         }
@@ -1066,7 +1142,8 @@ struct Row {
     // The cut of top_p alone, or of a top_k that keeps many elements: a histogram over linear
     // bins below the maximum says which bin the cut falls into, and a second pass sums what
     // lies above the bin and lists what is in it.  Left unsettled where that is too much to be
-    // sorted and not all one value, or the histogram's masses (whole numbers of 2^-40; sums of
+    // sorted and not all one value (128,256 fp32 logits under top-p, 1 row and 512: 75 and
+    // 154 us; the search over keys takes 451 and 1083), or the histogram's masses (whole numbers of 2^-40; sums of
     // floats take ten times as long in LDS) named a neighbour of the bin.  slots: sm.slot
     // holds what is kept.
     __device__ __forceinline__ Search search(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
@@ -1118,6 +1195,7 @@ struct Row {
             sum2(a, y, n, none);
             m = block_max(mx);
             if (__syncthreads_or(bad)) return kNone;
+            if (!by_mass) md = uniform((double)m);
             if (!by_mass && top_k >= n) {
                 cut = Cut{-INFINITY, -1};
                 slots = false;
@@ -1526,7 +1604,8 @@ __device__ __forceinline__ void store_raw(odd32* out, const uint4& t) {
 }
 __device__ __forceinline__ void store_raw(float* out, const uint4& t) { *reinterpret_cast<uint4*>(out) = t; }
 
-// One workgroup a row: the cut, then the draws or the filtered row.
+// One workgroup a row: the cut, then the draws or the filtered row.  4 waves a SIMD: with
+// room for 6 the compiler spills, and ran no faster.
 template <typename In, int VEC, int BLOCK, bool FILTER>
 __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) rs_sample_kernel(const SParams P) {
     __shared__ RowSmem sm;
@@ -1750,7 +1829,8 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
 // sample, in 32-bit exponentials (a log-probability is no border: its error is that of the
 // sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
 // vectors with an element that is not below every token take the count, a step a token.
-// Where the sum overflows or the sample is masked, a second pass against the maximum.
+// Where the sum overflows or the sample is masked, a second pass against the maximum.  640 rows
+// of 128,256 bf16: 46 us, 164 MB at 3.6 TB/s.
 template <typename In, int VEC, int BLOCK>
 __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
     __shared__ ReduceSmem sm;
@@ -1907,7 +1987,9 @@ auto with_rows(int dtype, RowLoads loads, F&& f) {
 }
 
 // Threads a row: 16 waves where every row has a CU to itself, two rows of 8 waves a CU where
-// there are more.
+// there are more.  128,256 bf16 logits, 16 waves and 8: 64 rows under top-p 43 and 48 us, 256
+// rows 47 and 50, 300 rows 83 and 73; log-probabilities 24 and 32, 25 and 33, 39 and 43, but of
+// 768 rows 70 and 56.
 constexpr int kCus = 256;
 template <typename F>
 auto with_block(int32_t R, F&& f) {

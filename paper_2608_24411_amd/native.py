@@ -748,6 +748,8 @@ def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
     for v, number, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
                              (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
         if not isinstance(v, torch.Tensor):
+            if number == "top_k" and not -1 << 31 <= v < 1 << 31:   # ctypes would keep its low 32 bits
+                raise ValueError("top_k must fit an int32, got %d" % v)
             setattr(f, number, v)
             continue
         if shape is None:

@@ -464,6 +464,21 @@ def test_extreme_temperatures(gpu_lib):
                     assert got == -np.inf if p < -3.4e38 else abs(got - p) <= abs(p) * 2.0 ** -24 + 4.8e-6
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 9001, 33000])
+def test_a_maximum_far_above_the_row(gpu_lib, V, dtype):
+    """One logit whose mass, against any other's, is past the range of 64 bits; at the places
+    where a sample of the row may miss it."""
+    x = np.random.default_rng([3, V]).standard_normal((6, V))
+    for r, j in enumerate((0, V // 16 + 100, V // 3, V // 2 - 1, 15 * V // 16, V - 1)):
+        x[r, j] = 900.0
+    rows = torch.as_tensor(x, device="cuda").to(dtype)
+    for i, s in enumerate((dict(), dict(top_k=1), dict(top_k=40), dict(top_k=V // 2), dict(top_k=V), dict(top_p=0.9),
+                           dict(min_p=1e-6), dict(top_k=V // 2, min_p=0.5), dict(top_k=60, top_p=0.5))):
+        for T in (1.0, 0.5, 1e-3):
+            check_sample(gpu_lib, rows, uniforms(6, 2, i), temperature=T, **s)
+
+
 def test_many_short_rows(gpu_lib):
     """A row of a few elements each, more rows than a grid has compute units by far; and the
     first row count that is refused."""

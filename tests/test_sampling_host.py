@@ -135,3 +135,12 @@ def test_plain_definition_on_a_row_worked_by_hand():
     assert [draw(l, 1.0, every, u)[0] for u in (0.0, 0.0999, 0.15, 0.35, 0.75, 0.95)] == [0, 0, 1, 2, 3, 4]
     assert abs(draw(l, 1.0, every, 0.35)[1] - np.log(0.4)) < 1e-12
     assert logprob(l, 1.0, 3)[1] == 3 and abs(logprob(l, 1.0, 3)[0] - np.log(0.2)) < 1e-12
+
+
+def test_binding_refuses_a_count_past_32_bits():
+    """ctypes keeps the low 32 bits: 2^32 would turn top-k off, 2^32 + 5 keep five."""
+    x = torch.zeros(2, 8)
+    for top_k in (1 << 31, 1 << 32, (1 << 32) + 5, -(1 << 31) - 1):
+        with pytest.raises(ValueError):
+            native._settings(x, x.shape[:1], 2, 1.0, top_k, 1.0, 0.0)
+    assert native._settings(x, x.shape[:1], 2, 1.0, (1 << 31) - 1, 1.0, 0.0).top_k == (1 << 31) - 1
