@@ -21,7 +21,8 @@ namespace {
 // take.  So a lone row runs at one compute unit's pace through its phases: 1 x 32,000 fp32
 // under top-p 29 us, 1 x 128,256 bf16 under top-k 50 21 us, where the bytes would take less
 // than 0.1.  Many rows are bound by memory: a filter is two reads and a write (33 x 32 rows of
-// 128,256 bf16 183 us, 836 MB, 4.6 TB/s; a copy reaches 4.7), a cut and its draws are two
+// 128,256 bf16 183 us, 836 MB, 4.6 TB/s; a copy reaches 4.7), one and a write where registers
+// hold the row (rs_floor_kernel), a cut and its draws are two
 // reads (1024 x 151,936 bf16 under top-p 134 us, 583 MB fetched, 4.3 TB/s), a log-probability is
 // one (512 x 151,936 fp32, 20 tokens a row, 77-81 us, 311 MB, 3.8-4.0 TB/s; a sum reaches
 // 4.0).  fp32 rows under top-p take their two passes of fp64 exponentials instead: 256 x
@@ -1825,6 +1826,68 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
     }
 }
 
+// Filtered rows under min-p alone, or under nothing, that fit the registers of a workgroup (64 of
+// the 128 that a lane has at 4 waves a SIMD): the maximum alone decides, so that a row is read
+// once, where the kernel above reads it again to write it.  1344 rows of 32,001 fp32 65 us
+// (344 MB, 5.3 TB/s), by the kernel above 102; of 128,256 bf16, which take 16 waves, 151 and
+// 200; one such row 15 and 23; no size measured from 8,000 up is slower.
+constexpr int kHeldVecs = 16;   // of a lane
+template <typename In, int VEC, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) rs_floor_kernel(const SParams P) {
+    __shared__ ReduceSmem sm;
+    constexpr int N = kHeldVecs;
+    const int tid = threadIdx.x;
+    const int64_t r = blockIdx.x;
+    const int64_t entry = r / P.rows_per_entry;
+    const float T = P.temperatures ? P.temperatures[entry] : P.temperature;
+    const float min_p = P.min_ps ? P.min_ps[entry] : P.min_p;
+    using RowT = Row<In, VEC, BLOCK, ReduceSmem>;
+    RowT row{reinterpret_cast<const In*>(P.logits) + r * P.stride, P.V, P.G, P.nslots, 0.0f, 0.0, 0.0, uniform((double)T), sm};
+    In* out = reinterpret_cast<In*>(P.out) + r * P.out_stride;
+    int status = RS_SEQ_OK, n = 0, none = 0, bad = 0;
+    if (!(T > 0.0f && T < INFINITY && min_p >= 0.0f && min_p <= 1.0f)) status = RS_SEQ_BAD_PARAM;
+    typename Vec<In, VEC>::raw t[N];
+    float mx = -INFINITY, floor = NAN;   // nothing is above a NaN
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i * BLOCK * VEC < P.V) t[i] = Vec<In, VEC>::template load_full<true>(row.row, min((i * BLOCK + tid) * VEC, P.V - VEC));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i * BLOCK * VEC >= P.V) continue;
+        row.cut_off(t[i], (i * BLOCK + tid) * VEC);
+        float v[VEC];
+        Vec<In, VEC>::unpack(t[i], v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            mx = fmaxf(mx, v[e]);
+            bad |= !(v[e] < INFINITY);
+        }
+    }
+    row.m = row.block_max(mx);
+    if ((__syncthreads_or(bad) || row.m == -INFINITY) && status == RS_SEQ_OK) status = RS_SEQ_UNDERFLOW;
+    if (status == RS_SEQ_OK) floor = min_p > 0.0f ? fmaxf(row.min_floor((double)min_p), -FLT_MAX) : -FLT_MAX;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i * BLOCK * VEC >= P.V) continue;
+        const int j = (i * BLOCK + tid) * VEC;
+        float v[VEC];
+        Vec<In, VEC>::unpack(t[i], v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const bool in = v[e] >= floor;
+            n += in;
+            v[e] = in ? v[e] : -INFINITY;
+        }
+        store_vec<In, VEC>(out, j, P.V, v);
+    }
+    double x = 0.0, y = 0.0;
+    row.sum2(x, y, n, none);
+    if (tid == 0) {
+        if (P.kept) P.kept[r] = status == RS_SEQ_OK ? n : -1;
+        if (P.status) P.status[r] = status;
+    }
+}
+
 // One workgroup a row, one pass: the sum of the row's masses against the highest element of its
 // sample, in 32-bit exponentials (a log-probability is no border: its error is that of the
 // sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
@@ -2045,8 +2108,17 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
     P.status = out_status;
     const RowLoads in = strided_loads(logits, row_stride, V, filter->logits_dtype);
     const RowLoads to = strided_loads(out, out_row_stride, V, filter->logits_dtype);
+    // only the numbers are known here: rows with arrays of top_k or top_p go the general way
+    const bool floors = !filter->top_ks && filter->top_k == 0 && !filter->top_ps && filter->top_p == 1.0f;
     const hipError_t e = with_rows(filter->logits_dtype, in > to ? in : to, [&](auto in, auto vec) {
         set_slots<vec()>(P);
+        if constexpr (vec() > 1)
+            if (floors && V <= kHeldVecs * 1024 * vec())
+                return with_block(V <= kHeldVecs * 512 * vec() ? R : 1, [&](auto block) {
+                    hipLaunchKernelGGL((rs_floor_kernel<decltype(in), vec(), block()>), dim3((unsigned)R), dim3(block()), 0,
+                                       (hipStream_t)stream, P);
+                    return hipGetLastError();
+                });
         return with_block(R, [&](auto block) {
             hipLaunchKernelGGL((rs_sample_kernel<decltype(in), vec(), block(), true>), dim3((unsigned)R),
                                dim3(block()), 0, (hipStream_t)stream, P);

@@ -310,6 +310,51 @@ def test_filter_sizes_strides_and_places(gpu_lib, V, dtype):
             assert torch.isnan(whole.view(13, V + pad)[:, V:]).all()
 
 
+HELD = {F32: [4, 31, 2047, 2048, 2049, 32767, 32768, 32769, 65535, 65536, 65537],
+        BF16: [8, 33, 4095, 4096, 4097, 65535, 65536, 65537, 131071, 131072, 131073]}
+
+
+@pytest.mark.parametrize("V, dtype", [(V, d) for d in HELD for V in HELD[d]], ids=str)
+def test_filter_under_min_p_alone(gpu_lib, V, dtype):
+    """Rows that registers hold, and the first that they do not: padded, in place, a setting a
+    row, faulted rows among them."""
+    R = 7
+    for i, (kind, pad, offset) in enumerate((("zipf", 0, 0), ("masked", 3, 1), ("lowest", 8, 0), ("few", 1, 5))):
+        rows = make_rows(R, V, dtype, 31 + i, kind, pad=pad, offset=offset)
+        for min_p in (0.0, 0.03, 1.0):
+            each = [dict(min_p=min_p)] * R
+            want, count = expected_filter(rows, each)
+            out, n, st = gpu_lib.resispec_filter_logits(rows, min_p=min_p)
+            torch.cuda.synchronize()
+            assert same_bits(out, want) and n.tolist() == count and (st == 0).all()
+        per_row = torch.linspace(0.001, 0.9, R, device="cuda")
+        warm = torch.linspace(0.3, 2.0, R, device="cuda")
+        want, count = expected_filter(rows, [dict(min_p=float(p), T=float(t)) for p, t in zip(per_row, warm)])
+        base = rows._base.clone() if rows._base is not None else rows.clone()
+        out, n, st = gpu_lib.resispec_filter_logits(rows, min_p=per_row, temperature=warm, out=rows)
+        torch.cuda.synchronize()
+        assert same_bits(out, want) and n.tolist() == count and (st == 0).all()
+        flat = rows._base if rows._base is not None else rows
+        if pad:      # what lies between the rows is as it was
+            between = torch.ones(flat.numel(), dtype=torch.bool, device="cuda")
+            between[offset:].view(R, V + pad)[:, :V] = False
+            assert same_bits(flat.flatten()[between], base.flatten()[between])
+    rows = make_rows(R, V, dtype, 40)
+    rows[1, V - 1] = float("nan")
+    rows[2, V // 2] = float("inf")
+    rows[3] = float("-inf")
+    rows[4, 0] = -torch.tensor(float("nan"))
+    per_row = torch.full((R,), 0.1, device="cuda")
+    per_row[5] = 1.5
+    out, n, st = gpu_lib.resispec_filter_logits(rows, min_p=per_row)
+    torch.cuda.synchronize()
+    bad, param = gpu_lib.RS_SEQ_UNDERFLOW, gpu_lib.RS_SEQ_BAD_PARAM
+    assert st.tolist() == [0, bad, bad, bad, bad, param, 0]
+    assert (out[1:6] == float("-inf")).all() and (n[1:6] == -1).all()
+    want, count = expected_filter(rows[[0, 6]], [dict(min_p=float(np.float32(0.1)))] * 2)
+    assert same_bits(out[[0, 6]], want) and n[[0, 6]].tolist() == count
+
+
 def test_filter_signed_zeros(gpu_lib):
     """-0 and +0 are equal in the order, and are written as they were."""
     for dtype in (F32, BF16):
