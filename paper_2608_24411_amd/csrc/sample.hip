@@ -19,14 +19,14 @@ namespace {
 // What bounds the kernels.  A row is one workgroup's: a cut needs the row's sums before the
 // next pass begins, and a launch or a wait over compute units costs what most of these passes
 // take.  So a lone row runs at one compute unit's pace through its phases: 1 x 32,000 fp32
-// under top-p 29 us, 1 x 128,256 bf16 under top-k 50 21 us, where the bytes would take less
+// under top-p 30 us, 1 x 128,256 bf16 under top-k 50 22 us, where the bytes would take less
 // than 0.1.  Many rows are bound by memory: a filter is two reads and a write (33 x 32 rows of
 // 128,256 bf16 183 us, 836 MB, 4.6 TB/s; a copy reaches 4.7), one and a write where registers
 // hold the row (rs_floor_kernel), a cut and its draws are two
 // reads (1024 x 151,936 bf16 under top-p 134 us, 583 MB fetched, 4.3 TB/s), a log-probability is
 // one (512 x 151,936 fp32, 20 tokens a row, 77-81 us, 311 MB, 3.8-4.0 TB/s; a sum reaches
 // 4.0).  fp32 rows under top-p take their two passes of fp64 exponentials instead: 256 x
-// 151,936 with a setting a row 106-117 us for 156 MB.
+// 151,936 with a setting a row 100-106 us for 156 MB.
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
@@ -1828,8 +1828,8 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
 
 // Filtered rows under min-p alone, or under nothing, that fit the registers of a workgroup (64 of
 // the 128 that a lane has at 4 waves a SIMD): the maximum alone decides, so that a row is read
-// once, where the kernel above reads it again to write it.  1344 rows of 32,001 fp32 65 us
-// (344 MB, 5.3 TB/s), by the kernel above 102; of 128,256 bf16, which take 16 waves, 151 and
+// once, where the kernel above reads it again to write it.  1344 rows of 32,001 fp32 68 us
+// (344 MB, 5.1 TB/s), by the kernel above 102; of 128,256 bf16, which take 16 waves, 151 and
 // 200; one such row 15 and 23; no size measured from 8,000 up is slower.
 constexpr int kHeldVecs = 16;   // of a lane
 template <typename In, int VEC, int BLOCK>
@@ -1893,7 +1893,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
 // sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
 // vectors with an element that is not below every token take the count, a step a token.
 // Where the sum overflows or the sample is masked, a second pass against the maximum.  640 rows
-// of 128,256 bf16: 46 us, 164 MB at 3.6 TB/s.
+// of 128,256 bf16: 47 us, 164 MB at 3.5 TB/s.
 template <typename In, int VEC, int BLOCK>
 __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
     __shared__ ReduceSmem sm;
