@@ -480,6 +480,34 @@ def test_captured_and_replayed(gpu_lib, R):
         torch.randn(1 << 20, device="cuda").sum().item()
 
 
+@pytest.mark.parametrize("dtype, V", [(F32, 20011), (F32, 60001), (BF16, 128257)], ids=str)
+def test_min_p_alone_captured_and_on_other_streams(gpu_lib, dtype, V):
+    """Rows that registers hold, filtered in place in a replayed graph and by two streams at
+    once; and the cut of a batch is that of its rows alone."""
+    rows = make_rows(300, V, dtype, 51)
+    work = rows.clone()
+    want, count = expected_filter(rows[:3], [dict(min_p=0.05, T=0.8)] * 3)
+    whole, n0, _ = gpu_lib.resispec_filter_logits(rows, min_p=0.05, temperature=0.8)
+    torch.cuda.synchronize()
+    assert same_bits(whole[:3], want) and n0[:3].tolist() == count
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, n, st = gpu_lib.resispec_filter_logits(work, min_p=0.05, temperature=0.8, out=work)
+    for _ in range(3):
+        work.copy_(rows)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same_bits(work, whole) and torch.equal(n, n0) and (st == 0).all()
+        torch.randn(1 << 20, device="cuda").sum().item()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    parts = [gpu_lib.resispec_filter_logits(rows[i:i + 100], min_p=0.05, temperature=0.8, stream=streams[i // 100])
+             for i in (0, 100)]
+    torch.cuda.synchronize()
+    for i, (out, m, _) in enumerate(parts):
+        assert same_bits(out, whole[100 * i:100 * i + 100]) and torch.equal(m, n0[100 * i:100 * i + 100])
+
+
 def test_empty_batches(gpu_lib):
     x = torch.empty((0, 100), device="cuda")
     tok, lp, n, st = gpu_lib.resispec_sample(x, torch.empty((0, 2), device="cuda"))
