@@ -612,8 +612,11 @@ struct Row {
     }
 
     // The cut of top_k and top_p from the counts of a row's values.  Where it falls among the
-    // values below all bins, the search ends it.
-    __device__ __forceinline__ Ties cut_values(int top_k, double top_p) const {
+    // values below all bins, the search ends it, whose histogram lies over the counts: nothing
+    // reads those of a cut down there.  With min_p (`floored`) there is no such cut: its floor
+    // is above -1020 (min_p is at least 2^-149, and count_values has seen 2^-150 there) and the
+    // counts say what it keeps, so the elements below the bins need no order.
+    __device__ __forceinline__ Ties cut_values(int top_k, double top_p, bool floored) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
         const bool want_mass = top_p < 1.0;
         // lane i: the count of the wave's i-th group, and then its mass
@@ -641,7 +644,7 @@ struct Row {
             // into the last bin, which holds -inf too; it has no mass, so top_p cuts above it
             int below = 0, none = 0;
             double x = 0.0, y = 0.0;
-            if (!want_mass) {
+            if (!want_mass && !floored) {
                 each([&](float l, int) { below += l > -INFINITY && l <= bin_value(kLastBin); });
                 sum2(x, y, below, none);
                 if (all + below > top_k)
@@ -1644,7 +1647,7 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         if constexpr (kCounts) {
             if (found == Row<In, VEC, BLOCK>::kUnsettled) {
                 counts = row.count_values(bad);
-                if (counts && filters) ties = row.cut_values(top_k, (double)top_p);
+                if (counts && filters) ties = row.cut_values(top_k, (double)top_p, min_p > 0.0f);
             }
         }
         if (bad || found == Row<In, VEC, BLOCK>::kNone) {
