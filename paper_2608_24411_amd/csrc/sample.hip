@@ -1037,24 +1037,34 @@ struct Row {
         return lo;
     }
     // Adds the masses of sm.sorted[0 .. n) to the slots' sums (CLEAR: which were none), as
-    // whole numbers of 2^power, so that their order does not count; none is above 2^52 of them.
+    // whole numbers, so that their order does not count.  Each slot's unit goes by the largest
+    // mass in it, which is between 2^51 and 2^52 of them (below the normal range, where the
+    // exponent field is 0, a mass is a whole number of the smallest one): with one unit for
+    // all, a slot of elements 2^-52 below the row's maximum would hold no mass, and a draw of
+    // u = 0 would pass over them.
     template <bool CLEAR>
-    __device__ __forceinline__ void add_to_slots(int n, int power) const {
+    __device__ __forceinline__ void add_to_slots(int n) const {
         const int tid = threadIdx.x;
         unsigned long long* sums = reinterpret_cast<unsigned long long*>(sm.running);
+        int* field = reinterpret_cast<int*>(sums + kRowSlots);   // the largest mass's exponent field
+        auto slot_of = [&](int i) { return (uint32_t)sm.sorted[i] / (uint32_t)(G * CHUNK); };
         __syncthreads();
-        for (int i = tid; i < kRowSlots; i += BLOCK) sums[i] = 0;
+        for (int i = tid; i < kRowSlots; i += BLOCK) {
+            sums[i] = 0;
+            field[i] = 0;
+        }
         __syncthreads();
-        for (int i = tid; i < n && power > -1000; i += BLOCK)
-            atomicAdd(&sums[(uint32_t)sm.sorted[i] / (uint32_t)(G * CHUNK)],
-                      (unsigned long long)(__builtin_ldexp(mass(sorted_value(i)), -power) + 0.5));
+        for (int i = tid; i < n; i += BLOCK) atomicMax(&field[slot_of(i)], __double2hiint(mass(sorted_value(i))) >> 20);
+        __syncthreads();
+        for (int i = tid; i < n; i += BLOCK) {
+            const int at = slot_of(i);
+            atomicAdd(&sums[at], (unsigned long long)(__builtin_ldexp(mass(sorted_value(i)), 1074 - field[at]) + 0.5));
+        }
         __syncthreads();
         for (int i = tid; i < nslots; i += BLOCK)
-            sm.slot[i] = (CLEAR ? 0.0 : sm.slot[i]) + __builtin_ldexp((double)sums[i], power);
+            sm.slot[i] = (CLEAR ? 0.0 : sm.slot[i]) + __builtin_ldexp((double)sums[i], field[i] - 1074);
         __syncthreads();
     }
-    // For masses of at most w (far below zero where w has none).
-    __device__ __forceinline__ static int mass_power(double w) { return ilogb(w) + 1 - 52; }
 
     // kTied: the cut's value is known, and how many of the elements equal to it are kept
     enum Search { kFound, kTied, kNone, kUnsettled };
@@ -1123,7 +1133,7 @@ struct Row {
             }
             sum2(x, y, kept, bad);
             slots = true;
-            add_to_slots<true>(n, mass_power(1.0));
+            add_to_slots<true>(n);
             return kFound;
         }
         if (n > kRanked) n = trim(n, top_k, ref);
@@ -1139,7 +1149,7 @@ struct Row {
         cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
         kept = keep;
         slots = want_slots;
-        if (want_slots) add_to_slots<true>(keep, mass_power(1.0));
+        if (want_slots) add_to_slots<true>(keep);
         return kFound;
     }
 
@@ -1277,7 +1287,7 @@ struct Row {
         cut = Cut{sorted_value(keep - 1), (int)(uint32_t)sm.sorted[keep - 1]};
         kept = by_mass ? keep + above : top_k;
         slots = want_slots && by_mass && !(min_p > 0.0 && min_floor(min_p) > cut.tau);
-        if (slots) add_to_slots<false>(keep, mass_power(mass(sorted_value(0))));
+        if (slots) add_to_slots<false>(keep);
         return kFound;
     }
     __device__ __forceinline__ static int linear_bin(float l, float ref) {
@@ -1361,7 +1371,7 @@ struct Row {
                     if (tie) atomicAdd(&sm.ties[(uint32_t)x / (uint32_t)(G * CHUNK)], 1);
                     sm.sorted[i] = tie ? (uint64_t)~key_of(-INFINITY) << 32 | (uint32_t)x : x;
                 }
-                add_to_slots<true>(all, -51);
+                add_to_slots<true>(all);
                 return true;
             }
             for (int i = tid; i <= end - top + 1; i += BLOCK)
