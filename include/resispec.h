@@ -478,7 +478,8 @@ rs_status resispec_verify_tree_debug(const void* target_logits, const void* draf
  * top_k of that order; top_p, of what top_k keeps, the shortest prefix whose mass reaches
  * top_p times that of what top_k keeps; min_p those with w_j >= min_p (the maximum has w =
  * 1).  The first element is always kept.  All sums and comparisons are in 64 bits, the
- * exponentials to 4e-14 of their value.
+ * exponentials to 4e-14 of their value; below 2^-1023, under the 64-bit type's normal range,
+ * one may be zero, and its element then has no mass.
  */
 typedef struct {
     int32_t logits_dtype;        /* rs_dtype */

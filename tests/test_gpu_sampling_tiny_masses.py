@@ -2,13 +2,18 @@
 the first kept element with any mass, whichever way the cut was found.  Against the plain
 definition (sampling_util), whose running sums begin with those masses and hold them; draws
 are compared where u times the total lies far from every border (0, or less than a tenth or
-more than ten times any running sum before the row's maximum)."""
+more than ten times any running sum before the row's maximum).
+
+The range of the masses.  64-bit numbers have 2^-1022 as their smallest normal one; numpy's
+exponential goes on below it, with fewer and fewer bits, to 2^-1075, the kernels' is zero from
+2^-1023 on (the exponent field of 2^x is x + 1023, and there is none below 0).  rs_filter says
+so: such masses count as none.  An element has one where (l - m) / T < -1023 ln 2 = -709.09;
+among the rows below that is 12.33 and less at T = 0.008, and no element within 1e-6 of it."""
 import numpy as np
 import pytest
 import torch
 
 from sampling_util import draw, kept, to64
-from test_gpu_sampling import check_sample
 
 pytestmark = pytest.mark.gpu
 
@@ -24,6 +29,23 @@ def rows_with_a_peak(V, dtype, seed):
     x[2, [7, 700, V // 2]] = 12.75, 14.0, 14.5
     x[:, 2 * V // 3] = 18.0
     return torch.as_tensor(x, device="cuda").to(dtype)
+
+
+def check_draws(native, rows, u, s):
+    """One call against the definition, masses below 2^-1023 of the maximum counting as none."""
+    tok, lp, n, st = native.resispec_sample(rows, u, **s)
+    torch.cuda.synchronize()
+    l, uu, T = to64(rows), u.cpu().numpy(), s["temperature"]
+    for r in range(rows.shape[0]):
+        mask = kept(l[r], **{"T" if k == "temperature" else k: v for k, v in s.items()})
+        assert int(st[r]) == native.RS_SEQ_OK and int(n[r]) == mask.sum()
+        x = (l[r] - l[r].max()) / float(np.float32(T)) / np.log(2.0)
+        assert (np.abs(x + 1023.0) > 1e-6).all()
+        for i in range(u.shape[1]):
+            j, p = draw(l[r], T, mask & (x > -1023.0), uu[r, i])
+            assert int(tok[r, i]) == j, (r, int(tok[r, i]), j, uu[r, i])
+            # half a step of the result, and the 64-bit sums
+            assert abs(float(lp[r, i]) - p) <= abs(p) * 2.0 ** -24 + 1e-12
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
@@ -46,7 +68,7 @@ def test_draws_among_tiny_masses(gpu_lib, T, V, dtype):
                 # a border within a factor of ten: the sums' rounding may decide
                 near = ((before > x / 10.0) & (before < x * 10.0)).any()
                 u[r, i] = 0.0 if near else x
-        check_sample(gpu_lib, rows, torch.as_tensor(u, device="cuda"), **s)
+        check_draws(gpu_lib, rows, torch.as_tensor(u, device="cuda"), s)
 
 
 def test_the_first_kept_token_whatever_the_search(gpu_lib):
