@@ -283,7 +283,7 @@ struct Row {
         }
     }
 
-    // Sums over the workgroup in a fixed order, to every thread.
+    // Sums over the workgroup in an order fixed by its size, to every thread.
     __device__ __forceinline__ void sum2(double& a, double& b, int& p, int& q) const {
         const int lane = threadIdx.x & 63, wid = wave_id();
         const double wa = wave_sum(a), wb = wave_sum(b);
@@ -308,6 +308,55 @@ struct Row {
         b = uniform(b);
         p = __builtin_amdgcn_readfirstlane(p);
         q = __builtin_amdgcn_readfirstlane(q);
+    }
+    // Sums of masses in an order that does not depend on the workgroup's size: that of kMaxWaves
+    // waves, of which a wave takes kParts, its own number and those kWaves apart.  Cuts follow
+    // from them, and one on a border (a share of the mass to the last bit) would fall on
+    // another side of it in another batch.
+    static constexpr int kParts = kMaxWaves / kWaves;
+    static_assert(kParts * kWaves == kMaxWaves, "whole parts");
+    __device__ __forceinline__ double sum_parts(const double (&v)[kParts]) const {
+        const int lane = threadIdx.x & 63, wid = wave_id();
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) {
+            const double t = wave_sum(v[q]);
+            if (lane == 0) sm.red[0][wid + q * kWaves] = t;
+        }
+        __syncthreads();
+        double a = 0.0;
+        for (int w = 0; w < kMaxWaves; ++w) a += sm.red[0][w];
+        return uniform(a);
+    }
+    // Sums of what body(l, a, b) adds to a and b over the row's elements, one a load.
+    template <typename Body>
+    __device__ __forceinline__ void sum_each(Body&& body, double& a, double& b) const {
+        using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
+        const int lane = threadIdx.x & 63, wid = wave_id();
+        __syncthreads();
+#pragma unroll 1
+        for (int q = 0; q < kParts; ++q) {
+            double x = 0.0, y = 0.0;
+            for (int j = threadIdx.x + q * BLOCK; j < V; j += kMaxWaves * 64) {
+                float v[1];
+                load_vec<E, 1>(reinterpret_cast<const E*>(row), j, V, v);
+                body(v[0], x, y);
+            }
+            x = wave_sum(x);
+            y = wave_sum(y);
+            if (lane == 0) {
+                sm.red[0][wid + q * kWaves] = x;
+                sm.red[1][wid + q * kWaves] = y;
+            }
+        }
+        __syncthreads();
+        a = b = 0.0;
+        for (int w = 0; w < kMaxWaves; ++w) {
+            a += sm.red[0][w];
+            b += sm.red[1][w];
+        }
+        a = uniform(a);
+        b = uniform(b);
     }
     __device__ __forceinline__ float block_max(float v) const {
         v = wave_max(v);
@@ -416,11 +465,10 @@ struct Row {
             int turned = 0;   // which way the search has gone
             for (;;) {
                 // what lies above the bin, what in it, and the range of the keys in it
-                mass_a = mass_in = 0.0;
                 na = nin = 0;
                 kmin = ~0u;
                 kmax = 0u;
-                each([&](float l, int) {
+                sum_each([&](float l, double& up, double& inside) {
                     const uint32_t k = key_of(l);
                     if (!(l > -INFINITY) || k < lo) return;
                     const int b = k > hi ? -1 : (int)((hi - k) >> shift);
@@ -428,15 +476,16 @@ struct Row {
                     const double w = MASS || want_mass ? mass(l) : 0.0;
                     if (b < bin) {
                         ++na;
-                        mass_a += w;
+                        up += w;
                     } else {
                         ++nin;
-                        mass_in += w;
+                        inside += w;
                         kmin = min(kmin, k);
                         kmax = max(kmax, k);
                     }
-                });
-                sum2(mass_a, mass_in, na, nin);
+                }, mass_a, mass_in);
+                double none = 0.0, none2 = 0.0;
+                sum2(none, none2, na, nin);
                 range(kmin, kmax);
                 a = MASS ? mass_a : (double)na;
                 in = MASS ? mass_in : (double)nin;
@@ -1000,7 +1049,8 @@ struct Row {
     // Running sums of the masses of sm.sorted[0 .. n) into sm.running.
     __device__ __forceinline__ void prefix(int n) const {
         const int tid = threadIdx.x, lane = tid & 63, wid = wave_id();
-        const int per = (n + BLOCK - 1) / BLOCK;
+        static_assert(BLOCK >= 512, "as many elements a thread in every workgroup");
+        const int per = (n + 511) / 512;
         double own = 0.0;
         for (int q = 0; q < per; ++q)
             if (tid * per + q < n) own += mass(sorted_value(tid * per + q));
@@ -1177,7 +1227,7 @@ struct Row {
             for (int i = tid; i < kLinearBins / 2; i += BLOCK) reinterpret_cast<ulonglong2*>(sm.bins)[i] = make_ulonglong2(0, 0);
             __syncthreads();
             float mx = -INFINITY;
-            double a = 0.0, y = 0.0;
+            double a = 0.0, parts[kParts] = {};
             int n = 0, bad = 0;
             auto add = [&](float l, uint64_t q) {
                 atomicAdd(reinterpret_cast<unsigned long long*>(&sm.bins[linear_bin(l, ref)]), (unsigned long long)q);
@@ -1193,7 +1243,10 @@ struct Row {
                         // the low bits of 2^52 + w 2^40 are the mass in its units
                         add(v[e], __double_as_longlong(fma(w, 1.0 / kMassUnit, 0x1p52)) & 0xfffffffffffffull);
                     }
-                }, [](int) {});
+                }, [&](int s) {
+                    parts[s / kWaves % kParts == 0 ? 0 : kParts - 1] += a;
+                    a = 0.0;
+                });
             } else {
                 sweep<false>([&](const float(&v)[VEC], int) {
 #pragma unroll
@@ -1205,8 +1258,13 @@ struct Row {
                     }
                 }, [](int) {});
             }
-            int none = 0;
-            sum2(a, y, n, none);
+            if (by_mass) {
+                a = sum_parts(parts);
+            } else {
+                double y = 0.0;
+                int none = 0;
+                sum2(a, y, n, none);
+            }
             m = block_max(mx);
             if (__syncthreads_or(bad)) return kNone;
             if (!by_mass) md = uniform((double)m);
@@ -1678,11 +1736,8 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
                 if (cuts_k) ties = row.template select<false>((double)top_k, lo, hi, 0.0, top_p < 1.0f, mass);
                 if (top_p < 1.0f) {
                     if (!cuts_k) {
-                        double a = 0.0, b = 0.0;
-                        int x = 0, y = 0;
-                        row.each([&](float l, int) { a += row.mass(l); });
-                        row.sum2(a, b, x, y);
-                        mass = a;
+                        double none = 0.0;
+                        row.sum_each([&](float l, double& a, double&) { a += row.mass(l); }, mass, none);
                     }
                     ties = row.template select<true>((double)top_p * mass, lo, hi, 0.0, false, mass);
                 }
