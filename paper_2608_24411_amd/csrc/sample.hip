@@ -1104,11 +1104,21 @@ struct Row {
             field[i] = 0;
         }
         __syncthreads();
-        for (int i = tid; i < n; i += BLOCK) atomicMax(&field[slot_of(i)], __double2hiint(mass(sorted_value(i))) >> 20);
+        double w[kSorted / BLOCK];
+#pragma unroll
+        for (int q = 0; q < kSorted / BLOCK; ++q) {
+            const int i = tid + q * BLOCK;
+            if (i >= n) break;
+            w[q] = mass(sorted_value(i));
+            atomicMax(&field[slot_of(i)], __double2hiint(w[q]) >> 20);
+        }
         __syncthreads();
-        for (int i = tid; i < n; i += BLOCK) {
-            const int at = slot_of(i);
-            atomicAdd(&sums[at], (unsigned long long)(__builtin_ldexp(mass(sorted_value(i)), 1074 - field[at]) + 0.5));
+#pragma unroll
+        for (int q = 0; q < kSorted / BLOCK; ++q) {
+            const int i = tid + q * BLOCK;
+            if (i >= n) break;
+            const uint32_t at = slot_of(i);
+            atomicAdd(&sums[at], (unsigned long long)(__builtin_ldexp(w[q], 1074 - field[at]) + 0.5));
         }
         __syncthreads();
         for (int i = tid; i < nslots; i += BLOCK)
