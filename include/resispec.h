@@ -545,7 +545,10 @@ rs_status resispec_filter_logits(const void* logits, int64_t row_stride, int32_t
  *                 out_tokens): log-probability 0, rank 0
  *   filter      : the rows' type and temperature; its top_k, top_p and min_p must be off
  *   out_logprob : [R][k] fp32: (l_x - m) / T - ln sum_j exp((l_j - m) / T), its sum over
- *                 32-bit exponentials (5e-6 off at most, 1e-7 or so on rows of logits)
+ *                 32-bit exponentials against the highest of a sample of the row and of the
+ *                 row's tokens: 1e-7 or so off on rows of logits, 3e-6 at most where one of
+ *                 these is the row's maximum, and 1.7e-5 at most where the maximum is far above
+ *                 them all (resispec_sample's are from 64-bit sums); never above 0
  *   out_rank    : [R][k] int32, may be NULL: 1 + the number of elements before the token in
  *                 the order of rs_filter
  *   out_status  : [R] int32, may be NULL: RS_SEQ_BAD_TOKEN for an id outside [-1, V),

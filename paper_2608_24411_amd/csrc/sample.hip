@@ -1899,7 +1899,8 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
         const int token = row.draw(P.u[r * P.k + i], total, cut, l);
         if (lane == 0) {
             P.token[r * P.k + i] = token;
-            if (P.logprob) P.logprob[r * P.k + i] = (float)(((double)l - row.md) / (double)T - log(total));
+            // not above 0, where the sums' last bits would say so
+            if (P.logprob) P.logprob[r * P.k + i] = (float)fmin(((double)l - row.md) / (double)T - log(total), 0.0);
         }
     }
 }
@@ -1967,11 +1968,13 @@ __global__ void __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4)))
 }
 
 // One workgroup a row, one pass: the sum of the row's masses against the highest element of its
-// sample, in 32-bit exponentials (a log-probability is no border: its error is that of the
-// sum, 1e-7 or so), and for every token how many elements come before it in the order.  Only
-// vectors with an element that is not below every token take the count, a step a token.
-// Where the sum overflows or the sample is masked, a second pass against the maximum.  640 rows
-// of 128,256 bf16: 47 us, 164 MB at 3.5 TB/s.
+// sample and of the tokens, in 32-bit exponentials (a log-probability is no border: its error
+// is that of the sum, 1e-7 or so, and 1.6e-5 at most, where the row's maximum is 2^127 above
+// both: the exponent, up to 128, is rounded three times).  That element's own term is exactly
+// 1, and no token is above it, so no log-probability is above 0.  For every token, how many
+// elements come before it in the order: only vectors with an element that is not below every
+// token take the count, a step a token.  Where the sum overflows or the sample is masked, a
+// second pass against the maximum.  640 rows of 128,256 bf16: 47 us, 164 MB at 3.5 TB/s.
 template <typename In, int VEC, int BLOCK>
 __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
     __shared__ ReduceSmem sm;
@@ -1999,12 +2002,17 @@ __global__ void __launch_bounds__(BLOCK) rs_logprob_kernel(const SParams P) {
             token_rank[tid] = 0;
         }
         __syncthreads();
-        float lowest = INFINITY;
-        for (int i = 0; i < P.k; ++i) lowest = fminf(lowest, token_logit[i]);
+        // the tokens' lowest logit, and their highest
+        float lowest = INFINITY, highest = -INFINITY;
+        for (int i = 0; i < P.k; ++i) {
+            const float l = token_logit[i];
+            lowest = fminf(lowest, l);
+            highest = fmaxf(highest, l < INFINITY ? l : -INFINITY);
+        }
         lowest = uniform(P.rank ? lowest : INFINITY);
         float v0[RowT::kSampleLane];
         row.load_sample(v0);
-        float ref = row.sample_max(v0);
+        float ref = fmaxf(row.sample_max(v0), highest);
         if (!(ref > -INFINITY && ref < INFINITY)) ref = 0.0f;
         // c in two parts, both above zero: a -inf element's exponent is -inf, not a NaN
         float ch = (float)fmin(row.c, (double)FLT_MAX);
