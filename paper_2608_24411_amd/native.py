@@ -739,6 +739,15 @@ def _rows(t, name):
     return t.data_ptr(), step, shape[:-1], R, V
 
 
+def _overlap(a, a_step, b, b_step, R, V, size):
+    """Whether R rows of V elements of `size` bytes at a and b, one step apart, may share
+    memory.  Rows of one step can lie between each other (two halves of each row of a
+    tensor); of different steps, their whole ranges must be apart."""
+    if R == 0 or a + ((R - 1) * a_step + V) * size <= b or b + ((R - 1) * b_step + V) * size <= a:
+        return False
+    return a_step != b_step or not V * size <= (b - a) % (a_step * size) <= (a_step - V) * size
+
+
 def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
     """rs_filter of settings that are numbers, or device tensors with an entry a row ([R] or
     [B, N]) or a sequence ([B])."""
@@ -843,10 +852,8 @@ def resispec_filter_logits(logits, *, temperature=1.0, top_k=0, top_p=1.0, min_p
             raise TypeError("out must be %s" % logits.dtype)
         if y.get_device() != logits.get_device():
             raise ValueError("all tensors must be on one device, got %s" % {y.device, dev})
-        if R and not (to == ptr and to_step == step):
-            size = logits.element_size()
-            if to < ptr + ((R - 1) * step + V) * size and ptr < to + ((R - 1) * to_step + V) * size:
-                raise ValueError("out must not overlap logits, unless it is the same rows")
+        if not (to == ptr and to_step == step) and _overlap(ptr, step, to, to_step, R, V, logits.element_size()):
+            raise ValueError("out must not overlap logits, unless it is the same rows")
         kept = torch.empty(lead, dtype=torch.int32, device=dev) if out_kept is None else out_kept
         st = torch.empty(lead, dtype=torch.int32, device=dev) if out_status is None else out_status
         _check(lib.resispec_filter_logits(ptr, step, R, V, ctypes.byref(f), to, to_step,
