@@ -17,16 +17,17 @@ namespace {
 // 1e-6 (what 32-bit exponentials give) of a draw now and then.
 //
 // What bounds the kernels.  A row is one workgroup's: a cut needs the row's sums before the
-// next pass begins, and a launch or a wait over compute units costs what most of these passes
-// take.  So a lone row runs at one compute unit's pace through its phases: 1 x 32,000 fp32
-// under top-p 30 us, 1 x 128,256 bf16 under top-k 50 22 us, where the bytes would take less
-// than 0.1.  Many rows are bound by memory: a filter is two reads and a write (33 x 32 rows of
-// 128,256 bf16 183 us, 836 MB, 4.6 TB/s; a copy reaches 4.7), one and a write where registers
-// hold the row (rs_floor_kernel), a cut and its draws are two
-// reads (1024 x 151,936 bf16 under top-p 134 us, 583 MB fetched, 4.3 TB/s), a log-probability is
-// one (512 x 151,936 fp32, 20 tokens a row, 77-81 us, 311 MB, 3.8-4.0 TB/s; a sum reaches
-// 4.0).  fp32 rows under top-p take their two passes of fp64 exponentials instead: 256 x
-// 151,936 with a setting a row 100-106 us for 156 MB.
+// next pass begins.  So a lone row runs at one compute unit's pace through its phases: 1 x
+// 32,000 fp32 under top-p 30 us, 1 x 128,256 bf16 under top-k 50 23 us, where the bytes would
+// take less than 0.1.  With many rows a filter is two reads and a write (33 x 32 rows of 128,256
+// bf16 178 us, 837 MB, 4.7 TB/s, a copy's rate), one and a write where registers hold the row
+// (rs_floor_kernel), a cut and its draws are two reads (1024 x 151,936 bf16 under top-p 138 us,
+// 581 MB fetched, 4.2 TB/s), a log-probability is one (512 x 151,936 fp32, 20 tokens a row,
+// 79-85 us, 311 MB, 3.7-4.0 TB/s).  Rows that are only read, without a pause, come at 6 to 7
+// TB/s on this card, so the last two are not at the rate of memory, nor at that of the vector
+// ALU (56 % and 43 % of the time).  A batch with a setting a row waits for its slowest rows:
+// 256 x 151,936 fp32 101-110 us, where its rows under top-p alone, whose histogram takes an
+// fp64 exponential an element, need 101 to 122 and the others 37 to 51.
 
 constexpr int kRowSlots = 256;      // runs of chunks with sums of their own
 constexpr int kBins = 2048;         // histogram bins of a search for a cut
@@ -844,7 +845,8 @@ struct Row {
 
     // The row's sample: the first elements of eight slots spread over it, whatever the
     // workgroup's size, so that what is relative to it does not depend on that; 16 elements
-    // for each lane of the first eight waves.
+    // for each lane of the first eight waves.  The first run begins the row: a vocabulary whose
+    // likely tokens crowd there is over-counted, and few() gives up on it (below).
     static constexpr int kSampleSlots = 8, kSampleVecs = VEC == 4 ? 4 : 2;
     static constexpr int kSampleLane = kSampleVecs * VEC, kSample = kSampleSlots * 64 * kSampleLane;
     __device__ __forceinline__ void load_sample(float (&v)[kSampleLane]) const {
@@ -1133,9 +1135,12 @@ struct Row {
     // elements, in one pass: a sample of the row gives a threshold with some more elements
     // above it, the pass lists those, and the sorted list is cut (min_p's needs no order).
     // Left unsettled where they are too many or too few.  slots: sm.slot holds what is kept.
-    // 128,256 logits under top-k 50, 1 row and 512: bf16 draws 24 and 43 us (from the counts
-    // of values 31 and 55), filtered rows 27 and 72 (30 and 89), fp32 draws 25 and 57 (the
-    // search over keys takes 498 and 1360).
+    // 128,256 logits under top-k 50, 1 row and 512: bf16 draws 24 and 45 us (from the counts
+    // of values 31 and 55), filtered rows 27 and 72 (30 and 89), fp32 draws 24 and 59 (the
+    // search over keys takes 498 and 1360).  What is left to others for their number alone:
+    // the threshold's margin passes kRoom from a top_k of about 560 on (V 32,000: 790), and
+    // bf16 rows then take 40 and 68 us, fp32 rows under top_p too 545 and 1540.  For too few:
+    // where likely tokens crowd into the first 1024, 41 and 77 us, and 513 and 1350.
     __device__ __forceinline__ Search few(int top_k, double top_p, double min_p, bool want_slots, Cut& cut,
                                           bool& slots, int& kept) {
         constexpr float kRoom = 0.5f * (float)kSorted;
@@ -2135,10 +2140,13 @@ auto with_rows(int dtype, RowLoads loads, F&& f) {
     return with_layout(dtype, loads, [&](auto in, auto vec, auto) { return f(in, vec); });
 }
 
-// Threads a row: 16 waves where every row has a CU to itself, two rows of 8 waves a CU where
-// there are more.  128,256 bf16 logits, 16 waves and 8: 64 rows under top-p 43 and 48 us, 256
-// rows 47 and 50, 300 rows 83 and 73; log-probabilities 24 and 32, 25 and 33, 39 and 43, but of
-// 768 rows 70 and 56.
+// Threads a row: 16 waves where every row has a CU to itself, 8 where there are more, so that a
+// CU holds two rows or more (registers allow the draws two, the filter of bf16 rows three, the
+// log-probabilities four).  128,256 bf16 logits, 16 waves and 8: 64 rows under top-p 44 and 48
+// us, 256 rows 48 and 51, 300 rows 83 and 73, 768 rows 127 and 111; filtered 38 and 48, 46 and
+// 52, 81 and 68, 145 and 131; log-probabilities 24 and 32, 25 and 33, 39 and 43, 70 and 57.
+// Those alone would take 16 waves up to some 350 rows (400: 47 and 44); one rule for all costs
+// them a tenth between.
 constexpr int kCus = 256;
 template <typename F>
 auto with_block(int32_t R, F&& f) {
