@@ -443,8 +443,11 @@ struct Row {
     // The cut at which the order's prefix reaches `target`, its number of elements (MASS
     // false) or its mass, known to lie among the keys from lo to hi, with `above` of the
     // target's units above them.  Bins of a histogram narrow the range until one value is
-    // left; the mass above a bin is summed in fp64 in a fixed order, and the histogram's
-    // 32-bit sums only say where to look.  `total_mass`: of the prefix, where wanted.
+    // left; the histogram's 32-bit sums, whose order is not fixed, only say where to look.  The
+    // mass above a bin and the mass down to its end are summed in fp64 over the same elements
+    // in the same order as the next bin's, so that each is the other to the last bit and one
+    // bin alone has the target between the two, wherever the search began.  `total_mass`: of
+    // the prefix, where wanted.
     template <bool MASS>
     __device__ __forceinline__ Ties select(double target, uint32_t lo, uint32_t hi, double above, bool want_mass,
                                            double& total_mass) const {
@@ -460,36 +463,36 @@ struct Row {
                     unsafeAtomicAdd(&sm.hist[(hi - k) >> shift], MASS ? (float)mass(l) : 1.0f);
             });
             int bin = crossing(above, target);
-            double a, in, mass_a, mass_in;
+            double a, end, mass_a, mass_end;
             int na, nin;
             uint32_t kmin, kmax;
             int turned = 0;   // which way the search has gone
             for (;;) {
-                // what lies above the bin, what in it, and the range of the keys in it
+                // what lies above the bin, what down to its end, and the range of the keys in it
                 na = nin = 0;
                 kmin = ~0u;
                 kmax = 0u;
-                sum_each([&](float l, double& up, double& inside) {
+                sum_each([&](float l, double& up, double& upto) {
                     const uint32_t k = key_of(l);
                     if (!(l > -INFINITY) || k < lo) return;
                     const int b = k > hi ? -1 : (int)((hi - k) >> shift);
                     if (b > bin) return;
                     const double w = MASS || want_mass ? mass(l) : 0.0;
+                    upto += w;
                     if (b < bin) {
                         ++na;
                         up += w;
                     } else {
                         ++nin;
-                        inside += w;
                         kmin = min(kmin, k);
                         kmax = max(kmax, k);
                     }
-                }, mass_a, mass_in);
+                }, mass_a, mass_end);
                 double none = 0.0, none2 = 0.0;
                 sum2(none, none2, na, nin);
                 range(kmin, kmax);
                 a = MASS ? mass_a : (double)na;
-                in = MASS ? mass_in : (double)nin;
+                end = MASS ? mass_end : (double)na + (double)nin;
                 // the 32-bit sums may have named a neighbour of the bin
                 if (MASS && a >= target && turned <= 0) {
                     int b = bin - 1;
@@ -500,7 +503,7 @@ struct Row {
                         continue;
                     }
                 }
-                if (MASS && a + in < target && turned >= 0) {
+                if (MASS && end < target && turned >= 0) {
                     int b = bin + 1;
                     while (b < kBins && sm.hist[b] == 0.0f) ++b;
                     if (b < kBins) {
