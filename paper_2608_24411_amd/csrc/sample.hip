@@ -1291,7 +1291,8 @@ struct Row {
                 slots = false;
                 return kFound;
             }
-            // the units' 52 bits hold masses below 2^12
+            // the units' 52 bits hold masses below 2^12 (thousands of them in one bin pass its
+            // 64 bits, and the bin found may be any: the second pass, which sums anew, says so)
             if (by_mass && ((double)m - md) * c > 10.0) {
                 ref = m;
                 continue;

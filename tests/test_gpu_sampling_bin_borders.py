@@ -5,6 +5,9 @@ import numpy as np
 import pytest
 import torch
 
+from sampling_util import kept, to64
+from test_gpu_sampling import check_sample, uniforms
+
 pytestmark = pytest.mark.gpu
 
 
@@ -52,3 +55,29 @@ def test_cuts_between_two_bins(gpu_lib, V, high, top_k, spread):
             assert torch.equal(part[0], first[0][lo:hi])
     # copies of a row in one batch
     assert (first[1].view(-1, 50) == first[1][:50]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("noise", [1e-4, 2e-3, 0.3])
+def test_bins_whose_sums_pass_64_bits(gpu_lib, noise, dtype):
+    """Nearly all of a row lies 6.8 above the eight runs that are its sample: masses of 2^9.8
+    against the sample's maximum, 2^49.8 units each, 140,000 of them in a few bins."""
+    V = 151936
+    g = np.random.default_rng([111, int(noise * 1e5)])
+    x = 6.8 + noise * np.abs(g.standard_normal((2, V)))
+    x = np.minimum(x, 6.9)
+    unit = 512 if dtype == torch.float32 else 1024          # elements of a chunk, 256 slots at most
+    slots = -(-V // unit)
+    per = -(-slots // 256)
+    slots = -(-slots // per)
+    for w in range(8):
+        at = w * slots // 8 * per * unit
+        x[:, at:at + 1024] = -0.01 * g.random((2, len(x[0, at:at + 1024])))
+    rows = torch.as_tensor(x, device="cuda").to(dtype)
+    for i, s in enumerate((dict(top_p=0.9), dict(top_p=0.3), dict(top_p=1.0 - 2.0 ** -24), dict(top_p=1e-6),
+                           dict(top_k=30000), dict(top_p=0.5, min_p=0.999), dict())):
+        check_sample(gpu_lib, rows, uniforms(2, 3, i), **s)
+        mask = np.stack([kept(l, **s) for l in to64(rows)])
+        out, n, st = gpu_lib.resispec_filter_logits(rows, **s)
+        torch.cuda.synchronize()
+        assert (torch.isfinite(out).cpu().numpy() == mask).all() and n.tolist() == mask.sum(1).tolist()
