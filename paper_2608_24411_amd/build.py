@@ -5,6 +5,7 @@ import re
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -16,7 +17,7 @@ PROBE_LIB = os.path.join(HERE, "libresispec_probe.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Wall", "-Wno-unused-function",
     # packed fp32 instructions stay off: ordinary fp32 code only
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -65,36 +66,56 @@ def _scratch_users(asm_text):
     return users
 
 
+def _object(src, work, extra):
+    """Compile one source in a folder of its own: (object, command, result, scratch users or
+    None where no device assembly was found)."""
+    where = os.path.join(work, os.path.basename(src) + ".d")
+    os.mkdir(where)
+    obj = os.path.join(where, "out.o")
+    # -save-temps keeps the device assembly for the scratch check
+    cmd = ([HIPCC, "-c"] + FLAGS + list(extra) + ["-Rpass-analysis=kernel-resource-usage", "-save-temps",
+                                                  "-I", os.path.join(ROOT, "include"), "-o", obj, src])
+    r = subprocess.run(cmd, capture_output=True, text=True, cwd=where)
+    asm = [os.path.join(where, f) for f in os.listdir(where)
+           if f.endswith(".s") and "amdgcn" in f and "gfx950" in f]
+    users = set()
+    for path in asm:
+        with open(path) as fh:
+            users |= _scratch_users(fh.read())
+    return obj, cmd, r, users if asm else None
+
+
 def _compile(srcs, lib, verbose, extra=()):
+    """The sources side by side, then the library from their objects."""
     tmp = lib + ".tmp%d" % os.getpid()
-    # -save-temps keeps the device assembly (in a scratch directory) for the scratch check
-    cmd = ([HIPCC] + FLAGS + list(extra) + ["-Rpass-analysis=kernel-resource-usage", "-save-temps",
-                                            "-I", os.path.join(ROOT, "include"), "-o", tmp] + srcs)
-    if verbose:
-        print(" ".join(cmd), flush=True)
     with tempfile.TemporaryDirectory() as work:
-        r = subprocess.run(cmd, capture_output=True, text=True, cwd=work)
-        asm = [os.path.join(work, f) for f in os.listdir(work)
-               if f.endswith(".s") and "amdgcn" in f and "gfx950" in f]
-        users = set()
-        for path in asm:
-            with open(path) as fh:
-                users |= _scratch_users(fh.read())
-    other = [l for l in r.stderr.splitlines()
-             if "kernel-resource-usage" not in l and "packed-fp32-ops" not in l and l.strip()]
-    if r.returncode != 0:
-        sys.stderr.write("\n".join(other) + "\n")
-        raise subprocess.CalledProcessError(r.returncode, cmd)
-    if verbose and other:
-        print("\n".join(other), flush=True)
-    # A register spilled inside a branch that only some lanes take is stored for those
-    # lanes alone; a value that other lanes still hold would come back from stale
-    # scratch.  Every kernel is built to fit its registers, and the build checks it.
-    bad = _spills(r.stderr, users if asm else None)
-    if bad:
-        os.remove(tmp)
-        raise RuntimeError("registers spill to scratch in: " +
-                           ", ".join("%s (%d VGPRs, %d B/lane)" % b for b in bad))
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            parts = list(pool.map(lambda src: _object(src, work, extra), srcs))
+        bad, failed = [], None
+        for obj, cmd, r, users in parts:
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            other = [l for l in r.stderr.splitlines()
+                     if "kernel-resource-usage" not in l and "packed-fp32-ops" not in l and l.strip()]
+            if r.returncode != 0:
+                sys.stderr.write("\n".join(other) + "\n")
+                failed = failed or subprocess.CalledProcessError(r.returncode, cmd)
+                continue
+            if verbose and other:
+                print("\n".join(other), flush=True)
+            # A register spilled inside a branch that only some lanes take is stored for those
+            # lanes alone; a value that other lanes still hold would come back from stale
+            # scratch.  Every kernel is built to fit its registers, and the build checks it.
+            bad += _spills(r.stderr, users)
+        if failed:
+            raise failed
+        if bad:
+            raise RuntimeError("registers spill to scratch in: " +
+                               ", ".join("%s (%d VGPRs, %d B/lane)" % b for b in bad))
+        cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + list(extra) + ["-o", tmp] + [p[0] for p in parts]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
     os.replace(tmp, lib)
 
 
