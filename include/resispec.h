@@ -79,8 +79,11 @@ typedef enum {
                                     rejected its one candidate, or is a leaf, and its draw
                                     is left to the walk (resispec_walk_draw), which makes it
                                     only where a walk ends */
-    RS_SEQ_BAD_PARAM = 10        /* rows with sampling settings of their own (rs_filter): one
-                                    of them is out of its range */
+    RS_SEQ_BAD_PARAM = 10,       /* rows with sampling settings of their own (rs_filter): one
+                                    of them is out of its range; a sequence's score, length,
+                                    count or parent is */
+    RS_SEQ_BAD_PAGE = 11,        /* a page number or slot outside the cache */
+    RS_SEQ_NO_ROOM = 12          /* resispec_plan_cache: not enough free pages, or slots */
 } rs_seq_status;
 
 typedef enum { RS_MODE_RESISPEC = 0, RS_MODE_SPECINFER = 1 } rs_mode;
@@ -560,6 +563,183 @@ rs_status resispec_token_logprobs(const void* logits, int64_t row_stride, const 
                                   int32_t R, int32_t V, int32_t k, const rs_filter* filter,
                                   float* out_logprob, int32_t* out_rank, int32_t* out_status,
                                   void* stream);
+
+/*
+ * Where rows of `row_bytes` bytes lie: the row of (o, p, i, t) starts at base +
+ * o * outer_stride + p * page_stride + i * inner_stride + t * position_stride (bytes).  States
+ * by beam: p is the beam, t its position.  A paged cache: p is the page, t the position in it,
+ * and slot p * positions + t is the row's place in the cache.  `outer` are layers, keys and
+ * values; `inner` what lies between a page and its positions (heads).  Strides may be larger
+ * than what they step over; rows do not overlap.
+ */
+typedef struct {
+    int64_t outer, pages, inner, positions, row_bytes;    /* >= 1 each */
+    int64_t outer_stride, page_stride, inner_stride, position_stride;
+} rs_rows;
+
+/*
+ * Beam search's choice: of all continuations of a sequence's W beams the k best.
+ *   logits      : [B * W] rows of V elements, `row_stride` (>= V) elements from row to row; the
+ *                 rows of beams that are not there or have ended are not read
+ *   scores      : [B][W] fp32, the log-probability of each beam so far; -inf: there is no such
+ *                 beam (a first step has one)
+ *   ended       : [B][W] bytes, may be NULL; nonzero: the beam has ended
+ *   end_token   : the token of an ended beam's continuation
+ *   filter      : the rows' type and temperature; its top_k, top_p and min_p must be off (rows
+ *                 cut by resispec_filter_logits are taken as they are)
+ * A live beam w goes on with every token v whose logit is finite, at the score
+ * (l_v - m) / T - ln sum_j exp((l_j - m) / T) + scores[w], m the row's maximum; an ended one
+ * with end_token alone, at its own score.  The order is by score, equal ones by beam, within a
+ * beam by logit and then by token.  It is decided in 64 bits, by sums of exponentials to 4e-14
+ * of their value.
+ *   out_parent, out_token : [B][k] int32, the best first: the beam, in [0, W), and the token; -1
+ *                 past the last continuation
+ *   out_score   : [B][k] fp32, its score (that of a 32-bit sum, 1e-6 off at most besides the
+ *                 rounding of the result); -inf past the last
+ *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_UNDERFLOW: a live beam's row has
+ *                 no finite logit, or a NaN or +inf; RS_SEQ_BAD_PARAM: a score that is NaN or
+ *                 +inf, or a temperature out of its range.  Such a sequence's parents and tokens
+ *                 are -1 and its scores NaN.
+ *   workspace   : device buffer of at least resispec_beam_workspace_bytes(B, W, V) bytes,
+ *                 16-byte aligned; contents on entry are ignored.  Calls that overlap on one
+ *                 workspace race.
+ * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, V, W or k <= 0, k > W * V, row_stride < V, or a
+ * number in `filter` out of its range; RS_ERR_UNSUPPORTED for V > RS_MAX_VOCAB, W or k >
+ * RS_MAX_CANDIDATES or B * W >= 2^23; RS_ERR_WORKSPACE.  B = 0 is a no-op.  A sequence's
+ * outputs depend on its rows, scores and ends alone, not on the batch.
+ */
+rs_status resispec_beam_select(const void* logits, int64_t row_stride, const float* scores,
+                               const uint8_t* ended, int32_t end_token, int32_t B, int32_t W,
+                               int32_t V, int32_t k, const rs_filter* filter,
+                               int32_t* out_parent, int32_t* out_token, float* out_score,
+                               int32_t* out_status, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* Workspace bytes resispec_beam_select needs (0 if a size is out of its range). */
+size_t resispec_beam_workspace_bytes(int32_t B, int32_t W, int32_t V);
+
+/*
+ * The states of the chosen beams: for all k at once, dst[b][k] = src[b][parent[b][k]].
+ *   src, src_rows : states of B * W beams (pages = B * W), of `positions` positions each
+ *   dst, dst_rows : those of B * K beams; outer, inner, positions and row_bytes as src_rows.
+ *                 `dst` may be `src` with the same layout (then K = W): the states change
+ *                 places; it must not overlap it otherwise
+ *   parent      : [B][K] int32 in [0, W); -1: that state of dst stays as it is
+ *   lengths     : [B] int32, may be NULL: only the first lengths[b] positions are moved
+ *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_PARAM: a parent or a length
+ *                 out of its range; nothing of that sequence is moved.
+ * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, W or K <= 0, or layouts that do not fit;
+ * RS_ERR_UNSUPPORTED for W or K > RS_MAX_CANDIDATES, or 2^31 rows of one beam and layer or
+ * more.  B = 0 is a no-op.
+ */
+rs_status resispec_beam_reorder(const void* src, const rs_rows* src_rows, void* dst,
+                                const rs_rows* dst_rows, const int32_t* parent,
+                                const int32_t* lengths, int32_t B, int32_t W, int32_t K,
+                                int32_t* out_status, void* stream);
+
+/*
+ * The same for beams whose positions lie in the pages of a cache: position t of beam n is in
+ * page table[n][t / P] at t % P, P = positions.
+ *   src_table, dst_table : [B * W] and [B * K] rows of int32 page numbers, `src_table_stride`
+ *                 and `dst_table_stride` entries from row to row, `max_pages` entries each
+ *   dst         : may be `src` with the same layout.  A row of dst may then also be one of src,
+ *                 if it is so at the same position of the same sequence (one table given twice;
+ *                 beams that share the pages of their prompt), and not otherwise.
+ *   lengths     : [B] int32, at most max_pages * P
+ *   out_status  : RS_SEQ_BAD_PARAM as above; RS_SEQ_BAD_PAGE: a page number outside the cache;
+ *                 the rows that it is for are not moved
+ * Errors as resispec_beam_reorder.
+ */
+rs_status resispec_beam_reorder_paged(const void* src, const rs_rows* src_rows,
+                                      const int32_t* src_table, int64_t src_table_stride,
+                                      void* dst, const rs_rows* dst_rows,
+                                      const int32_t* dst_table, int64_t dst_table_stride,
+                                      int32_t max_pages, const int32_t* parent,
+                                      const int32_t* lengths, int32_t B, int32_t W, int32_t K,
+                                      int32_t* out_status, void* stream);
+
+/*
+ * Pages and slots of a step's new rows in a paged cache.  Request r keeps its first kept[r]
+ * positions and is given added[r] more; it needs want = ceil((kept + added) / page_size) pages
+ * and holds the first held[r] entries of its row of the block table.  Pages past `want` go onto
+ * the stack of free pages, requests in order and each request's in table order; then requests
+ * in order take from its top what they lack.
+ *   kept, added, held : [R] int32.  A finished request keeps 0 and is given 0; a new one holds 0.
+ *   block_table : [R] rows of int32 page numbers, `table_stride` entries from row to row,
+ *                 `max_pages` entries each; pages taken are entered, entries past those held
+ *                 are left as they were
+ *   free_pages  : [num_pages] int32 stack of page numbers in [0, num_pages), of which the first
+ *                 free_count[0] are free; in and out
+ *   out_held, out_free_count : [R], [1] int32; may be `held` and `free_count`
+ *   out_starts  : [R + 1] int32, the running sum of added: request r's new rows are
+ *                 out_starts[r] .. out_starts[r + 1] - 1
+ *   out_slots   : [T] int32, the slot page * page_size + position % page_size of each new row;
+ *                 -1 past the last row and where a request has been refused
+ *   out_positions, out_requests : [T] int32, may be NULL: the position in its request of each
+ *                 row, and the request; -1 as above
+ *   out_status  : [R] int32 rs_seq_status, may be NULL.  RS_SEQ_NO_ROOM: there are not enough
+ *                 free pages (for it and all requests before it), or its rows pass T;
+ *                 RS_SEQ_BAD_PARAM: a negative number, more pages than max_pages, or a stack
+ *                 that would hold more than num_pages.  Such a request is refused: it keeps what
+ *                 it holds.  RS_SEQ_BAD_PAGE: a page number outside [0, num_pages); its rows'
+ *                 slots are -1.
+ * A request with RS_SEQ_BAD_PARAM for its own numbers counts as given no rows in out_starts; a
+ * refused one counts with its rows.
+ * RS_ERR_INVALID_ARG for a NULL pointer, R < 0, T < 0, page_size, num_pages or max_pages <= 0, or
+ * table_stride < max_pages; RS_ERR_UNSUPPORTED for num_pages * page_size or max_pages *
+ * page_size >= 2^31.  R = 0 sets out_starts[0], out_free_count and the padding.
+ */
+rs_status resispec_plan_cache(const int32_t* kept, const int32_t* added, const int32_t* held,
+                              int32_t R, int32_t page_size, int32_t* block_table,
+                              int64_t table_stride, int32_t max_pages, int32_t* free_pages,
+                              const int32_t* free_count, int32_t num_pages, int32_t* out_held,
+                              int32_t* out_free_count, int32_t* out_starts, int32_t T,
+                              int32_t* out_slots, int32_t* out_positions,
+                              int32_t* out_requests, int32_t* out_status, void* stream);
+
+/*
+ * The accepted nodes of verified trees: the way from the root down whose nodes carry the
+ * accepted tokens.
+ *   parent, node_token : [B][N] int32, as for resispec_verify_tree
+ *   tokens, accepted_len : [B][max_depth + 1] and [B] int32, its outputs; accepted_len -1 (a
+ *                 fault) gives no path
+ *   out_path    : [B][max_depth + 1] int32: 0 (the root), then the accepted nodes, -1 after the
+ *                 last.  Where nodes of several ways carry the same tokens, the way that ends at
+ *                 the lowest node.
+ *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_TREE: a malformed parent
+ *                 array, or no way carries the tokens; RS_SEQ_DEPTH_EXCEEDED: accepted_len
+ *                 outside [-1, max_depth].  Such a sequence has no path.
+ * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, N <= 0 or max_depth < 0; RS_ERR_UNSUPPORTED for
+ * N > RS_MAX_PATH_NODES.  B = 0 is a no-op.
+ */
+#define RS_MAX_PATH_NODES 8192
+rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_token,
+                                 const int32_t* tokens, const int32_t* accepted_len, int32_t B,
+                                 int32_t N, int32_t max_depth, int32_t* out_path,
+                                 int32_t* out_status, void* stream);
+
+/*
+ * The accepted rows at their places in the cache: node path[b][i] was given slot
+ * slots[b][path[b][i]] for the verification and belongs at slots[b][i], behind the i accepted
+ * nodes before it.  For every b and i up to the path's first -1:
+ *   cache[slots[b][i]] = source row (page b, position path[b][i]), or, if source is NULL,
+ *   cache[slots[b][i]] = cache[slots[b][path[b][i]]], all i at once.
+ *   cache, cache_rows : the paged cache
+ *   slots       : [B][N] int32; the slots of one call's nodes differ from each other
+ *   path        : [B][depth] int32, nodes in ascending order, -1 after the last
+ *   source, source_rows : NULL, or the rows of the trees' nodes outside the cache (pages = B,
+ *                 positions = N; outer, inner and row_bytes as cache_rows); must not overlap it
+ *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_TREE: a path that does not
+ *                 ascend or has a node outside [0, N); RS_SEQ_BAD_PAGE: a slot of it outside
+ *                 the cache.  Nothing of that sequence is moved.
+ * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, N or depth <= 0, or layouts that do not fit;
+ * RS_ERR_UNSUPPORTED for N or depth > RS_MAX_PATH_NODES or pages * positions >= 2^31.  B = 0 is a
+ * no-op.
+ */
+rs_status resispec_commit_path(void* cache, const rs_rows* cache_rows, const int32_t* slots,
+                               const int32_t* path, const void* source,
+                               const rs_rows* source_rows, int32_t B, int32_t N, int32_t depth,
+                               int32_t* out_status, void* stream);
 
 /* Static description of a status code. */
 const char* resispec_status_string(int32_t status);

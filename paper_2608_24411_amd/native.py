@@ -6,6 +6,7 @@ runs in the library's kernels.  There is no fallback: if the library cannot be l
 the import fails.
 """
 import ctypes
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -15,10 +16,11 @@ LIB_PATH = os.environ.get("RESISPEC_LIBRARY") or os.path.join(HERE, "libresispec
 RS_OK, RS_ERR_INVALID_ARG, RS_ERR_WORKSPACE, RS_ERR_UNSUPPORTED, RS_ERR_HIP = range(5)
 (RS_SEQ_OK, RS_SEQ_BAD_TOKEN, RS_SEQ_ZERO_DRAFT, RS_SEQ_UNDERFLOW, RS_SEQ_BAD_TREE,
  RS_SEQ_BAD_UNIFORM, RS_SEQ_DEPTH_EXCEEDED, RS_SEQ_TOO_MANY_CHILDREN, RS_SEQ_GROUP_TIMEOUT,
- RS_SEQ_DEFERRED, RS_SEQ_BAD_PARAM) = range(11)
+ RS_SEQ_DEFERRED, RS_SEQ_BAD_PARAM, RS_SEQ_BAD_PAGE, RS_SEQ_NO_ROOM) = range(13)
 RS_MODE_RESISPEC, RS_MODE_SPECINFER = 0, 1
 RS_F32, RS_BF16 = 0, 1
 RS_MAX_CANDIDATES = 64
+RS_MAX_PATH_NODES = 8192
 
 MODES = {"resispec": RS_MODE_RESISPEC, "specinfer": RS_MODE_SPECINFER}
 
@@ -36,7 +38,9 @@ EXPORTS = ("resispec_verify", "resispec_verify_tree", "resispec_verify_tree_noal
            "resispec_verify_nodes", "resispec_walk", "resispec_node_outcomes",
            "resispec_workspace_bytes", "resispec_validate_tree_host",
            "resispec_verify_tree_debug", "resispec_sample", "resispec_filter_logits",
-           "resispec_token_logprobs", "resispec_status_string", "resispec_abi_version")
+           "resispec_token_logprobs", "resispec_beam_select", "resispec_beam_workspace_bytes",
+           "resispec_beam_reorder", "resispec_beam_reorder_paged", "resispec_plan_cache",
+           "resispec_accepted_path", "resispec_commit_path", "resispec_status_string", "resispec_abi_version")
 
 
 class RsParams(ctypes.Structure):
@@ -51,6 +55,12 @@ class RsFilter(ctypes.Structure):
                 ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
                 ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
                 ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p)]
+
+
+class RsRows(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in
+                ("outer", "pages", "inner", "positions", "row_bytes", "outer_stride", "page_stride",
+                 "inner_stride", "position_stride")]
 
 
 class ResiSpecError(RuntimeError):
@@ -127,6 +137,21 @@ def _load():
     lib.resispec_filter_logits.restype = i32
     lib.resispec_token_logprobs.argtypes = [P, i64, P, i32, i32, i32, flt, P, P, P, P]
     lib.resispec_token_logprobs.restype = i32
+    lib.resispec_beam_select.argtypes = [P, i64, P, P, i32, i32, i32, i32, i32, flt, P, P, P, P, P, sz, P]
+    lib.resispec_beam_select.restype = i32
+    lib.resispec_beam_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.resispec_beam_workspace_bytes.restype = sz
+    rows = ctypes.POINTER(RsRows)
+    lib.resispec_beam_reorder.argtypes = [P, rows, P, rows, P, P, i32, i32, i32, P, P]
+    lib.resispec_beam_reorder.restype = i32
+    lib.resispec_beam_reorder_paged.argtypes = [P, rows, P, i64, P, rows, P, i64, i32, P, P, i32, i32, i32, P, P]
+    lib.resispec_beam_reorder_paged.restype = i32
+    lib.resispec_plan_cache.argtypes = [P, P, P, i32, i32, P, i64, i32, P, P, i32, P, P, P, i32, P, P, P, P, P]
+    lib.resispec_plan_cache.restype = i32
+    lib.resispec_accepted_path.argtypes = [P, P, P, P, i32, i32, i32, P, P, P]
+    lib.resispec_accepted_path.restype = i32
+    lib.resispec_commit_path.argtypes = [P, rows, P, P, P, rows, i32, i32, i32, P, P]
+    lib.resispec_commit_path.restype = i32
     lib.resispec_status_string.argtypes = [i32]
     lib.resispec_status_string.restype = ctypes.c_char_p
     lib.resispec_abi_version.argtypes = []
@@ -887,3 +912,330 @@ def resispec_token_logprobs(logits, tokens, *, temperature=1.0, out_logprob=None
                                            _given(st, lead, torch.int32, logits, "out_status"), handle))
         return lp, rank, st
     return _row_call(logits, stream, call)
+
+
+# ------------------------------------------------------------------- beams --
+
+def resispec_beam_workspace_bytes(B: int, W: int, V: int) -> int:
+    return lib.resispec_beam_workspace_bytes(int(B), int(W), int(V))
+
+
+def _int32(v, name):
+    """A whole number that ctypes will not cut to its low 32 bits."""
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError("%s must fit an int32, got %d" % (name, v))
+    return v
+
+
+def resispec_beam_select(logits, scores, *, k=None, temperature=1.0, ended=None, end_token=-1, out_parent=None,
+                         out_token=None, out_score=None, out_status=None, workspace=None, stream=None):
+    """The k best continuations (default: as many as beams) of each sequence's beams.
+
+    logits: [B, W, V] or [B * W, V], the rows one stride apart; scores: [B, W] fp32, the beams'
+    log-probabilities so far, -inf where there is no beam; ended: [B, W] uint8 or bool, beams
+    that go on with `end_token` alone, at their score; temperature: a number, or a device
+    tensor with an entry a row or a sequence.  Returns (parent beam, token, score, each [B, k],
+    best first; status [B])."""
+    import torch
+    ptr, step, lead, R, V = _rows(logits, "logits")
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2:
+        raise ValueError("scores must be a [B, W] tensor")
+    shape = scores.shape
+    B, W = shape
+    if R != B * W or (len(lead) == 2 and lead != shape):
+        raise ValueError("logits has rows %s, expected %s" % (tuple(lead), tuple(shape)))
+    k = W if k is None else _int32(k, "k")
+    end_token = _int32(end_token, "end_token")
+    if isinstance(temperature, torch.Tensor):
+        f = _settings(logits, shape, R, temperature, 0, 1.0, 0.0)
+    else:
+        f = _number_settings(logits.dtype is torch.bfloat16, float(temperature))
+    sp = _given(scores, shape, torch.float32, logits, "scores")
+    ep = None
+    if ended is not None:
+        ep = _given(ended, shape, torch.bool if ended.dtype is torch.bool else torch.uint8, logits, "ended")
+    dev, to = logits.device, (B, k)
+    need = lib.resispec_beam_workspace_bytes(B, W, V)
+
+    def call(handle):
+        parent = torch.empty(to, dtype=torch.int32, device=dev) if out_parent is None else out_parent
+        token = torch.empty(to, dtype=torch.int32, device=dev) if out_token is None else out_token
+        score = torch.empty(to, dtype=torch.float32, device=dev) if out_score is None else out_score
+        st = torch.empty(B, dtype=torch.int32, device=dev) if out_status is None else out_status
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev) if workspace is None else workspace
+        _check(lib.resispec_beam_select(ptr, step, sp, ep, end_token, B, W, V, k, ctypes.byref(f),
+                                        _given(parent, to, torch.int32, logits, "out_parent"),
+                                        _given(token, to, torch.int32, logits, "out_token"),
+                                        _given(score, to, torch.float32, logits, "out_score"),
+                                        _given(st, (B,), torch.int32, logits, "out_status"),
+                                        _given(ws, ws.shape, torch.uint8, logits, "workspace"), ws.numel(), handle))
+        return parent, token, score, st
+    return _row_call(logits, stream, call)
+
+
+@functools.lru_cache(maxsize=256)
+def _number_settings(bf16, temperature):
+    return RsFilter(RS_BF16 if bf16 else RS_F32, 1, temperature, 0, 1.0, 0.0)
+
+
+@functools.lru_cache(maxsize=1024)
+def _layout(shape, stride, size, page_dim, position_dim, name):
+    """(rs_rows, bytes from the first to past the last) of rows in a tensor: the dimensions
+    before page_dim are outer, those between it and position_dim inner, those after
+    position_dim (without one: after page_dim) the row, which has to lie together."""
+    def place(d, what):
+        if not -len(shape) <= d < len(shape):
+            raise ValueError("%s of %s is %d, of %d dimensions" % (what, name, d, len(shape)))
+        return d % len(shape)
+
+    def joined(dims, what):
+        n, step = 1, 0
+        for d in reversed(dims):
+            if shape[d] == 1:
+                continue
+            if n == 1:
+                step = stride[d]
+            elif stride[d] != n * step:
+                raise ValueError("%s: its %s dimensions must lie one stride apart" % (name, what))
+            n *= shape[d]
+        return n, step
+
+    page_dim = place(page_dim, "page_dim")
+    if min(shape) < 1:
+        raise ValueError("%s has shape %s" % (name, shape))
+    dims = range(len(shape))
+    if position_dim is None:
+        at, inner, positions = page_dim, (1, 0), (1, 0)
+    else:
+        at = place(position_dim, "position_dim")
+        if at <= page_dim:
+            raise ValueError("%s: the positions must come after the pages or beams" % name)
+        inner, positions = joined(dims[page_dim + 1:at], "inner"), joined(dims[at:at + 1], "position")
+    outer, pages = joined(dims[:page_dim], "outer"), joined(dims[page_dim:page_dim + 1], "page")
+    row, step = joined(dims[at + 1:], "row")
+    if row > 1 and step != 1:
+        raise ValueError("%s: the elements of a row must be adjacent" % name)
+    span = row
+    for n, d in sorted((x for x in (outer, pages, inner, positions) if x[0] > 1), key=lambda x: x[1]):
+        if d < span:
+            raise ValueError("%s: rows must not overlap" % name)
+        span += (n - 1) * d
+    r = RsRows(outer[0], pages[0], inner[0], positions[0], row * size,
+               *(d * size for _, d in (outer, pages, inner, positions)))
+    return r, span * size
+
+
+def _row_layout(t, page_dim, position_dim, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    return _layout(t.shape, t.stride(), t.element_size(), page_dim, position_dim, name)
+
+
+def _table(t, rows, like, name):
+    """(address, entries from row to row, entries a row) of a block table."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dtype is not torch.int32:
+        raise TypeError("%s must be torch.int32" % name)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < 1:
+        raise ValueError("%s has shape %s, expected %d rows" % (name, tuple(t.shape), rows))
+    step, n = t.stride(0) if rows > 1 else t.shape[1], t.shape[1]
+    if (n > 1 and t.stride(1) != 1) or step < n:
+        raise ValueError("%s: the entries of a row must be adjacent, and rows must not overlap" % name)
+    if t.get_device() != like.get_device():
+        raise ValueError("all tensors must be on one device, got %s" % {t.device, like.device})
+    return t.data_ptr(), step, n
+
+
+def _moved_to(src, layout, span, dst, name, *dims):
+    """Where rows go: (address, layout).  The same rows, or apart from them."""
+    if dst is None or dst is src:
+        return src.data_ptr(), layout
+    to, to_span = _row_layout(dst, *dims, name)
+    if dst.dtype is not src.dtype:
+        raise TypeError("%s must be %s" % (name, src.dtype))
+    if dst.get_device() != src.get_device():
+        raise ValueError("all tensors must be on one device, got %s" % {dst.device, src.device})
+    a, b = src.data_ptr(), dst.data_ptr()
+    if a < b + to_span and b < a + span and not (a == b and bytes(layout) == bytes(to)):
+        raise ValueError("%s must be apart from the rows it is taken from, or the same rows" % name)
+    return b, to
+
+
+def _beams(parent, n, like, name):
+    import torch
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
+        raise ValueError("parent must be a [B, K] tensor")
+    B, K = parent.shape
+    if B < 1 or n % B:
+        raise ValueError("%s has %d beams, parent %d sequences" % (name, n, B))
+    return B, n // B, K, _given(parent, parent.shape, torch.int32, like, "parent")
+
+
+def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengths=None, out=None, out_status=None,
+                          stream=None):
+    """The states of the chosen beams: beam k of sequence b becomes beam parent[b, k] (int32 [B,
+    K]; -1: stays as it is).  state: any tensor with B * W beams along beam_dim; out: the same
+    with B * K, or None for a move in place (K = W).  lengths (int32 [B], with position_dim):
+    only so many positions are moved.  Returns (out, status)."""
+    import torch
+    src, span = _row_layout(state, beam_dim, position_dim, "state")
+    B, W, K, pp = _beams(parent, src.pages, state, "state")
+    if lengths is not None and position_dim is None:
+        raise ValueError("lengths need position_dim")
+    if out is None and K != W:
+        raise ValueError("a move in place needs as many beams as there are, %d, got %d" % (W, K))
+    to, dst = _moved_to(state, src, span, out, "out", beam_dim, position_dim)
+    if dst.pages != B * K:
+        raise ValueError("out has %d beams, expected %d" % (dst.pages, B * K))
+    lp = None if lengths is None else _given(lengths, (B,), torch.int32, state, "lengths")
+
+    def call(handle):
+        st = torch.empty(B, dtype=torch.int32, device=state.device) if out_status is None else out_status
+        _check(lib.resispec_beam_reorder(state.data_ptr(), src, to, dst, pp, lp, B, W, K,
+                                         _given(st, (B,), torch.int32, state, "out_status"), handle))
+        return (state if out is None else out), st
+    return _row_call(state, stream, call)
+
+
+def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim=0, position_dim=1, out_table=None,
+                                out=None, out_status=None, stream=None):
+    """resispec_beam_reorder for beams whose positions lie in the pages of a cache: block_table
+    is [B * W, pages] int32, lengths [B] int32 positions.  out_table ([B * K, pages]; default:
+    block_table) says where the chosen beams' positions go, in `out` (default: the cache
+    itself).  Returns (out, status)."""
+    import torch
+    src, span = _row_layout(cache, page_dim, position_dim, "cache")
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [B * W, pages] tensor")
+    B, W, K, pp = _beams(parent, block_table.shape[0], cache, "block_table")
+    tp, tstep, n = _table(block_table, B * W, cache, "block_table")
+    if out_table is None:
+        if K != W:
+            raise ValueError("a move in place needs as many beams as there are, %d, got %d" % (W, K))
+        op, ostep = tp, tstep
+    else:
+        op, ostep, on = _table(out_table, B * K, cache, "out_table")
+        if on != n:
+            raise ValueError("out_table has %d entries a row, block_table %d" % (on, n))
+    if out is None and K != W:
+        raise ValueError("a move within the cache needs as many beams as there are, %d, got %d" % (W, K))
+    to, dst = _moved_to(cache, src, span, out, "out", page_dim, position_dim)
+    lp = _given(lengths, (B,), torch.int32, cache, "lengths")
+
+    def call(handle):
+        st = torch.empty(B, dtype=torch.int32, device=cache.device) if out_status is None else out_status
+        _check(lib.resispec_beam_reorder_paged(cache.data_ptr(), src, tp, tstep, to, dst, op, ostep, n, pp, lp, B, W, K,
+                                               _given(st, (B,), torch.int32, cache, "out_status"), handle))
+        return (cache if out is None else out), st
+    return _row_call(cache, stream, call)
+
+
+# ------------------------------------------------------------------- cache --
+
+def resispec_plan_cache(kept, added, held, block_table, free_pages, free_count, *, page_size, max_slots=None,
+                        out_slots=None, out_positions=None, out_requests=None, out_starts=None, out_held=None,
+                        out_free_count=None, out_status=None, stream=None):
+    """Pages and slots for a step's new rows.  Request r keeps its first kept[r] positions and
+    gets added[r] more; it holds the first held[r] pages of its row of block_table (all int32
+    [R]; the table [R, pages]).  free_pages: int32 stack of free page numbers with an entry for
+    every page of the cache, the first free_count[0] of them free.  block_table and free_pages
+    are brought up to date.  There is room for max_slots new rows (or as out_slots has); out_held
+    and out_free_count may be held and free_count.  Returns (slots, positions, requests, each
+    [max_slots] with -1 past the last row; starts [R + 1]; held [R]; free_count [1]; status
+    [R])."""
+    import torch
+    if not isinstance(kept, torch.Tensor) or kept.dim() != 1:
+        raise ValueError("kept must be a [R] tensor")
+    R, like = kept.shape[0], kept
+    kp, ap, hp = (_given(t, (R,), torch.int32, like, n) for t, n in ((kept, "kept"), (added, "added"), (held, "held")))
+    tp, step, n = _table(block_table, R, like, "block_table")
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
+        raise ValueError("free_pages must be a [pages] tensor")
+    pages = free_pages.shape[0]
+    fp = _given(free_pages, (pages,), torch.int32, like, "free_pages")
+    cp = _given(free_count, (1,), torch.int32, like, "free_count")
+    if max_slots is None:
+        if out_slots is None:
+            raise ValueError("max_slots or out_slots is required")
+        T = out_slots.shape[0] if out_slots.dim() == 1 else -1
+    else:
+        T = _int32(max_slots, "max_slots")
+    if T < 0:
+        raise ValueError("out_slots must be a [T] tensor, max_slots >= 0")
+    page_size = _int32(page_size, "page_size")
+
+    def call(handle):
+        e = lambda given, m: torch.empty(m, dtype=torch.int32, device=kept.device) if given is None else given  # noqa: E731
+        slots, positions, requests = e(out_slots, T), e(out_positions, T), e(out_requests, T)
+        starts, got, count, st = e(out_starts, R + 1), e(out_held, R), e(out_free_count, 1), e(out_status, R)
+        i32 = torch.int32
+        _check(lib.resispec_plan_cache(kp, ap, hp, R, page_size, tp, step, n, fp, cp, pages,
+                                       _given(got, (R,), i32, like, "out_held"),
+                                       _given(count, (1,), i32, like, "out_free_count"),
+                                       _given(starts, (R + 1,), i32, like, "out_starts"), T,
+                                       _given(slots, (T,), i32, like, "out_slots"),
+                                       _given(positions, (T,), i32, like, "out_positions"),
+                                       _given(requests, (T,), i32, like, "out_requests"),
+                                       _given(st, (R,), i32, like, "out_status"), handle))
+        return slots, positions, requests, starts, got, count, st
+    return _row_call(like, stream, call)
+
+
+def resispec_accepted_path(parent, node_token, tokens, accepted_len, *, out_path=None, out_status=None, stream=None):
+    """The accepted nodes of verified trees: parent and node_token [B, N], and a verification's
+    tokens [B, max_depth + 1] and accepted_len [B], all int32.  Returns (path [B, max_depth + 1]:
+    the root 0, then the accepted nodes, -1 after the last; status [B])."""
+    import torch
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 2 or not isinstance(tokens, torch.Tensor) or tokens.dim() != 2:
+        raise ValueError("parent must be [B, N], tokens [B, max_depth + 1]")
+    B, N = parent.shape
+    shape = (B, tokens.shape[1])
+    i32, like = torch.int32, parent
+    pp, np_ = _given(parent, (B, N), i32, like, "parent"), _given(node_token, (B, N), i32, like, "node_token")
+    tp, lp = _given(tokens, shape, i32, like, "tokens"), _given(accepted_len, (B,), i32, like, "accepted_len")
+
+    def call(handle):
+        path = torch.empty(shape, dtype=i32, device=parent.device) if out_path is None else out_path
+        st = torch.empty(B, dtype=i32, device=parent.device) if out_status is None else out_status
+        _check(lib.resispec_accepted_path(pp, np_, tp, lp, B, N, shape[1] - 1,
+                                          _given(path, shape, i32, like, "out_path"),
+                                          _given(st, (B,), i32, like, "out_status"), handle))
+        return path, st
+    return _row_call(like, stream, call)
+
+
+def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, position_dim=1, out_status=None, stream=None):
+    """The rows of accepted nodes at their places in a paged cache: for every entry path[b, i]
+    (int32 [B, depth], ascending, -1 after the last) the node's row goes to slot slots[b, i]
+    (int32 [B, N]).  It comes from `source`, laid out as the cache with trees for pages and nodes
+    for positions, or, without one, from the node's own slot.  Returns (cache, status)."""
+    import torch
+    rows, span = _row_layout(cache, page_dim, position_dim, "cache")
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 2 or not isinstance(path, torch.Tensor) or path.dim() != 2:
+        raise ValueError("slots must be [B, N], path [B, depth]")
+    B, N = slots.shape
+    i32 = torch.int32
+    sp, pp = _given(slots, (B, N), i32, cache, "slots"), _given(path, (B, path.shape[1]), i32, cache, "path")
+    at = rows_of = None
+    if source is not None:
+        rows_of, source_span = _row_layout(source, page_dim, position_dim, "source")
+        at = source.data_ptr()
+        if source.dtype is not cache.dtype:
+            raise TypeError("source must be %s" % cache.dtype)
+        if source.get_device() != cache.get_device():
+            raise ValueError("all tensors must be on one device, got %s" % {source.device, cache.device})
+        if at < cache.data_ptr() + span and cache.data_ptr() < at + source_span:
+            raise ValueError("source must be apart from the cache")
+        if rows_of.pages != B or rows_of.positions != N:
+            raise ValueError("source has %d trees of %d nodes, expected %d of %d" % (rows_of.pages, rows_of.positions, B, N))
+
+    def call(handle):
+        st = torch.empty(B, dtype=i32, device=cache.device) if out_status is None else out_status
+        _check(lib.resispec_commit_path(cache.data_ptr(), rows, sp, pp, at, rows_of, B, N, path.shape[1],
+                                        _given(st, (B,), i32, cache, "out_status"), handle))
+        return cache, st
+    return _row_call(cache, stream, call)
