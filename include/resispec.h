@@ -594,7 +594,7 @@ typedef struct {
  * of their value.
  *   out_parent, out_token : [B][k] int32, the best first: the beam, in [0, W), and the token; -1
  *                 past the last continuation
- *   out_score   : [B][k] fp32, its score (that of a 32-bit sum, 1e-6 off at most besides the
+ *   out_score   : [B][k] fp32, its score (that of a 32-bit sum, 1.3e-6 off at most besides the
  *                 rounding of the result); -inf past the last
  *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_UNDERFLOW: a live beam's row has
  *                 no finite logit, or a NaN or +inf; RS_SEQ_BAD_PARAM: a score that is NaN or

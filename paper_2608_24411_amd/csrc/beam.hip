@@ -9,21 +9,30 @@ namespace {
 
 // Mathematics.  The score of token v after beam w is s_w + (l_v - m)/T - L, L = ln sum_j
 // exp((l_j - m)/T): within a row the order is that of the logits, across rows the sums decide.
-// Two launches.  The first reads the rows once, in chunks of 512 elements that any wave may
-// take: a chunk leaves its maximum and the sum of its masses against that maximum.  The second,
-// a workgroup a sequence, adds the chunks up and chooses: of all a sequence's elements in order
-// the first k lie in the first k chunks, ordered by their maximum, then by place.  (If an
-// element's chunk were behind k others, each of these would hold an element before it.)  So
-// only k chunks are read again.
+// Two launches.  The first reads the rows once, in units of four chunks of 1024 elements that
+// any wave may take: a chunk leaves its maximum, a unit the sum of its masses against its own.
+// The second, a workgroup a sequence, adds the units up and chooses: the k largest maxima of
+// chunks are k elements, so whatever is chosen is not below the last of them, and only chunks
+// that reach so far, about k of a sequence's hundreds, are read again.
+//
+// Sums are of 32-bit masses: a 64-bit exponential takes twice the vector ALU's time.  A sum is
+// off by 1.3e-6 of itself at most: an exponent x by 3 * 2^-24 of itself (difference, scale and
+// product are rounded), so a mass by 0.693 of that and 2^-23, the mean of |x| by mass over a
+// unit of 4096 elements whose maximum is at 0 is 8.1 at most, and three additions are in 32
+// bits.  That is enough for a score, and for an order too unless two beams' scores are closer
+// than the two errors: then the rows concerned are summed again in 64 bits and the order is
+// decided by that.
 
-constexpr int kChunk = 512;              // elements of a chunk
+constexpr int kChunk = 1024;             // elements of a chunk
+constexpr int kUnitChunks = 4;           // chunks of a unit
+constexpr int kUnit = kChunk * kUnitChunks;
 constexpr int kRowsBlock = 256, kRowsWaves = kRowsBlock / 64;
 constexpr int kMergeBlock = 1024, kMergeWaves = kMergeBlock / 64;
+constexpr double kNear = 3.0e-6;         // scores this close are told apart in 64 bits
 
-struct ChunkSum {
+struct UnitSum {
     double sum;                          // of 2^((l - max) c)
-    float max;
-    float pad;
+    float max, pad;
 };
 
 struct BeamParams {
@@ -36,8 +45,9 @@ struct BeamParams {
     int32_t rows_per_entry;
     float temperature;
     const float* temperatures;
-    int32_t nch, parts;                  // chunks a row, workgroups a row
-    ChunkSum* chunks;                    // [B * W][nch]
+    int32_t units, parts;                // units a row, workgroups a row
+    UnitSum* sums;                       // [B * W][units]
+    float* maxima;                       // [B * W][units * kUnitChunks], of the chunks
     int32_t *parent, *token, *status;
     float* score;
     __device__ __forceinline__ float T(int64_t r) const {
@@ -54,14 +64,14 @@ struct Chunk {
     using W = Vec<In, VEC>;
     static constexpr int UNR = kChunk / (64 * VEC), N = UNR * VEC;
     typename W::raw t[UNR];
-    // Loads take no branch: what lies past the row reads its last elements, and is put right
-    // when it is unpacked.
+    // Loads take no branch: what lies past the row reads its last elements, and settle() puts
+    // it right, once.
     __device__ __forceinline__ void load(const In* row, int c, int V) {
         const int j0 = c * kChunk + (threadIdx.x & 63) * VEC;
 #pragma unroll
         for (int u = 0; u < UNR; ++u) t[u] = W::template load_full<false>(row, min(j0 + u * 64 * VEC, V - VEC));
     }
-    __device__ __forceinline__ void unpack(int c, int V, float (&v)[N]) {
+    __device__ __forceinline__ void settle(int c, int V) {
         const int j0 = c * kChunk + (threadIdx.x & 63) * VEC;
         if (c * kChunk + kChunk > V) {
 #pragma unroll
@@ -76,6 +86,8 @@ struct Chunk {
                 }
             }
         }
+    }
+    __device__ __forceinline__ void unpack(float (&v)[N]) const {
 #pragma unroll
         for (int u = 0; u < UNR; ++u) {
             float x[VEC];
@@ -90,6 +102,20 @@ struct Chunk {
     }
 };
 
+// The maxima over the wave of four values a lane: lanes q, q + 4, q + 8 .. get that of value q.
+__device__ __forceinline__ float wave_max4(float a, float b, float c, float d) {
+    const int lane = threadIdx.x & 63;
+    const bool odd = lane & 1, high = lane & 2;
+    const float ab = fmaxf(odd ? b : a, dpp_f<kDppXor1>(odd ? a : b));
+    const float cd = fmaxf(odd ? d : c, dpp_f<kDppXor1>(odd ? c : d));
+    float m = fmaxf(high ? cd : ab, dpp_f<kDppXor2>(high ? ab : cd));
+    constexpr int kDppRowRor4 = 0x124, kDppRowRor8 = 0x128;
+    m = fmaxf(m, dpp_f<kDppRowRor4>(m));
+    m = fmaxf(m, dpp_f<kDppRowRor8>(m));
+    m = fmaxf(m, __shfl_xor(m, 16));
+    return fmaxf(m, __shfl_xor(m, 32));
+}
+
 template <typename In, int VEC>
 __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const BeamParams P) {
     using C = Chunk<In, VEC>;
@@ -97,27 +123,41 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const BeamPara
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (!P.live(r)) return;
     const In* row = reinterpret_cast<const In*>(P.logits) + r * P.stride;
-    const double c2 = uniform(1.4426950408889634 / (double)P.T(r));
-    for (int c = (int)(blockIdx.x % P.parts) * kRowsWaves + wave; c < P.nch; c += P.parts * kRowsWaves) {
-        C chunk;
-        chunk.load(row, c, P.V);
-        float v[C::N];
-        chunk.unpack(c, P.V, v);
-        float m = v[0];
+    const float c = (float)fmin(1.4426950408889634 / (double)P.T(r), (double)FLT_MAX);
+    for (int unit = (int)(blockIdx.x % P.parts) * kRowsWaves + wave; unit < P.units; unit += P.parts * kRowsWaves) {
+        C chunk[kUnitChunks];
 #pragma unroll
-        for (int i = 1; i < C::N; ++i) m = fmaxf(m, v[i]);
-        m = wave_max(m);
+        for (int q = 0; q < kUnitChunks; ++q) chunk[q].load(row, unit * kUnitChunks + q, P.V);
+        float top[kUnitChunks];
+#pragma unroll
+        for (int q = 0; q < kUnitChunks; ++q) {
+            chunk[q].settle(unit * kUnitChunks + q, P.V);
+            float v[C::N];
+            chunk[q].unpack(v);
+            top[q] = v[0];
+#pragma unroll
+            for (int i = 1; i < C::N; ++i) top[q] = fmaxf(top[q], v[i]);
+        }
+        const float each = wave_max4(top[0], top[1], top[2], top[3]);
+        float m = fmaxf(each, dpp_f<kDppXor1>(each));
+        m = uniform(fmaxf(m, dpp_f<kDppXor2>(m)));
         const float ref = m > -INFINITY ? m : 0.0f;
+        // a NaN or +inf makes the sum a NaN
         double sum = 0.0;
-        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < C::N; ++i) {
-            bad |= !(v[i] < INFINITY);
-            sum += exp2_64(((double)v[i] - (double)ref) * c2);
+        for (int q = 0; q < kUnitChunks; ++q) {
+            float v[C::N];
+            chunk[q].unpack(v);
+#pragma unroll
+            for (int i = 0; i < C::N; ++i) v[i] = exp2_fast((v[i] - ref) * c);
+#pragma unroll
+            for (int i = 0; i < C::N; i += 8)
+                sum += (double)(((v[i] + v[i + 1]) + (v[i + 2] + v[i + 3])) +
+                                ((v[i + 4] + v[i + 5]) + (v[i + 6] + v[i + 7])));
         }
         sum = wave_sum(sum);
-        if (__ballot(bad)) sum = NAN;
-        if (lane == 0) P.chunks[r * P.nch + c] = {sum, m, 0.0f};
+        if (lane < kUnitChunks) P.maxima[(r * P.units + unit) * kUnitChunks + lane] = each;
+        if (lane == 0) P.sums[r * P.units + unit] = {sum, m, 0.0f};
     }
 }
 
@@ -147,178 +187,412 @@ __device__ __forceinline__ Place wave_first(Place a) {
     return a;
 }
 
+constexpr int kBins = 1024;              // of scores of chunks, from the best downwards
+constexpr double kBinsPerUnit = 32.0;
+constexpr int kChunkList = 512, kList = 1024;
+constexpr int kKeys = 8192;              // scores of chunks held in LDS
+
 struct MergeSmem {
     double log_sum[RS_MAX_CANDIDATES];
+    double best[RS_MAX_CANDIDATES];      // a beam's best continuation
     float max[RS_MAX_CANDIDATES], s[RS_MAX_CANDIDATES], T[RS_MAX_CANDIDATES];
+    float cut[RS_MAX_CANDIDATES];        // a row's logits that are listed
     int32_t kind[RS_MAX_CANDIDATES];     // 0: no beam, 1: live, 2: ended
-    int32_t status;
-    Place place[2][kMergeWaves];
-    Place chosen[RS_MAX_CANDIDATES];     // chunks
+    int32_t status, nchunks, nlist, kth_bin;
+    uint32_t doubt[2];                   // beams to be summed in 64 bits
+    double part[kMergeWaves];
+    union {
+        struct {
+            float key[kKeys];
+            int32_t bin[kBins];
+        };
+        struct {
+            double score[kList];
+            float l[kList];
+            int32_t w[kList], j[kList];
+        };
+        struct {
+            Place place[2][kMergeWaves];
+            Place chosen[RS_MAX_CANDIDATES];
+        };
+    };
+    int32_t chunks[kChunkList];          // those to read again: beam * chunks a row + chunk
+};
+
+template <typename In, int VEC>
+struct Merge {
+    using C = Chunk<In, VEC>;
+    using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
+    const BeamParams& P;
+    MergeSmem& sm;
+    const int64_t b, r0;
+    const int tid, lane, wave, nch;
+
+    __device__ __forceinline__ const In* row(int w) const {
+        return reinterpret_cast<const In*>(P.logits) + (r0 + w) * P.stride;
+    }
+    __device__ __forceinline__ float chunk_max(int w, int c) const {
+        return P.maxima[(r0 + w) * (int64_t)nch + c];
+    }
+    __device__ __forceinline__ double score(int w, float l) const {
+        if (sm.kind[w] == 2) return (double)sm.s[w];
+        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - sm.log_sum[w]) + (double)sm.s[w];
+    }
+
+    // Every beam's kind, maximum and sum, a wave a beam.
+    __device__ __forceinline__ void sums() {
+        for (int w = wave; w < P.W; w += kMergeWaves) {
+            const float s = P.scores[r0 + w], T = P.T(r0 + w);
+            const int kind = s == -INFINITY ? 0 : P.ended && P.ended[r0 + w] ? 2 : 1;
+            int st = RS_SEQ_OK;
+            if (!(s < INFINITY) || (kind == 1 && !(T > 0.0f && T < INFINITY))) st = RS_SEQ_BAD_PARAM;
+            float m = -INFINITY;
+            double sum = 0.0;
+            if (kind == 1 && st == RS_SEQ_OK) {
+                const UnitSum* units = P.sums + (r0 + w) * P.units;
+                const double c2 = 1.4426950408889634 / (double)T;
+                for (int u = lane; u < P.units; u += 64) m = fmaxf(m, units[u].max);
+                m = wave_max(m);
+                for (int u = lane; u < P.units; u += 64) {
+                    const UnitSum x = units[u];
+                    if (x.sum != 0.0) sum += x.sum * exp2_64(((double)x.max - (double)m) * c2);
+                }
+                sum = wave_sum(sum);
+                if (!(m > -INFINITY && m < INFINITY && sum < INFINITY)) st = RS_SEQ_UNDERFLOW;
+            }
+            if (lane == 0) {
+                const double log_sum = kind == 1 && st == RS_SEQ_OK ? log(sum) : 0.0;
+                sm.kind[w] = kind;
+                sm.s[w] = s;
+                sm.T[w] = T;
+                sm.max[w] = m;
+                sm.log_sum[w] = log_sum;
+                sm.best[w] = (double)s - log_sum;
+                if (st != RS_SEQ_OK) atomicMax(&sm.status, st);
+            }
+        }
+    }
+
+    // Row w's sum in 64 bits, by all threads.
+    __device__ __forceinline__ void sum_again(int w) {
+        const double c2 = 1.4426950408889634 / (double)sm.T[w], md = (double)sm.max[w];
+        double sum = 0.0;
+        for (int c = wave; c < nch; c += kMergeWaves) {
+            if (c * (int64_t)kChunk >= P.V) break;
+            C chunk;
+            chunk.load(row(w), c, P.V);
+            chunk.settle(c, P.V);
+            float v[C::N];
+            chunk.unpack(v);
+#pragma unroll
+            for (int i = 0; i < C::N; ++i) sum += exp2_64(((double)v[i] - md) * c2);
+        }
+        sum = wave_sum(sum);
+        __syncthreads();
+        if (lane == 0) sm.part[wave] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            sum = 0.0;
+            for (int i = 0; i < kMergeWaves; ++i) sum += sm.part[i];
+            sm.log_sum[w] = log(sum);
+        }
+    }
+
+    // How far a score is below the best, in bins.
+    __device__ __forceinline__ float depth(double best, double bins_per_unit, double s) const {
+        return (float)fmin((best - s) * bins_per_unit, (double)FLT_MAX);
+    }
+    __device__ __forceinline__ void count(float d) { atomicAdd(&sm.bin[(int)fminf(d, kBins - 1)], 1); }
+
+    // The bin in which the k-th counted lies, or the last one if there are fewer.
+    __device__ __forceinline__ int bin_of_kth() {
+        __syncthreads();
+        if (wave == 0) {
+            constexpr int kLaneBins = kBins / 64;
+            int n[kLaneBins], mine = 0;
+#pragma unroll
+            for (int i = 0; i < kLaneBins; ++i) mine += n[i] = sm.bin[lane * kLaneBins + i];
+            int upto = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
+            }
+            const uint64_t reached = __ballot(upto >= P.k);
+            if (lane == (reached ? __builtin_ctzll(reached) : 63)) {
+                int kth = kLaneBins - 1;
+#pragma unroll
+                for (int i = kLaneBins - 1; i >= 0; --i) {
+                    if (upto >= P.k) kth = i;
+                    upto -= n[i];
+                }
+                sm.kth_bin = lane * kLaneBins + kth;
+            }
+        }
+        __syncthreads();
+        return sm.kth_bin;
+    }
+
+    // Rows' least logits whose scores may be within `far` of the best.
+    __device__ __forceinline__ void cut_at(double best, double far) {
+        if (tid < P.W && sm.kind[tid] == 1) {
+            const double l = (best - far - (double)sm.s[tid] + sm.log_sum[tid]) * (double)sm.T[tid] + (double)sm.max[tid];
+            sm.cut[tid] = fmaxf((float)(l - fabs(l) * 0x1p-23), -FLT_MAX);
+        }
+        __syncthreads();
+    }
+
+    // body(w, l, j) for what the listed chunks hold above the cuts.
+    template <typename Body>
+    __device__ __forceinline__ void each_listed(Body&& body) {
+        const int n = sm.nchunks;
+        for (int i = wave; i < n; i += kMergeWaves) {
+            const int id = __builtin_amdgcn_readfirstlane(sm.chunks[i]), w = id / nch, c = id - w * nch;
+            if (sm.kind[w] == 2) {
+                if (lane == 0) body(w, 0.0f, P.end_token);
+                continue;
+            }
+            C chunk;
+            chunk.load(row(w), c, P.V);
+            chunk.settle(c, P.V);
+            float v[C::N];
+            chunk.unpack(v);
+            const float cut = sm.cut[w];
+#pragma unroll
+            for (int e = 0; e < C::N; ++e)
+                if (v[e] >= cut) body(w, v[e], C::at(c, e));
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ void list_listed() {
+        each_listed([&](int w, float l, int j) {
+            const int at = atomicAdd(&sm.nlist, 1);
+            if (at < kList) {
+                sm.score[at] = score(w, l);
+                sm.l[at] = l;
+                sm.w[at] = w;
+                sm.j[at] = j;
+            }
+        });
+    }
+
+    // Lists every continuation that can be among the first k.  False where the lists are too
+    // short for it: many equal elements, or large vocabularies with no order to speak of.
+    __device__ __forceinline__ bool list() {
+        const int n = P.W * nch;
+        double best = -INFINITY;
+        for (int w = 0; w < P.W; ++w)
+            if (sm.kind[w]) best = fmax(best, sm.best[w]);
+        auto key = [&](int i) {
+            const int w = i / nch, c = i - w * nch, kind = sm.kind[w];
+            if (kind == 0 || (kind == 2 && c > 0)) return INFINITY;
+            const float l = kind == 2 ? 0.0f : chunk_max(w, c);
+            return l == -INFINITY ? INFINITY : depth(best, kBinsPerUnit, score(w, l));
+        };
+        for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kMergeBlock) {
+            const float d = key(i);
+            if (i < kKeys) sm.key[i] = d;
+            if (d < INFINITY) count(d);
+        }
+        int bin = bin_of_kth();
+        // the last bin has no end, so all chunks are listed
+        bool all = bin == kBins - 1;
+        double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + 2.0 * kNear;
+        const float limit = all ? FLT_MAX : (float)(far * kBinsPerUnit * (1.0 + 1e-6));
+        for (int i = tid; i < n; i += kMergeBlock) {
+            const float d = i < kKeys ? sm.key[i] : key(i);
+            if (d <= limit) {
+                const int at = atomicAdd(&sm.nchunks, 1);
+                if (at < kChunkList) sm.chunks[at] = i;
+            }
+        }
+        cut_at(best, far);
+        if (sm.nchunks > kChunkList) return false;
+        if (!all) {
+            list_listed();
+            if (sm.nlist <= kList) return true;
+        }
+        // finer, by the elements themselves
+        const double bins_per_unit = all ? kBinsPerUnit : kBins / far;
+        __syncthreads();
+        for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
+        if (tid == 0) sm.nlist = 0;
+        __syncthreads();
+        each_listed([&](int w, float l, int) { count(depth(best, bins_per_unit, score(w, l))); });
+        bin = bin_of_kth();
+        if (bin < kBins - 1) cut_at(best, (bin + 1) / bins_per_unit + 2.0 * kNear);
+        list_listed();
+        return sm.nlist <= kList;
+    }
+    __device__ __forceinline__ void put(int i, int w, int j, double s) const {
+        P.parent[b * P.k + i] = w;
+        P.token[b * P.k + i] = j;
+        P.score[b * P.k + i] = (float)s;
+    }
+
+    // The places of the listed continuations in the order, 16 lanes each: how many come before.
+    // FINAL: the first k are put out; else beams are marked whose scores are too close to call.
+    template <bool FINAL>
+    __device__ __forceinline__ void rank() {
+        const int n = sm.nlist, sub = lane & 15;
+        for (int i = tid >> 4; i < n; i += kMergeBlock / 16) {
+            const Place mine = {sm.score[i], sm.w[i], sm.l[i], sm.j[i]};
+            int ahead = 0;
+            uint64_t close = 0;
+            for (int x = sub; x < n; x += 16) {
+                const Place other = {sm.score[x], sm.w[x], sm.l[x], sm.j[x]};
+                ahead += before(other, mine);
+                if (!FINAL && other.w != mine.w && fabs(other.score - mine.score) <= kNear) close |= 1ull << other.w;
+            }
+            ahead += dpp_i<kDppXor1>(ahead);
+            ahead += dpp_i<kDppXor2>(ahead);
+            ahead += dpp_i<kDppHalfMirror>(ahead);
+            ahead += dpp_i<kDppMirror>(ahead);
+            if (ahead >= P.k) continue;
+            if (FINAL) {
+                if (sub == 0) put(ahead, mine.w, mine.j, mine.score);
+            } else if (close) {
+                close |= 1ull << mine.w;
+                atomicOr(&sm.doubt[0], (uint32_t)close);
+                atomicOr(&sm.doubt[1], (uint32_t)(close >> 32));
+            }
+        }
+    }
+
+    __device__ __forceinline__ Place first_of_all(Place mine, int parity) {
+        if (lane == 0) sm.place[parity][wave] = mine;
+        __syncthreads();
+        Place best = sm.place[parity][0];
+        for (int w = 1; w < kMergeWaves; ++w)
+            if (before(sm.place[parity][w], best)) best = sm.place[parity][w];
+        return best;
+    }
+
+    // The choice where lists do not do: the first k chunks by their maxima hold it (if an
+    // element's chunk were behind k others, each of these would hold an element before it), and
+    // one place is settled after another.  Sums in 64 bits have been taken.
+    __device__ __forceinline__ int one_by_one() {
+        Place prev = {INFINITY, -1, INFINITY, -1};
+        int nsel = 0;
+        for (int i = 0; i < P.k; ++i) {
+            Place best = nothing();
+            for (int w = 0; w < P.W; ++w) {
+                const int kind = sm.kind[w];
+                if (kind == 0) continue;
+                for (int c = tid; c < (kind == 2 ? 1 : nch); c += kMergeBlock) {
+                    const float l = kind == 2 ? 0.0f : chunk_max(w, c);
+                    if (l == -INFINITY) continue;
+                    const Place x = {score(w, l), w, l, c};
+                    if (before(prev, x) && before(x, best)) best = x;
+                }
+            }
+            best = first_of_all(wave_first(best), i & 1);
+            if (best.w == kNoBeam) break;
+            if (tid == 0) sm.chosen[i] = best;
+            prev = best;
+            nsel = i + 1;
+        }
+        __syncthreads();
+        // the first element of each chunk that comes after what has been put out
+        prev = {INFINITY, -1, INFINITY, -1};
+        auto first_of = [&](int i) {
+            const Place ch = sm.chosen[i];
+            Place best = nothing();
+            if (sm.kind[ch.w] == 2) {
+                const Place x = {ch.score, ch.w, 0.0f, P.end_token};
+                if (lane == 0 && before(prev, x)) best = x;
+            } else {
+                C chunk;
+                chunk.load(row(ch.w), ch.j, P.V);
+                chunk.settle(ch.j, P.V);
+                float v[C::N];
+                chunk.unpack(v);
+#pragma unroll
+                for (int e = 0; e < C::N; ++e) {
+                    if (v[e] == -INFINITY || v[e] < best.l) continue;
+                    const Place x = {score(ch.w, v[e]), ch.w, v[e], C::at(ch.j, e)};
+                    if (before(prev, x) && before(x, best)) best = x;
+                }
+            }
+            return wave_first(best);
+        };
+        constexpr int kEach = RS_MAX_CANDIDATES / kMergeWaves;
+        Place head[kEach];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const int i = wave + q * kMergeWaves;
+            head[q] = nothing();
+            if (i < nsel) head[q] = first_of(i);
+        }
+        int found = 0;
+        for (int i = 0; i < P.k; ++i) {
+            Place mine = head[0];
+#pragma unroll
+            for (int q = 1; q < kEach; ++q)
+                if (before(head[q], mine)) mine = head[q];
+            prev = first_of_all(mine, i & 1);
+            if (prev.w == kNoBeam) break;
+            found = i + 1;
+            if (tid == 0) put(i, prev.w, prev.j, prev.score);
+#pragma unroll
+            for (int q = 0; q < kEach; ++q)
+                if (head[q].w == prev.w && head[q].j == prev.j) head[q] = first_of(wave + q * kMergeWaves);
+        }
+        return found;
+    }
+
+    __device__ __forceinline__ void run() {
+        if (tid == 0) {
+            sm.status = RS_SEQ_OK;
+            sm.nchunks = sm.nlist = 0;
+            sm.doubt[0] = sm.doubt[1] = 0;
+        }
+        __syncthreads();
+        sums();
+        __syncthreads();
+        const int status = sm.status;
+        int found = 0;
+        if (status == RS_SEQ_OK) {
+            if (list()) {
+                found = min(sm.nlist, P.k);
+                rank<false>();
+                __syncthreads();
+                const uint64_t doubt = (uint64_t)sm.doubt[1] << 32 | sm.doubt[0];
+                if (doubt) {
+                    for (int w = 0; w < P.W; ++w)
+                        if ((doubt >> w & 1) && sm.kind[w] == 1) sum_again(w);
+                    __syncthreads();
+                    for (int i = tid; i < sm.nlist; i += kMergeBlock) sm.score[i] = score(sm.w[i], sm.l[i]);
+                    __syncthreads();
+                }
+                rank<true>();
+            } else {
+                for (int w = 0; w < P.W; ++w)
+                    if (sm.kind[w] == 1) sum_again(w);
+                __syncthreads();
+                found = one_by_one();
+            }
+        }
+        const float none = status == RS_SEQ_OK ? -INFINITY : NAN;
+        for (int i = found + tid; i < P.k; i += kMergeBlock) put(i, -1, -1, none);
+        if (tid == 0 && P.status) P.status[b] = status;
+    }
 };
 
 template <typename In, int VEC>
 __global__ void __launch_bounds__(kMergeBlock) rs_beam_merge_kernel(const BeamParams P) {
-    using C = Chunk<In, VEC>;
     __shared__ MergeSmem sm;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t b = blockIdx.x, r0 = b * P.W;
-    const ChunkSum* chunks = P.chunks + r0 * P.nch;
-    if (tid == 0) sm.status = RS_SEQ_OK;
-    __syncthreads();
-    for (int w = wave; w < P.W; w += kMergeWaves) {
-        const float s = P.scores[r0 + w], T = P.T(r0 + w);
-        int kind = s == -INFINITY ? 0 : P.ended && P.ended[r0 + w] ? 2 : 1;
-        int st = RS_SEQ_OK;
-        if (!(s < INFINITY)) st = RS_SEQ_BAD_PARAM;
-        if (kind == 1 && !(T > 0.0f && T < INFINITY)) st = RS_SEQ_BAD_PARAM;
-        float m = -INFINITY;
-        double sum = 0.0;
-        if (kind == 1 && st == RS_SEQ_OK) {
-            for (int c = lane; c < P.nch; c += 64) m = fmaxf(m, chunks[w * P.nch + c].max);
-            m = wave_max(m);
-            const double c2 = 1.4426950408889634 / (double)T;
-            for (int c = lane; c < P.nch; c += 64) {
-                const ChunkSum x = chunks[w * P.nch + c];
-                if (x.sum != 0.0) sum += x.sum * exp2_64(((double)x.max - (double)m) * c2);
-            }
-            sum = wave_sum(sum);
-            if (!(m > -INFINITY && m < INFINITY && sum < INFINITY)) st = RS_SEQ_UNDERFLOW;
-        }
-        if (lane == 0) {
-            sm.kind[w] = kind;
-            sm.s[w] = s;
-            sm.T[w] = T;
-            sm.max[w] = m;
-            sm.log_sum[w] = kind == 1 && st == RS_SEQ_OK ? log(sum) : 0.0;
-            if (st != RS_SEQ_OK) atomicMax(&sm.status, st);
-        }
-    }
-    __syncthreads();
-    const int status = sm.status;
-    if (status != RS_SEQ_OK) {
-        for (int i = tid; i < P.k; i += kMergeBlock) {
-            P.parent[b * P.k + i] = P.token[b * P.k + i] = -1;
-            P.score[b * P.k + i] = NAN;
-        }
-        if (tid == 0 && P.status) P.status[b] = status;
-        return;
-    }
-    auto score = [&](int w, float l) {
-        if (sm.kind[w] == 2) return (double)sm.s[w];
-        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - sm.log_sum[w]) + (double)sm.s[w];
-    };
-    // the first k chunks, one after another
-    Place prev = {INFINITY, -1, INFINITY, -1};
-    int nsel = 0;
-    for (int i = 0; i < P.k; ++i) {
-        Place best = nothing();
-        for (int w = 0; w < P.W; ++w) {
-            const int kind = sm.kind[w];
-            if (kind == 0) continue;
-            for (int c = tid; c < (kind == 2 ? 1 : P.nch); c += kMergeBlock) {
-                const float l = kind == 2 ? 0.0f : chunks[w * P.nch + c].max;
-                if (l == -INFINITY) continue;
-                const Place x = {score(w, l), w, l, c};
-                if (before(prev, x) && before(x, best)) best = x;
-            }
-        }
-        best = wave_first(best);
-        if (lane == 0) sm.place[i & 1][wave] = best;
-        __syncthreads();
-        best = sm.place[i & 1][0];
-        for (int w = 1; w < kMergeWaves; ++w)
-            if (before(sm.place[i & 1][w], best)) best = sm.place[i & 1][w];
-        if (best.w == kNoBeam) break;
-        if (tid == 0) sm.chosen[i] = best;
-        prev = best;
-        nsel = i + 1;
-    }
-    __syncthreads();
-    // their elements, a wave up to four chunks, and the first k of those
-    constexpr int kEach = RS_MAX_CANDIDATES / kMergeWaves;
-    float v[kEach][C::N];
-    Place head[kEach];
-    auto first_of = [&](int q) {
-        const int i = wave + q * kMergeWaves;
-        head[q] = nothing();
-        if (i >= nsel) return;
-        const Place ch = sm.chosen[i];
-        if (sm.kind[ch.w] == 2) {
-            if (v[q][0] == 0.0f) head[q] = {ch.score, ch.w, 0.0f, P.end_token};
-            return;
-        }
-        float l = -INFINITY;
-        int at = INT_MAX;
-#pragma unroll
-        for (int e = 0; e < C::N; ++e)
-            if (v[q][e] > l) {
-                l = v[q][e];
-                at = C::at(ch.j, e);
-            }
-        const float top = wave_max(l);
-        if (top == -INFINITY) return;
-        int j = l == top ? at : INT_MAX;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) j = min(j, __shfl_xor(j, d));
-        head[q] = {score(ch.w, top), ch.w, top, j};
-    };
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        const int i = wave + q * kMergeWaves;
-        if (i < nsel) {
-            const Place ch = sm.chosen[i];
-            if (sm.kind[ch.w] == 2) {
-                v[q][0] = 0.0f;
-            } else {
-                C chunk;
-                chunk.load(reinterpret_cast<const In*>(P.logits) + (r0 + ch.w) * P.stride, ch.j, P.V);
-                chunk.unpack(ch.j, P.V, v[q]);
-            }
-        }
-        first_of(q);
-    }
-    int found = 0;
-    for (int i = 0; i < P.k; ++i) {
-        Place mine = head[0];
-#pragma unroll
-        for (int q = 1; q < kEach; ++q)
-            if (before(head[q], mine)) mine = head[q];
-        if (lane == 0) sm.place[i & 1][wave] = mine;
-        __syncthreads();
-        Place best = sm.place[i & 1][0];
-        for (int w = 1; w < kMergeWaves; ++w)
-            if (before(sm.place[i & 1][w], best)) best = sm.place[i & 1][w];
-        if (best.w == kNoBeam) break;
-        found = i + 1;
-        if (tid == 0) {
-            P.parent[b * P.k + i] = best.w;
-            P.token[b * P.k + i] = best.j;
-            P.score[b * P.k + i] = (float)best.score;
-        }
-#pragma unroll
-        for (int q = 0; q < kEach; ++q)
-            if (head[q].w == best.w && head[q].j == best.j) {
-                const Place ch = sm.chosen[wave + q * kMergeWaves];
-                if (sm.kind[ch.w] == 2) {
-                    v[q][0] = -INFINITY;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < C::N; ++e)
-                        if (C::at(ch.j, e) == best.j) v[q][e] = -INFINITY;
-                }
-                first_of(q);
-            }
-    }
-    for (int i = found + tid; i < P.k; i += kMergeBlock) {
-        P.parent[b * P.k + i] = P.token[b * P.k + i] = -1;
-        P.score[b * P.k + i] = -INFINITY;
-    }
-    if (tid == 0 && P.status) P.status[b] = RS_SEQ_OK;
+    const int tid = threadIdx.x;
+    Merge<In, VEC> m{P, sm, (int64_t)blockIdx.x, (int64_t)blockIdx.x * P.W, tid, tid & 63,
+                     __builtin_amdgcn_readfirstlane(tid >> 6), P.units * kUnitChunks};
+    m.run();
 }
 
 // ------------------------------------------------------------------- host ----
 
-int32_t chunks_of(int32_t V) { return (V + kChunk - 1) / kChunk; }
+int32_t units_of(int32_t V) { return (V + kUnit - 1) / kUnit; }
 
 constexpr int32_t kMostRows = (1 << 23) - 1;
 
@@ -329,7 +603,7 @@ extern "C" {
 size_t resispec_beam_workspace_bytes(int32_t B, int32_t W, int32_t V) {
     if (B <= 0 || W <= 0 || V <= 0 || W > RS_MAX_CANDIDATES || V > RS_MAX_VOCAB) return 0;
     if ((int64_t)B * W > kMostRows) return 0;
-    return (size_t)B * W * chunks_of(V) * sizeof(ChunkSum);
+    return (size_t)B * W * units_of(V) * (sizeof(UnitSum) + kUnitChunks * sizeof(float));
 }
 
 rs_status resispec_beam_select(const void* logits, int64_t row_stride, const float* scores, const uint8_t* ended,
@@ -364,13 +638,14 @@ rs_status resispec_beam_select(const void* logits, int64_t row_stride, const flo
     P.rows_per_entry = filter->rows_per_entry;
     P.temperature = filter->temperature;
     P.temperatures = filter->temperatures;
-    P.nch = chunks_of(V);
-    P.chunks = static_cast<ChunkSum*>(workspace);
+    P.units = units_of(V);
+    P.sums = static_cast<UnitSum*>(workspace);
+    P.maxima = reinterpret_cast<float*>(P.sums + (int64_t)B * W * P.units);
     P.parent = out_parent;
     P.token = out_token;
     P.score = out_score;
     P.status = out_status;
-    const int64_t R = (int64_t)B * W, most = (P.nch + kRowsWaves - 1) / kRowsWaves, share = (4096 + R - 1) / R;
+    const int64_t R = (int64_t)B * W, most = (P.units + kRowsWaves - 1) / kRowsWaves, share = (4096 + R - 1) / R;
     P.parts = (int32_t)(most < share ? most : share);
     const int64_t esz = filter->logits_dtype == RS_BF16 ? 2 : 4;
     RowLoads loads = row_loads(logits, logits, V, filter->logits_dtype);
