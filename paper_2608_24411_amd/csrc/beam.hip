@@ -66,10 +66,11 @@ struct Chunk {
     typename W::raw t[UNR];
     // Loads take no branch: what lies past the row reads its last elements, and settle() puts
     // it right, once.
+    template <bool NT>
     __device__ __forceinline__ void load(const In* row, int c, int V) {
         const int j0 = c * kChunk + (threadIdx.x & 63) * VEC;
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) t[u] = W::template load_full<false>(row, min(j0 + u * 64 * VEC, V - VEC));
+        for (int u = 0; u < UNR; ++u) t[u] = W::template load_full<NT>(row, min(j0 + u * 64 * VEC, V - VEC));
     }
     __device__ __forceinline__ void settle(int c, int V) {
         const int j0 = c * kChunk + (threadIdx.x & 63) * VEC;
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const BeamPara
     for (int unit = (int)(blockIdx.x % P.parts) * kRowsWaves + wave; unit < P.units; unit += P.parts * kRowsWaves) {
         C chunk[kUnitChunks];
 #pragma unroll
-        for (int q = 0; q < kUnitChunks; ++q) chunk[q].load(row, unit * kUnitChunks + q, P.V);
+        for (int q = 0; q < kUnitChunks; ++q) chunk[q].template load<true>(row, unit * kUnitChunks + q, P.V);
         float top[kUnitChunks];
 #pragma unroll
         for (int q = 0; q < kUnitChunks; ++q) {
@@ -190,22 +191,22 @@ __device__ __forceinline__ Place wave_first(Place a) {
 constexpr int kBins = 1024;              // of scores of chunks, from the best downwards
 constexpr double kBinsPerUnit = 32.0;
 constexpr int kChunkList = 512, kList = 1024;
-constexpr int kKeys = 8192;              // scores of chunks held in LDS
+constexpr int kHeld = 2;                 // maxima of chunks a thread holds
+// what is listed besides: two sums' errors, and the rounding of a distance in bins
+constexpr double kSlack = 2.0 * kNear + 1.0e-5;
 
 struct MergeSmem {
     double log_sum[RS_MAX_CANDIDATES];
     double best[RS_MAX_CANDIDATES];      // a beam's best continuation
     float max[RS_MAX_CANDIDATES], s[RS_MAX_CANDIDATES], T[RS_MAX_CANDIDATES];
     float cut[RS_MAX_CANDIDATES];        // a row's logits that are listed
+    float below[RS_MAX_CANDIDATES], per_logit[RS_MAX_CANDIDATES];
     int32_t kind[RS_MAX_CANDIDATES];     // 0: no beam, 1: live, 2: ended
     int32_t status, nchunks, nlist, kth_bin;
     uint32_t doubt[2];                   // beams to be summed in 64 bits
     double part[kMergeWaves];
     union {
-        struct {
-            float key[kKeys];
-            int32_t bin[kBins];
-        };
+        int32_t bin[kBins];
         struct {
             double score[kList];
             float l[kList];
@@ -242,6 +243,9 @@ struct Merge {
     // Every beam's kind, maximum and sum, a wave a beam.
     __device__ __forceinline__ void sums() {
         for (int w = wave; w < P.W; w += kMergeWaves) {
+            // asked for before it is known whether they are wanted
+            const UnitSum* units = P.sums + (r0 + w) * P.units;
+            const UnitSum x = lane < P.units ? units[lane] : UnitSum{0.0, -INFINITY, 0.0f};
             const float s = P.scores[r0 + w], T = P.T(r0 + w);
             const int kind = s == -INFINITY ? 0 : P.ended && P.ended[r0 + w] ? 2 : 1;
             int st = RS_SEQ_OK;
@@ -249,14 +253,15 @@ struct Merge {
             float m = -INFINITY;
             double sum = 0.0;
             if (kind == 1 && st == RS_SEQ_OK) {
-                const UnitSum* units = P.sums + (r0 + w) * P.units;
-                const double c2 = 1.4426950408889634 / (double)T;
-                for (int u = lane; u < P.units; u += 64) m = fmaxf(m, units[u].max);
+                m = x.max;
+                for (int u = lane + 64; u < P.units; u += 64) m = fmaxf(m, units[u].max);
                 m = wave_max(m);
-                for (int u = lane; u < P.units; u += 64) {
-                    const UnitSum x = units[u];
-                    if (x.sum != 0.0) sum += x.sum * exp2_64(((double)x.max - (double)m) * c2);
-                }
+                const double c2 = 1.4426950408889634 / (double)T;
+                auto add = [&](const UnitSum& y) {
+                    if (y.sum != 0.0) sum += y.sum * exp2_64(((double)y.max - (double)m) * c2);
+                };
+                add(x);
+                for (int u = lane + 64; u < P.units; u += 64) add(units[u]);
                 sum = wave_sum(sum);
                 if (!(m > -INFINITY && m < INFINITY && sum < INFINITY)) st = RS_SEQ_UNDERFLOW;
             }
@@ -280,7 +285,7 @@ struct Merge {
         for (int c = wave; c < nch; c += kMergeWaves) {
             if (c * (int64_t)kChunk >= P.V) break;
             C chunk;
-            chunk.load(row(w), c, P.V);
+            chunk.template load<false>(row(w), c, P.V);
             chunk.settle(c, P.V);
             float v[C::N];
             chunk.unpack(v);
@@ -353,7 +358,7 @@ struct Merge {
                 continue;
             }
             C chunk;
-            chunk.load(row(w), c, P.V);
+            chunk.template load<false>(row(w), c, P.V);
             chunk.settle(c, P.V);
             float v[C::N];
             chunk.unpack(v);
@@ -378,36 +383,55 @@ struct Merge {
 
     // Lists every continuation that can be among the first k.  False where the lists are too
     // short for it: many equal elements, or large vocabularies with no order to speak of.
-    __device__ __forceinline__ bool list() {
+    // maxima: those of the chunks tid, tid + kMergeBlock ..
+    __device__ __forceinline__ bool list(const float (&maxima)[kHeld]) {
         const int n = P.W * nch;
         double best = -INFINITY;
         for (int w = 0; w < P.W; ++w)
             if (sm.kind[w]) best = fmax(best, sm.best[w]);
-        auto key = [&](int i) {
-            const int w = i / nch, c = i - w * nch, kind = sm.kind[w];
-            if (kind == 0 || (kind == 2 && c > 0)) return INFINITY;
-            const float l = kind == 2 ? 0.0f : chunk_max(w, c);
-            return l == -INFINITY ? INFINITY : depth(best, kBinsPerUnit, score(w, l));
-        };
+        // a row's best is this far below the best, and a unit of logits so many of scores
+        if (tid < P.W) {
+            sm.below[tid] = (float)(best - sm.best[tid]);
+            sm.per_logit[tid] = (float)(1.0 / (double)sm.T[tid]);
+        }
         for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += kMergeBlock) {
-            const float d = key(i);
-            if (i < kKeys) sm.key[i] = d;
-            if (d < INFINITY) count(d);
+        // how far the score of chunk i's first element is below the best, in bins, in 32 bits:
+        // 2^-22 of it off, 2e-4 bins at most where bins are told apart
+        auto key = [&](int i, float l) {
+            const int w = i / nch, kind = sm.kind[w];
+            if (kind == 0 || (kind == 2 && i != w * nch)) return INFINITY;
+            if (kind == 2) return sm.below[w] * (float)kBinsPerUnit;
+            if (l == -INFINITY) return INFINITY;
+            return fminf((sm.below[w] + (sm.max[w] - l) * sm.per_logit[w]) * (float)kBinsPerUnit, FLT_MAX);
+        };
+        float held[kHeld];
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = tid + h * kMergeBlock;
+            held[h] = i < n ? key(i, maxima[h]) : INFINITY;
+            if (held[h] < INFINITY) count(held[h]);
         }
+        auto later = [&](auto&& body) {
+            for (int i = tid + kHeld * kMergeBlock; i < n; i += kMergeBlock) {
+                const float d = key(i, P.maxima[r0 * nch + i]);
+                if (d < INFINITY) body(i, d);
+            }
+        };
+        later([&](int, float d) { count(d); });
         int bin = bin_of_kth();
         // the last bin has no end, so all chunks are listed
-        bool all = bin == kBins - 1;
-        double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + 2.0 * kNear;
-        const float limit = all ? FLT_MAX : (float)(far * kBinsPerUnit * (1.0 + 1e-6));
-        for (int i = tid; i < n; i += kMergeBlock) {
-            const float d = i < kKeys ? sm.key[i] : key(i);
-            if (d <= limit) {
-                const int at = atomicAdd(&sm.nchunks, 1);
-                if (at < kChunkList) sm.chunks[at] = i;
-            }
-        }
+        const bool all = bin == kBins - 1;
+        const double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + kSlack;
+        const float limit = all ? FLT_MAX : (float)((far + kSlack) * kBinsPerUnit);
+        auto pick = [&](int i, float d) {
+            if (!(d <= limit)) return;
+            const int at = atomicAdd(&sm.nchunks, 1);
+            if (at < kChunkList) sm.chunks[at] = i;
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) pick(tid + h * kMergeBlock, held[h]);
+        later(pick);
         cut_at(best, far);
         if (sm.nchunks > kChunkList) return false;
         if (!all) {
@@ -422,19 +446,19 @@ struct Merge {
         __syncthreads();
         each_listed([&](int w, float l, int) { count(depth(best, bins_per_unit, score(w, l))); });
         bin = bin_of_kth();
-        if (bin < kBins - 1) cut_at(best, (bin + 1) / bins_per_unit + 2.0 * kNear);
+        if (bin < kBins - 1) cut_at(best, (bin + 1) / bins_per_unit + kSlack);
         list_listed();
         return sm.nlist <= kList;
     }
+
     __device__ __forceinline__ void put(int i, int w, int j, double s) const {
         P.parent[b * P.k + i] = w;
         P.token[b * P.k + i] = j;
         P.score[b * P.k + i] = (float)s;
     }
 
-    // The places of the listed continuations in the order, 16 lanes each: how many come before.
-    // FINAL: the first k are put out; else beams are marked whose scores are too close to call.
-    template <bool FINAL>
+    // The listed continuations at their places in the order: 16 lanes count how many come before
+    // one.  Beams are marked whose scores are too close to call.
     __device__ __forceinline__ void rank() {
         const int n = sm.nlist, sub = lane & 15;
         for (int i = tid >> 4; i < n; i += kMergeBlock / 16) {
@@ -444,16 +468,15 @@ struct Merge {
             for (int x = sub; x < n; x += 16) {
                 const Place other = {sm.score[x], sm.w[x], sm.l[x], sm.j[x]};
                 ahead += before(other, mine);
-                if (!FINAL && other.w != mine.w && fabs(other.score - mine.score) <= kNear) close |= 1ull << other.w;
+                if (other.w != mine.w && fabs(other.score - mine.score) <= kNear) close |= 1ull << other.w;
             }
             ahead += dpp_i<kDppXor1>(ahead);
             ahead += dpp_i<kDppXor2>(ahead);
             ahead += dpp_i<kDppHalfMirror>(ahead);
             ahead += dpp_i<kDppMirror>(ahead);
             if (ahead >= P.k) continue;
-            if (FINAL) {
-                if (sub == 0) put(ahead, mine.w, mine.j, mine.score);
-            } else if (close) {
+            if (sub == 0) put(ahead, mine.w, mine.j, mine.score);
+            if (close) {
                 close |= 1ull << mine.w;
                 atomicOr(&sm.doubt[0], (uint32_t)close);
                 atomicOr(&sm.doubt[1], (uint32_t)(close >> 32));
@@ -505,7 +528,7 @@ struct Merge {
                 if (lane == 0 && before(prev, x)) best = x;
             } else {
                 C chunk;
-                chunk.load(row(ch.w), ch.j, P.V);
+                chunk.template load<false>(row(ch.w), ch.j, P.V);
                 chunk.settle(ch.j, P.V);
                 float v[C::N];
                 chunk.unpack(v);
@@ -549,15 +572,21 @@ struct Merge {
             sm.nchunks = sm.nlist = 0;
             sm.doubt[0] = sm.doubt[1] = 0;
         }
+        float maxima[kHeld];
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = tid + h * kMergeBlock;
+            maxima[h] = i < P.W * nch ? P.maxima[r0 * nch + i] : -INFINITY;
+        }
         __syncthreads();
         sums();
         __syncthreads();
         const int status = sm.status;
         int found = 0;
         if (status == RS_SEQ_OK) {
-            if (list()) {
+            if (list(maxima)) {
                 found = min(sm.nlist, P.k);
-                rank<false>();
+                rank();
                 __syncthreads();
                 const uint64_t doubt = (uint64_t)sm.doubt[1] << 32 | sm.doubt[0];
                 if (doubt) {
@@ -566,8 +595,8 @@ struct Merge {
                     __syncthreads();
                     for (int i = tid; i < sm.nlist; i += kMergeBlock) sm.score[i] = score(sm.w[i], sm.l[i]);
                     __syncthreads();
+                    rank();
                 }
-                rank<true>();
             } else {
                 for (int w = 0; w < P.W; ++w)
                     if (sm.kind[w] == 1) sum_again(w);
@@ -645,7 +674,8 @@ rs_status resispec_beam_select(const void* logits, int64_t row_stride, const flo
     P.token = out_token;
     P.score = out_score;
     P.status = out_status;
-    const int64_t R = (int64_t)B * W, most = (P.units + kRowsWaves - 1) / kRowsWaves, share = (4096 + R - 1) / R;
+    // a unit a wave, and less than 2^32 threads a launch
+    const int64_t R = (int64_t)B * W, most = (P.units + kRowsWaves - 1) / kRowsWaves, share = kMostRows / R;
     P.parts = (int32_t)(most < share ? most : share);
     const int64_t esz = filter->logits_dtype == RS_BF16 ? 2 : 4;
     RowLoads loads = row_loads(logits, logits, V, filter->logits_dtype);

@@ -4,19 +4,15 @@
 // (resispec_accepted_path) and their rows' places in the cache (resispec_commit_path).
 // Declared in resispec.h.
 
-#include <hip/hip_runtime.h>
+#include "common.h"
 
+#include <algorithm>
 #include <climits>
-#include <cstdint>
-#include <type_traits>
-
-#include "resispec.h"
 
 namespace {
 
 // Vectors of 16 bytes at any address: rows need not be a multiple of 16 bytes long, nor start
 // on one, and gfx950 loads and stores such vectors in one instruction.
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
@@ -39,19 +35,27 @@ template <typename T>
 __device__ __forceinline__ T load_at(const uint8_t* p) {
     return *reinterpret_cast<const typename Any<T>::type*>(p);
 }
+// Rows are stored past the caches, which they would only fill: 40 states of 492 KB 39 us with
+// ordinary stores and 25 with these, 1024 paths in rows of 1000 bytes 36 and 27.  Loads stay
+// ordinary: beams of one parent, and the ends of rows, share lines.
 template <typename T>
 __device__ __forceinline__ void store_at(uint8_t* p, T v) {
-    *reinterpret_cast<typename Any<T>::type*>(p) = v;
+    if constexpr (sizeof(T) == 1) *p = v;
+    else __builtin_nontemporal_store(v, reinterpret_cast<typename Any<T>::type*>(p));
 }
 
 __device__ __forceinline__ int uniform_i(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t readlane_i64(int64_t v, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, l);
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | lo);
+}
 
 // ---------------------------------------------------------------- reorder ----
 
-// States move for all beams of a sequence at once.  A lane owns a column, 16 bytes (or one)
-// at one place of every beam's state: it loads the new value of each beam and then stores
-// them, so a move in place needs no second buffer and no wait between workgroups.  A wave
-// takes a piece, positions that lie one after another, and its addresses are scalar.
+// States move for all beams of a sequence at once.  A lane owns columns, 16 bytes at one place
+// of every beam's state: it loads the new value of each beam and then stores them, so a move in
+// place needs no second buffer and no wait between workgroups.  A wave takes a piece, bytes that
+// lie one after another.
 struct ReorderParams {
     const uint8_t* src;
     uint8_t* dst;
@@ -62,15 +66,17 @@ struct ReorderParams {
     int64_t src_table_stride, dst_table_stride;
     int32_t max_pages;               // entries of a table's row
     int32_t W, K, G;                 // workgroups a sequence
-    int32_t step, per_page;          // positions a piece, pieces a page
+    int32_t together;                // positions lie one after another
+    int32_t pieces;                  // a page has so many (together), or a row
     int32_t* status;
 };
 
 constexpr int kReorderBlock = 256, kReorderWaves = kReorderBlock / 64;
-constexpr int64_t kPieceBytes = 4096;
 
-template <int KMAX, typename T, bool PAGED>
+// U: columns a lane and beam in a piece.
+template <int KMAX, typename T, int U, bool PAGED>
 __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const ReorderParams P) {
+    constexpr int64_t kPiece = 64 * U * sizeof(T);
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
     const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
     const int32_t* parent = P.parent + (int64_t)b * P.K;
@@ -99,60 +105,57 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
         if (threadIdx.x == 0) P.status[b] = st;
     }
     if (bad || len == 0) return;
-    const uint32_t full = (uint32_t)(len / S), rest = (uint32_t)(len % S);
-    const uint32_t nq = full * P.per_page + (rest + P.step - 1) / P.step;
-    const uint32_t inner = (uint32_t)P.s.inner, pieces = (uint32_t)P.s.outer * inner * nq;
-    for (uint32_t piece = g * kReorderWaves + wave; piece < pieces; piece += P.G * kReorderWaves) {
-        const uint32_t q = piece % nq, oi = piece / nq, i = oi % inner, o = oi / inner;
-        const uint32_t page = q / P.per_page, t = (q % P.per_page) * P.step;
-        const uint32_t end = min(t + P.step, page < full ? (uint32_t)S : rest);
-        const int64_t bytes = (int64_t)(end - t) * P.s.row_bytes;
-        const int64_t from0 = o * P.s.outer_stride + i * P.s.inner_stride + t * P.s.position_stride;
-        const int64_t to0 = o * P.d.outer_stride + i * P.d.inner_stride + t * P.d.position_stride;
-        const uint8_t* from[KMAX];
-        uint8_t* to[KMAX];
-#pragma unroll
-        for (int k = 0; k < KMAX; ++k) {
-            from[k] = nullptr;
-            to[k] = nullptr;
-            if (k >= P.K) continue;
-            const int w = parent[k];
-            if (w < 0) continue;
-            int64_t f, d;
+    const uint32_t full = (uint32_t)(len / S), rest = (uint32_t)(len % S), each = (uint32_t)P.pieces;
+    const int64_t row = P.s.row_bytes;
+    const uint32_t nq = P.together ? full * each + (uint32_t)((rest * row + kPiece - 1) / kPiece) : (uint32_t)len * each;
+    const uint32_t inner = (uint32_t)P.s.inner, all = (uint32_t)P.s.outer * inner * nq;
+    for (uint32_t piece = g * kReorderWaves + wave; piece < all; piece += P.G * kReorderWaves) {
+        // quotients are computed in vector registers
+        const uint32_t oi = uniform_i(piece / nq), q = piece - oi * nq, o = uniform_i(oi / inner), i = oi - o * inner;
+        uint32_t page = uniform_i(q / each), t = 0;
+        const int64_t first = (q - page * each) * kPiece;
+        int64_t bytes = row - first;
+        if (P.together) {
+            bytes = (page < full ? S : rest) * row - first;
+        } else {
+            const uint32_t p = uniform_i(page / (uint32_t)S);
+            t = page - p * (uint32_t)S;
+            page = p;
+        }
+        bytes = min(bytes, kPiece);
+        // lane k has beam k's addresses
+        int64_t from = o * P.s.outer_stride + i * P.s.inner_stride + t * P.s.position_stride + first;
+        int64_t to = o * P.d.outer_stride + i * P.d.inner_stride + t * P.d.position_stride + first;
+        bool moves = mine >= 0;
+        if (moves) {
+            int64_t f = (int64_t)b * P.W + mine, d = (int64_t)b * P.K + lane;
             if (PAGED) {
-                f = from_table[w * P.src_table_stride + page];
-                d = to_table[k * P.dst_table_stride + page];
-                if ((uint64_t)f >= (uint64_t)P.s.pages || (uint64_t)d >= (uint64_t)P.d.pages) continue;
-            } else {
-                f = (int64_t)b * P.W + w;
-                d = (int64_t)b * P.K + k;
+                f = from_table[mine * P.src_table_stride + page];
+                d = to_table[lane * P.dst_table_stride + page];
+                moves = (uint64_t)f < (uint64_t)P.s.pages && (uint64_t)d < (uint64_t)P.d.pages;
             }
-            const uint8_t* x = P.src + from0 + f * P.s.page_stride;
-            uint8_t* y = P.dst + to0 + d * P.d.page_stride;
-            if (x == y) continue;       // where it is
-            from[k] = x;
-            to[k] = y;
+            from += reinterpret_cast<int64_t>(P.src) + f * P.s.page_stride;
+            to += reinterpret_cast<int64_t>(P.dst) + d * P.d.page_stride;
         }
-        const int64_t whole = bytes / (int64_t)sizeof(T) * (int64_t)sizeof(T);
-        for (int64_t c = lane * (int64_t)sizeof(T); c < whole; c += 64 * sizeof(T)) {
-            T v[KMAX];
+        const uint64_t on = __ballot(moves && from != to);      // equal: where it is
+        auto move = [&](auto zero, uint32_t c) {
+            using E = decltype(zero);
+            E v[KMAX];
 #pragma unroll
             for (int k = 0; k < KMAX; ++k)
-                if (from[k]) v[k] = load_at<T>(from[k] + c);
+                if (on >> k & 1) v[k] = load_at<E>(reinterpret_cast<const uint8_t*>(readlane_i64(from, k)) + c);
 #pragma unroll
             for (int k = 0; k < KMAX; ++k)
-                if (from[k]) store_at<T>(to[k] + c, v[k]);
+                if (on >> k & 1) store_at<E>(reinterpret_cast<uint8_t*>(readlane_i64(to, k)) + c, v[k]);
+        };
+        // columns, and bytes at a run's end
+        const uint32_t whole = (uint32_t)bytes / sizeof(T) * sizeof(T);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t c = (u * 64 + lane) * sizeof(T);
+            if (c < whole) move(T{}, c);
         }
-        if (whole + lane < bytes) {
-            const int64_t c = whole + lane;
-            uint8_t v[KMAX];
-#pragma unroll
-            for (int k = 0; k < KMAX; ++k)
-                if (from[k]) v[k] = from[k][c];
-#pragma unroll
-            for (int k = 0; k < KMAX; ++k)
-                if (from[k]) to[k][c] = v[k];
-        }
+        if (whole + lane < bytes) move(uint8_t{}, whole + lane);
     }
 }
 
@@ -172,154 +175,346 @@ struct PlanParams {
     int32_t *slots, *positions, *requests, *status;
 };
 
-constexpr int kPlanBlock = 1024;
-
-// The sum over a workgroup's threads up to each, in order, and the whole sum.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t (&part)[kPlanBlock / 64], int64_t& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t x = __shfl_up(v, d);
-        if (lane >= d) v += x;
+// The sum over a workgroup's threads up to each, in order, and the whole sum.  Whole numbers in
+// fp64, exact to 2^53.  Two calls in a row need different halves of `part`.
+template <int BLOCK>
+__device__ __forceinline__ int64_t block_scan(int64_t v, double (&part)[BLOCK / 64], int64_t& total) {
+    const int lane = threadIdx.x & 63;
+    const double x = wave_incl_scan((double)v, lane);
+    if constexpr (BLOCK == 64) {
+        total = (int64_t)readlane_d(x, 63);
+        return (int64_t)x;
+    } else {
+        const int wave = uniform_i(threadIdx.x >> 6);
+        if (lane == 63) part[wave] = x;
+        __syncthreads();
+        double before = 0.0, all = 0.0;
+#pragma unroll 4
+        for (int w = 0; w < BLOCK / 64; ++w) {
+            before += w < wave ? part[w] : 0.0;
+            all += part[w];
+        }
+        total = (int64_t)all;
+        return (int64_t)(x + before);
     }
-    __syncthreads();
-    if (lane == 63) part[wave] = v;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-    for (int w = 0; w < kPlanBlock / 64; ++w) {
-        if (w < wave) before += part[w];
-        total += part[w];
-    }
-    return v + before;
 }
 
-// The slot, position and request of new row t.
-__device__ __forceinline__ void plan_row(const PlanParams& P, const int32_t* starts, int t) {
-    int slot = -1, position = -1, request = -1;
-    if (P.R > 0 && t < starts[P.R]) {
-        int lo = 0, hi = P.R;           // starts[lo] <= t < starts[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (starts[mid] <= t) lo = mid;
-            else hi = mid;
-        }
-        const int64_t k = P.kept[lo], n = P.added[lo], want = (k + n + P.page_size - 1) / P.page_size;
-        // granted: it holds what it wants, and its rows fit
-        if (P.out_held[lo] == want && starts[lo] + n <= P.T) {
-            const int p = (int)(k + t - starts[lo]);
-            const int page = P.table[lo * P.table_stride + p / P.page_size];
-            position = p;
-            request = lo;
-            if ((uint32_t)page < (uint32_t)P.num_pages) slot = page * P.page_size + p % P.page_size;
-            else if (P.status) P.status[lo] = RS_SEQ_BAD_PAGE;
-        }
-    }
-    P.slots[t] = slot;
-    if (P.positions) P.positions[t] = position;
-    if (P.requests) P.requests[t] = request;
+// The first of n running sums above x (there is one).
+template <typename Sums>
+__device__ __forceinline__ int first_above(const Sums& upto, int n, int x) {
+    int lo = 0;
+    for (int step = 1 << (31 - __builtin_clz(n)); step; step >>= 1)
+        if (lo + step <= n && upto[lo + step - 1] <= x) lo += step;
+    return lo;
 }
 
-// One workgroup, 1024 requests at a time, in two passes: the first has the running sums of
-// rows and gives pages back, the second takes pages.  ROWS: it does the new rows as well.
-template <bool ROWS>
-__global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P) {
-    __shared__ int64_t part[kPlanBlock / 64];
-    __shared__ int32_t released, taken;
-    const int tid = threadIdx.x;
-    const int count = P.free_count[0];
-    const bool count_ok = count >= 0 && count <= P.num_pages;
-    if (tid == 0) released = taken = 0;
+struct NewRow {
+    int slot, position, request;
+};
+__device__ __forceinline__ void put_row(const PlanParams& P, int t, const NewRow& x) {
+    P.slots[t] = x.slot;
+    if (P.positions) P.positions[t] = x.position;
+    if (P.requests) P.requests[t] = x.request;
+}
+// The place in a page of position p: entry p / page_size of the request's row, and the rest.
+__device__ __forceinline__ int slot_in(const PlanParams& P, int page, uint32_t rest) {
+    return (uint32_t)page < (uint32_t)P.num_pages ? (int)((uint32_t)page * (uint32_t)P.page_size + rest) : -1;
+}
 
-    struct Request {
-        int32_t held, want, give, need, status;
-        int64_t first;
-    };
-    int64_t rows = 0, given = 0;        // before this tile
-    int64_t given_before = 0;           // this request's place among the pages given back
-    auto look = [&](int r, Request& q) {
-        q = {0, 0, 0, 0, RS_SEQ_OK, 0};
-        int64_t n = 0;
+// A request's numbers, and its places in the running sums over those before it.
+struct Request {
+    int32_t kept, added, held, want, give, need, status;
+    int64_t first;                       // rows before it
+    int64_t gives, needs;                // pages given back, and taken, up to it
+};
+
+// The rules, for the BLOCK requests of a tile.
+template <int BLOCK>
+struct Plan {
+    const PlanParams& P;
+    double (&part)[3][BLOCK / 64];
+    const int count;                     // free pages
+    int64_t rows = 0, given = 0, needed = 0;   // before this tile
+
+    __device__ __forceinline__ void look(int r, Request& q) {
+        q = {0, 0, 0, 0, 0, 0, RS_SEQ_OK, 0, 0, 0};
+        const bool count_ok = count >= 0 && count <= P.num_pages;
         if (r < P.R) {
-            const int64_t k = P.kept[r];
-            n = P.added[r];
+            q.kept = P.kept[r];
+            q.added = P.added[r];
             q.held = P.held[r];
-            if (k < 0 || n < 0 || q.held < 0 || q.held > P.max_pages || k + n > (int64_t)P.max_pages * P.page_size) {
+            const int64_t n = (int64_t)q.kept + q.added;
+            if (q.kept < 0 || q.added < 0 || q.held < 0 || q.held > P.max_pages || n > (int64_t)P.max_pages * P.page_size) {
                 q.status = RS_SEQ_BAD_PARAM;
-                n = 0;
+                q.added = 0;
             } else {
-                q.want = (int32_t)((k + n + P.page_size - 1) / P.page_size);
+                q.want = (int32_t)(((uint32_t)n + (uint32_t)P.page_size - 1) / (uint32_t)P.page_size);
             }
         }
         int64_t total;
-        const int64_t upto = rows + block_scan(n, part, total);
+        const int64_t upto = rows + block_scan<BLOCK>(q.added, part[0], total);
         rows += total;
-        q.first = upto - n;
-        if (q.status == RS_SEQ_OK && n > 0 && upto > P.T) q.status = RS_SEQ_NO_ROOM;
+        q.first = upto - q.added;
+        if (q.status == RS_SEQ_OK && q.added > 0 && upto > P.T) q.status = RS_SEQ_NO_ROOM;
         if (q.status == RS_SEQ_OK) {
             q.give = max(q.held - q.want, 0);
             q.need = max(q.want - q.held, 0);
             if (!count_ok && (q.give || q.need)) q.status = RS_SEQ_BAD_PARAM;
         }
         if (q.status != RS_SEQ_OK) q.give = q.need = 0;
-        const int64_t gives = given + block_scan(q.give, part, total);
+        // requests that are refused here are the last that would give: what is given has no gaps
+        q.gives = given + block_scan<BLOCK>(q.give, part[1], total);
         given += total;
-        given_before = gives - q.give;
-        if (q.give && count + gives > P.num_pages) {
+        if (q.give && count + q.gives > P.num_pages) {
             q.status = RS_SEQ_BAD_PARAM;
             q.give = 0;
         }
-    };
-    Request q;
-    const int tiles = (P.R + kPlanBlock - 1) / kPlanBlock;
-    for (int i = 0; i < tiles; ++i) {
-        const int r = i * kPlanBlock + tid;
-        look(r, q);
-        for (int j = 0; j < q.give; ++j)
-            P.free_pages[count + given_before + j] = P.table[r * P.table_stride + q.want + j];
-        if (q.give) atomicAdd(&released, q.give);
     }
-    __syncthreads();
-    const int avail = count + released;
-    const int64_t all_rows = rows;
-    int64_t needed = 0;
-    rows = given = 0;
-    for (int i = 0; i < tiles; ++i) {
-        const int r = i * kPlanBlock + tid;
-        if (tiles > 1) look(r, q);
+    // what is there to be taken, once all of that has been given back; likewise without gaps
+    __device__ __forceinline__ void take(Request& q, int avail) {
         int64_t total;
-        const int64_t upto = needed + block_scan(q.need, part, total);
+        q.needs = needed + block_scan<BLOCK>(q.need, part[2], total);
         needed += total;
-        if (q.need && upto > avail) {
+        if (q.need && q.needs > avail) {
             q.status = RS_SEQ_NO_ROOM;
             q.need = 0;
         }
-        for (int j = 0; j < q.need; ++j)
-            P.table[r * P.table_stride + q.held + j] = P.free_pages[avail - 1 - (upto - q.need + j)];
+    }
+    __device__ __forceinline__ void put(int r, const Request& q) const {
+        P.out_held[r] = q.status == RS_SEQ_OK ? q.want : q.held;
+        P.out_starts[r] = (int32_t)min(q.first, (int64_t)INT_MAX);
+    }
+};
+
+// A step of up to BLOCK requests in one launch.  Every workgroup works out the running sums for
+// itself, and then everything from the inputs alone: pages that are given back and taken again
+// are found where their giver has them.  So no workgroup waits for another: some do the rows,
+// some the pages that are taken, or given back, some the requests' numbers, and a thread looks
+// up whose the next one is.  With several workgroups the outputs must not be inputs.
+constexpr int kTakers = 8, kGivers = 4, kTellers = 4;
+template <int BLOCK>
+__global__ void __launch_bounds__(BLOCK) rs_plan_step_kernel(const PlanParams P) {
+    __shared__ double part[3][BLOCK / 64];
+    __shared__ int32_t end[BLOCK], first[BLOCK], kept[BLOCK];        // rows
+    __shared__ int32_t gives[BLOCK], give_at[BLOCK];                 // pages given back up to it, where they are
+    __shared__ int32_t needs[BLOCK], held[BLOCK], want[BLOCK];
+    __shared__ int32_t touched[BLOCK], touch_at[BLOCK], wrong[BLOCK];
+    __shared__ int32_t released, taken;
+    const int tid = threadIdx.x;
+    const int count = P.free_count[0];
+    if (tid == 0) released = taken = 0;
+    __syncthreads();
+    Plan<BLOCK> plan{P, part, count};
+    Request q;
+    plan.look(tid, q);
+    if (q.give) atomicAdd(&released, q.give);
+    __syncthreads();
+    const int avail = count + released;
+    plan.take(q, avail);
+    if (q.need) atomicAdd(&taken, q.need);
+    const bool granted = q.status == RS_SEQ_OK;
+    const int64_t rows = plan.rows;
+    end[tid] = (int32_t)min(q.first + q.added, (int64_t)INT_MAX);
+    first[tid] = granted ? (int32_t)q.first : -1;
+    kept[tid] = q.kept;
+    gives[tid] = (int32_t)min(q.gives, (int64_t)INT_MAX);
+    give_at[tid] = q.want - (int32_t)(q.gives - q.give);
+    needs[tid] = (int32_t)min(q.needs, (int64_t)INT_MAX);
+    held[tid] = q.held;
+    want[tid] = q.want;
+    __syncthreads();
+    const int F = released, A = taken;
+    // page number x of those given back, and of those taken
+    auto given_page = [&](int x) {
+        const int r = first_above(gives, BLOCK, x);
+        return P.table[r * P.table_stride + give_at[r] + x];
+    };
+    auto taken_page = [&](int x) {
+        const int at = avail - 1 - x;
+        return at < count ? P.free_pages[at] : given_page(at - count);
+    };
+    auto page_of = [&](int r, int e) {
+        return e < held[r] ? P.table[r * P.table_stride + e] : taken_page(needs[r] - want[r] + e);
+    };
+    // the jobs' first workgroups and how many they have
+    const bool alone = gridDim.x == 1;
+    const int nrows = alone ? 1 : (int)gridDim.x - kTakers - kGivers - kTellers;
+    auto job = [&](int from, int groups, int n, auto&& body) {
+        if (alone) from = 0, groups = 1;
+        const int g = (int)blockIdx.x - from;
+        if (g < 0 || g >= groups) return;
+        for (int x = g * BLOCK + tid; x < n; x += groups * BLOCK) body(x);
+    };
+    job(nrows + kTakers, kGivers, F, [&](int x) { P.free_pages[count + x] = given_page(x); });
+    job(nrows, kTakers, A, [&](int x) {
+        const int r = first_above(needs, BLOCK, x);
+        P.table[r * P.table_stride + x - needs[r] + want[r]] = taken_page(x);
+    });
+    job(0, nrows, P.T, [&](int t) {
+        NewRow x = {-1, -1, -1};
+        if (t < rows) {
+            const int r = first_above(end, BLOCK, t);
+            if (first[r] >= 0) {
+                const uint32_t p = (uint32_t)kept[r] + (uint32_t)(t - first[r]), e = p / (uint32_t)P.page_size;
+                x = {slot_in(P, page_of(r, (int)e), p - e * (uint32_t)P.page_size), (int)p, r};
+            }
+        }
+        put_row(P, t, x);
+    });
+    const int teller = alone ? 0 : (int)blockIdx.x - nrows - kTakers - kGivers, tellers = alone ? 1 : kTellers;
+    if (teller < 0) return;
+    // every page that the new rows of this workgroup's requests lie in is looked at
+    const int own = BLOCK / tellers, r0 = teller * own;
+    const bool mine = tid >= r0 && tid < r0 + own && tid < P.R;
+    if (P.status) {
+        // from the page with position `kept` on
+        const int from = granted && q.added ? (int)((uint32_t)q.kept / (uint32_t)P.page_size) : q.want;
+        const int n = mine && granted ? q.want - from : 0;
+        int64_t all;
+        __syncthreads();
+        const int64_t upto = block_scan<BLOCK>(n, part[0], all);
+        touched[tid] = (int32_t)upto;
+        touch_at[tid] = from - (int32_t)(upto - n);
+        wrong[tid] = 0;
+        __syncthreads();
+        for (int x = tid; x < all; x += BLOCK) {
+            const int r = first_above(touched, BLOCK, x);
+            if ((uint32_t)page_of(r, touch_at[r] + x) >= (uint32_t)P.num_pages) wrong[r] = 1;
+        }
+        __syncthreads();
+        if (mine) P.status[tid] = granted && wrong[tid] ? RS_SEQ_BAD_PAGE : q.status;
+    }
+    if (mine) plan.put(tid, q);
+    if (teller == 0 && tid == 0) {
+        P.out_starts[P.R] = (int32_t)min(rows, (int64_t)INT_MAX);
+        P.out_free_count[0] = avail - A;
+    }
+}
+
+// Any number of requests, and outputs that are inputs: one workgroup, 1024 requests at a time,
+// in two passes (the first gives pages back, the second takes them), and the new rows in a
+// launch of their own.
+constexpr int kPlanBlock = 1024;
+__global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P) {
+    __shared__ double part[3][kPlanBlock / 64];
+    __shared__ int32_t upto_s[kPlanBlock], at_s[kPlanBlock];
+    __shared__ int32_t released, taken, in_tile;
+    const int tid = threadIdx.x;
+    const int count = P.free_count[0];
+    if (tid == 0) released = taken = in_tile = 0;
+    __syncthreads();
+    // body(r, entry, i) for pages i = 0 .. of the tile's requests, `mine` from entry `at` of
+    // request r's row on; upto: mine and those before
+    auto pages = [&](int tile, int mine, int upto, int at, auto&& body) {
+        if (!__syncthreads_or(mine)) return;
+        upto_s[tid] = upto;
+        at_s[tid] = at - (upto - mine);
+        if (mine) atomicMax(&in_tile, upto);
+        __syncthreads();
+        const int all = in_tile;
+        for (int i = tid; i < all; i += kPlanBlock) {
+            const int x = first_above(upto_s, kPlanBlock, i);
+            body(tile * kPlanBlock + x, at_s[x] + i, i);
+        }
+        __syncthreads();
+        if (tid == 0) in_tile = 0;
+        __syncthreads();
+    };
+    Plan<kPlanBlock> plan{P, part, count};
+    Request q;
+    const int tiles = (P.R + kPlanBlock - 1) / kPlanBlock;
+    for (int i = 0; i < tiles; ++i) {
+        const int64_t base = plan.given;
+        plan.look(i * kPlanBlock + tid, q);
+        if (q.give) atomicAdd(&released, q.give);
+        pages(i, q.give, (int)min(q.gives - base, (int64_t)INT_MAX), q.want, [&](int r, int e, int x) {
+            P.free_pages[count + base + x] = P.table[r * P.table_stride + e];
+        });
+    }
+    __syncthreads();
+    const int avail = count + released;
+    const int64_t rows = plan.rows;
+    plan.rows = plan.given = 0;
+    for (int i = 0; i < tiles; ++i) {
+        const int r = i * kPlanBlock + tid;
+        const int64_t base = plan.needed;
+        plan.look(r, q);
+        plan.take(q, avail);
         if (q.need) atomicAdd(&taken, q.need);
+        pages(i, q.need, (int)min(q.needs - base, (int64_t)INT_MAX), q.held, [&](int r, int e, int x) {
+            P.table[r * P.table_stride + e] = P.free_pages[avail - 1 - (base + x)];
+        });
         if (r < P.R) {
-            P.out_held[r] = q.status == RS_SEQ_OK ? q.want : q.held;
-            P.out_starts[r] = (int32_t)min(q.first, (int64_t)INT_MAX);
+            plan.put(r, q);
             if (P.status) P.status[r] = q.status;
         }
+        __syncthreads();
     }
     __syncthreads();
     if (tid == 0) {
-        P.out_starts[P.R] = (int32_t)min(all_rows, (int64_t)INT_MAX);
+        P.out_starts[P.R] = (int32_t)min(rows, (int64_t)INT_MAX);
         P.out_free_count[0] = avail - taken;
-    }
-    if (ROWS) {
-        __syncthreads();
-        for (int t = tid; t < P.T; t += kPlanBlock) plan_row(P, P.out_starts, t);
     }
 }
 
+// A row a thread, with the running sums of up to kStarts requests in LDS.
+constexpr int kStarts = 4096;
 __global__ void __launch_bounds__(256) rs_plan_rows_kernel(const PlanParams P) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t < P.T) plan_row(P, P.out_starts, (int)t);
+    __shared__ int32_t ends[kStarts];
+    const bool held = P.R <= kStarts;
+    if (held) {
+        for (int r = threadIdx.x; r < P.R; r += 256) ends[r] = P.out_starts[r + 1];
+        __syncthreads();
+    }
+    const int64_t t64 = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t64 >= P.T) return;
+    const int t = (int)t64;
+    NewRow x = {-1, -1, -1};
+    if (t < P.out_starts[P.R]) {
+        const int r = held ? first_above(ends, P.R, t) : first_above(P.out_starts + 1, P.R, t);
+        const int k = P.kept[r], n = P.added[r], first = P.out_starts[r];
+        const int want = (int)(((uint32_t)k + (uint32_t)n + (uint32_t)P.page_size - 1) / (uint32_t)P.page_size);
+        // granted: it holds what it wants, and its rows fit
+        if (P.out_held[r] == want && (int64_t)first + n <= P.T) {
+            const uint32_t p = (uint32_t)k + (uint32_t)(t - first), e = p / (uint32_t)P.page_size;
+            x = {slot_in(P, P.table[r * P.table_stride + e], p - e * (uint32_t)P.page_size), (int)p, r};
+            if (x.slot < 0 && P.status) P.status[r] = RS_SEQ_BAD_PAGE;
+        }
+    }
+    put_row(P, t, x);
 }
 
 // ------------------------------------------------------------------- path ----
+
+// Trees of up to 64 nodes, a wave a sequence: lane n has node n, and the nodes of a level that
+// carry the tokens are bits of a mask.
+constexpr int kPathWaves = 4;
+__global__ void __launch_bounds__(kPathWaves * 64) rs_path_wave_kernel(
+    const int32_t* __restrict__ parent, const int32_t* __restrict__ node_token, const int32_t* __restrict__ tokens,
+    const int32_t* __restrict__ accepted_len, int32_t B, int32_t N, int32_t max_depth, int32_t* __restrict__ path,
+    int32_t* status) {
+    const int lane = threadIdx.x & 63;
+    const int64_t b = (int64_t)blockIdx.x * kPathWaves + uniform_i(threadIdx.x >> 6), width = max_depth + 1;
+    if (b >= B) return;
+    const int len = accepted_len[b];
+    const int up = lane < N ? parent[b * N + lane] : 0, token = lane < N ? node_token[b * N + lane] : 0;
+    const int wanted = lane < max_depth ? tokens[b * width + lane] : 0;      // there are at most 63 levels
+    int st = len < -1 || len > max_depth ? RS_SEQ_DEPTH_EXCEEDED : RS_SEQ_OK;
+    const bool bad = lane < N && (lane == 0 ? up != -1 : up < 0 || up >= lane);
+    if (__ballot(bad) && st == RS_SEQ_OK) st = RS_SEQ_BAD_TREE;
+    uint64_t level = st == RS_SEQ_OK && len >= 0 && len < N ? 1 : 0;
+    for (int d = 0; d < len && level; ++d)
+        level = __ballot(lane > 0 && lane < N && (level >> (up & 63) & 1) && token == __builtin_amdgcn_readlane(wanted, d));
+    if (st == RS_SEQ_OK && len >= 0 && !level) st = RS_SEQ_BAD_TREE;
+    const int on = level ? len + 1 : 0;
+    int mine = -1, n = level ? __builtin_ctzll(level) : 0;
+    for (int i = on - 1; i >= 0; --i) {
+        if (lane == i) mine = n;
+        n = __builtin_amdgcn_readlane(up, n & 63);
+    }
+    for (int64_t i = lane; i < width; i += 64) path[b * width + i] = i < 64 ? mine : -1;
+    if (lane == 0 && status) status[b] = st;
+}
 
 // One workgroup a sequence.  A node of level d carries the tokens if its token is the d-th and
 // its parent carries those before: one step over the nodes for each accepted token, with the
@@ -387,75 +582,91 @@ struct CommitParams {
     int32_t* status;
 };
 
-constexpr int kCommitBlock = 256, kCommitWaves = kCommitBlock / 64, kCommitRows = 64;
+constexpr int kCommitBlock = 256, kCommitWaves = kCommitBlock / 64;
 
 // A lane owns a column of 16 bytes (or one) of all rows of a path, as in the reorder.  Paths
 // ascend, so path[j] >= j: the slot that row i goes to, slots[i], is the source of none after
-// it, and the rows are moved in order, eight loaded before they are stored.
+// it, and the rows are moved in order, eight loaded before they are stored.  Lane i has row i's
+// places, 64 at a time; no wave waits for another.
 __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitParams P) {
-    __shared__ int64_t from[kCommitRows], to[kCommitRows];
-    __shared__ int32_t count;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
     const int32_t* path = P.path + (int64_t)b * P.depth;
     const int32_t* slots = P.slots + (int64_t)b * P.N;
     const uint32_t room = (uint32_t)(P.c.pages * P.c.positions), page = (uint32_t)P.c.positions;
-    if (tid == 0) count = P.depth;
-    __syncthreads();
-    for (int i = tid; i < P.depth; i += kCommitBlock)
-        if (path[i] == -1) {
-            atomicMin(&count, i);
-            break;
-        }
-    __syncthreads();
-    const int n = count;
-    bool order = false, out = false;
-    for (int i = tid; i < n; i += kCommitBlock) {
-        const int x = path[i];
-        if (x < i || x >= P.N || (i > 0 && x <= path[i - 1])) order = true;
-        else out |= (uint32_t)slots[i] >= room || (!P.source && (uint32_t)slots[x] >= room);
-    }
-    const bool wrong = __syncthreads_or(order), outside = __syncthreads_or(out);
-    if (g == 0 && tid == 0 && P.status) P.status[b] = wrong ? RS_SEQ_BAD_TREE : outside ? RS_SEQ_BAD_PAGE : RS_SEQ_OK;
-    if (wrong || outside) return;
-    const uint32_t inner = (uint32_t)P.c.inner, pieces = (uint32_t)P.c.outer * inner;
-    const int64_t bytes = P.c.row_bytes, whole = bytes & ~(int64_t)15;
-    const uint8_t* source = P.source ? P.source : P.cache;
-    const rs_rows& s = P.source ? P.s : P.c;
-    for (int first = 0; first < n; first += kCommitRows) {
-        const int rows = min(n - first, kCommitRows);
-        __syncthreads();
-        if (tid < rows) {
-            const int x = path[first + tid];
-            const uint32_t slot = (uint32_t)slots[first + tid];
-            to[tid] = slot / page * P.c.page_stride + slot % page * P.c.position_stride;
+    // the rows of entries first .. first + 63: how many, and whether they can be moved
+    int64_t from = 0, to = 0;
+    int before = -1;                     // the entry before these
+    bool wrong = false, outside = false;
+    auto look = [&](int first) {
+        const int i = first + lane;
+        const int x = i < P.depth ? path[i] : -1;
+        const uint32_t slot = i < P.N ? (uint32_t)slots[i] : 0xffffffffu;
+        const uint64_t ends = __ballot(x == -1);
+        const int n = ends ? __builtin_ctzll(ends) : 64;
+        const int last = __shfl_up(x, 1);
+        const bool on = lane < n;
+        const bool order = on && (x < i || x >= P.N || x <= (lane == 0 ? before : last));
+        bool out = on && !order && slot >= room;
+        from = to = 0;
+        if (on && !order && !out) {
+            to = slot / page * P.c.page_stride + slot % page * P.c.position_stride;
             if (P.source) {
-                from[tid] = b * P.s.page_stride + x * P.s.position_stride;
+                from = b * P.s.page_stride + x * P.s.position_stride;
             } else {
                 const uint32_t was = (uint32_t)slots[x];
-                from[tid] = was / page * P.c.page_stride + was % page * P.c.position_stride;
+                out = was >= room;
+                from = was / page * P.c.page_stride + was % page * P.c.position_stride;
             }
         }
-        __syncthreads();
+        wrong |= __ballot(order) != 0;
+        outside |= __ballot(out) != 0;
+        before = n == 64 ? __builtin_amdgcn_readlane(x, 63) : before;
+        return n;
+    };
+    int n = look(0);
+    if (n == 64 && P.depth > 64) {       // the whole path is looked at before anything is moved
+        for (int first = 64, m = n; first < P.depth && m == 64; first += 64) m = look(first);
+        before = -1;
+        n = look(0);
+    }
+    if (g == 0 && threadIdx.x == 0 && P.status)
+        P.status[b] = wrong ? RS_SEQ_BAD_TREE : outside ? RS_SEQ_BAD_PAGE : RS_SEQ_OK;
+    if (wrong || outside) return;
+    const uint32_t inner = (uint32_t)P.c.inner, pieces = (uint32_t)P.c.outer * inner;
+    const uint32_t bytes = (uint32_t)P.c.row_bytes, whole = bytes & ~15u;
+    const uint8_t* source = P.source ? P.source : P.cache;
+    const int64_t outer_stride = P.source ? P.s.outer_stride : P.c.outer_stride;
+    const int64_t inner_stride = P.source ? P.s.inner_stride : P.c.inner_stride;
+    auto move_all = [&]() {
         for (uint32_t piece = g * kCommitWaves + wave; piece < pieces; piece += P.G * kCommitWaves) {
-            const uint32_t o = piece / inner, i = piece % inner;
-            const uint8_t* x = source + o * s.outer_stride + i * s.inner_stride;
+            const uint32_t o = uniform_i(piece / inner), i = piece - o * inner;
+            const uint8_t* x = source + o * outer_stride + i * inner_stride;
             uint8_t* y = P.cache + o * P.c.outer_stride + i * P.c.inner_stride;
-            auto move = [&](auto zero, int64_t c) {
+            auto move = [&](auto zero, uint32_t c) {
                 using T = decltype(zero);
-                for (int r = 0; r < rows; r += 8) {
+                for (int r = 0; r < n; r += 8) {
                     T v[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (r + j < rows) v[j] = load_at<T>(x + from[r + j] + c);
+                        if (r + j < n) v[j] = load_at<T>((x + readlane_i64(from, r + j)) + c);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (r + j < rows) store_at<T>(y + to[r + j] + c, v[j]);
+                        if (r + j < n) store_at<T>((y + readlane_i64(to, r + j)) + c, v[j]);
                 }
             };
-            for (int64_t c = lane * 16; c < whole; c += 64 * 16) move(u32x4{}, c);
-            if (whole + lane < bytes) move(uint8_t{}, whole + lane);
+            // what is left of a row: its last 16 bytes once more where they come from elsewhere
+            const uint32_t tail = bytes - whole;
+            const bool again = P.source && tail && whole;
+            for (uint32_t c = lane * 16; c < whole + (again ? 16 : 0); c += 64 * 16)
+                move(u32x4{}, c < whole ? c : bytes - 16);
+            if (!again && lane < tail) move(uint8_t{}, whole + lane);
         }
+    };
+    move_all();
+    for (int first = 64; n == 64 && first < P.depth; first += 64) {
+        n = look(first);
+        move_all();
     }
 }
 
@@ -480,10 +691,12 @@ bool counts_fit(const rs_rows& r, int64_t n) {
 // Workgroups a sequence: enough for the batch to fill the chip some times over, and no more
 // than there are pieces for.
 int32_t groups_for(int64_t pieces, int32_t B, int waves) {
-    constexpr int64_t kWorkgroups = 4096;
+    constexpr int64_t kWorkgroups = 8192;
     const int64_t most = (pieces + waves - 1) / waves, share = (kWorkgroups + B - 1) / B;
     return (int32_t)(most < share ? most : share);
 }
+
+constexpr int64_t kFewBytes = 4 << 20;    // of one beam of every sequence
 
 rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_table, int64_t src_table_stride,
                   void* dst, const rs_rows* dst_rows, const int32_t* dst_table, int64_t dst_table_stride,
@@ -522,30 +735,36 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
     P.W = W;
     P.K = K;
     P.status = out_status;
-    // positions that lie one after another in both are one piece
+    // positions that lie one after another in both are one run
     const int64_t row = src_rows->row_bytes, S = src_rows->positions;
-    P.step = 1;
-    if (src_rows->position_stride == row && dst_rows->position_stride == row) {
-        const int64_t n = (kPieceBytes + row - 1) / row;
-        P.step = (int32_t)(n < S ? n : S);
-    }
-    P.per_page = (int32_t)((S + P.step - 1) / P.step);
-    P.G = groups_for(src_rows->outer * src_rows->inner * P.per_page * (paged ? max_pages : 1), B, kReorderWaves);
-    if ((int64_t)P.G * B > INT_MAX / kReorderBlock) return RS_ERR_UNSUPPORTED;
-    auto launch = [&](auto kmax, auto zero, auto pages) {
-        hipLaunchKernelGGL((rs_reorder_kernel<kmax(), decltype(zero), pages()>), dim3((unsigned)P.G * B),
+    P.together = src_rows->position_stride == row && dst_rows->position_stride == row;
+    auto launch = [&](auto kmax, auto zero, auto u, auto pages) -> rs_status {
+        constexpr int64_t piece = 64 * u() * sizeof(zero);
+        const int64_t run = P.together ? S * row : row, runs = (P.together ? 1 : S) * (paged ? max_pages : 1);
+        const int64_t each = (run + piece - 1) / piece;
+        if (each > INT_MAX || runs > INT_MAX || !counts_fit(*src_rows, each * runs)) return RS_ERR_UNSUPPORTED;
+        P.pieces = (int32_t)each;
+        P.G = groups_for(src_rows->outer * src_rows->inner * each * runs, B, kReorderWaves);
+        if ((int64_t)P.G * B > INT_MAX / kReorderBlock) return RS_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((rs_reorder_kernel<kmax(), decltype(zero), u(), pages()>), dim3((unsigned)P.G * B),
                            dim3(kReorderBlock), 0, (hipStream_t)stream, P);
-        return hipGetLastError();
+        return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
     };
     auto by_beams = [&](auto pages) {
         using std::integral_constant;
-        if (K <= 4) return launch(integral_constant<int, 4>(), u32x4{}, pages);
-        if (K <= 8) return launch(integral_constant<int, 8>(), u32x4{}, pages);
-        if (K <= 16) return launch(integral_constant<int, 16>(), u32x4{}, pages);
-        return launch(integral_constant<int, 64>(), u32x2{}, pages);
+        const integral_constant<int, 1> one;
+        const integral_constant<int, 2> two;
+        // few bytes: every column a lane of its own
+        const bool few = src_rows->outer * src_rows->inner * longest * row <= kFewBytes / B;
+        if (K <= 4) return few ? launch(integral_constant<int, 4>(), u32x4{}, one, pages)
+                               : launch(integral_constant<int, 4>(), u32x4{}, integral_constant<int, 4>(), pages);
+        if (K <= 8) return few ? launch(integral_constant<int, 8>(), u32x4{}, one, pages)
+                               : launch(integral_constant<int, 8>(), u32x4{}, two, pages);
+        if (K <= 16) return launch(integral_constant<int, 16>(), u32x4{}, one, pages);
+        if (K <= 32) return launch(integral_constant<int, 32>(), u32x2{}, one, pages);
+        return launch(integral_constant<int, 64>(), u32x2{}, one, pages);
     };
-    const hipError_t e = paged ? by_beams(std::true_type()) : by_beams(std::false_type());
-    return e == hipSuccess ? RS_OK : RS_ERR_HIP;
+    return paged ? by_beams(std::true_type()) : by_beams(std::false_type());
 }
 
 }  // namespace
@@ -580,13 +799,19 @@ rs_status resispec_plan_cache(const int32_t* kept, const int32_t* added, const i
     if ((int64_t)num_pages * page_size > INT_MAX || (int64_t)max_pages * page_size > INT_MAX) return RS_ERR_UNSUPPORTED;
     PlanParams P{kept, added, held, R, page_size, block_table, table_stride, max_pages, free_pages, free_count, num_pages,
                  out_held, out_free_count, out_starts, T, out_slots, out_positions, out_requests, out_status};
-    constexpr int32_t kRowsAlone = 2048;
-    if (T <= kRowsAlone) {
-        hipLaunchKernelGGL(rs_plan_kernel<true>, dim3(1), dim3(kPlanBlock), 0, (hipStream_t)stream, P);
+    auto step = [&](auto block, unsigned groups) {
+        hipLaunchKernelGGL(rs_plan_step_kernel<block()>, dim3(groups), dim3(block()), 0, (hipStream_t)stream, P);
         return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
-    }
-    hipLaunchKernelGGL(rs_plan_kernel<false>, dim3(1), dim3(kPlanBlock), 0, (hipStream_t)stream, P);
+    };
+    using std::integral_constant;
+    if (R <= 64 && T <= 256) return step(integral_constant<int, 64>(), 1);
+    if (R <= 256 && T <= 1024) return step(integral_constant<int, 256>(), 1);
+    const unsigned groups = T <= 2048 ? 1 : std::min(((unsigned)T + 1023) / 1024, 224u) + kTakers + kGivers + kTellers;
+    if (R <= 1024 && (groups == 1 || (out_held != held && out_free_count != free_count)))
+        return step(integral_constant<int, 1024>(), groups);
+    hipLaunchKernelGGL(rs_plan_kernel, dim3(1), dim3(kPlanBlock), 0, (hipStream_t)stream, P);
     if (hipGetLastError() != hipSuccess) return RS_ERR_HIP;
+    if (T == 0) return RS_OK;
     hipLaunchKernelGGL(rs_plan_rows_kernel, dim3((unsigned)(((int64_t)T + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
                        P);
     return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
@@ -599,7 +824,13 @@ rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_toke
     if (N > RS_MAX_PATH_NODES) return RS_ERR_UNSUPPORTED;
     if (B == 0) return RS_OK;
     if (!parent || !node_token || !tokens || !accepted_len || !out_path) return RS_ERR_INVALID_ARG;
-    const int block = N <= 64 ? 64 : N <= 1024 ? 256 : 1024;
+    if (N <= 64) {
+        hipLaunchKernelGGL(rs_path_wave_kernel, dim3((unsigned)(((int64_t)B + kPathWaves - 1) / kPathWaves)),
+                           dim3(kPathWaves * 64), 0, (hipStream_t)stream, parent, node_token, tokens, accepted_len, B, N,
+                           max_depth, out_path, out_status);
+        return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
+    }
+    const int block = N <= 1024 ? 256 : 1024;
     hipLaunchKernelGGL(rs_path_nodes_kernel, dim3((unsigned)B), dim3(block), (size_t)N * 4, (hipStream_t)stream, parent,
                        node_token, tokens, accepted_len, N, max_depth, out_path, out_status);
     return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
@@ -618,6 +849,7 @@ rs_status resispec_commit_path(void* cache, const rs_rows* cache_rows, const int
     if (cache_rows->pages > INT_MAX || cache_rows->positions > INT_MAX ||
         cache_rows->pages * cache_rows->positions > INT_MAX || !counts_fit(*cache_rows, 1))
         return RS_ERR_UNSUPPORTED;
+    if (cache_rows->row_bytes > INT_MAX) return RS_ERR_UNSUPPORTED;
     if (B == 0) return RS_OK;
     if (!cache || !slots || !path) return RS_ERR_INVALID_ARG;
     CommitParams P{};

@@ -799,6 +799,10 @@ def _settings(logits, lead, R, temperature, top_k, top_p, min_p):
 def _given(t, shape, dtype, logits, name):
     """The address of a contiguous tensor on the rows' device."""
     import torch
+    # the usual case, in the fewest looks
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and
+            t.get_device() == logits.get_device() >= 0 and t.is_contiguous()):
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
     if t.dtype is not dtype:
