@@ -46,6 +46,7 @@ struct BeamParams {
     float temperature;
     const float* temperatures;
     int32_t units, parts;                // units a row, workgroups a row
+    uint32_t by_nch;                     // ceil(2^32 / chunks a row)
     UnitSum* sums;                       // [B * W][units]
     float* maxima;                       // [B * W][units * kUnitChunks], of the chunks
     int32_t *parent, *token, *status;
@@ -188,25 +189,25 @@ __device__ __forceinline__ Place wave_first(Place a) {
     return a;
 }
 
-constexpr int kBins = 1024;              // of scores of chunks, from the best downwards
-constexpr double kBinsPerUnit = 32.0;
+constexpr int kBins = 512;               // of scores of chunks, from the best downwards
+constexpr double kBinsPerUnit = 16.0;
 constexpr int kChunkList = 512, kList = 1024;
 constexpr int kHeld = 2;                 // maxima of chunks a thread holds
-// what is listed besides: two sums' errors, and the rounding of a distance in bins
-constexpr double kSlack = 2.0 * kNear + 1.0e-5;
+// what is listed besides: the errors of two sums and of their logarithms in 32 bits (2e-6 each),
+// and the rounding of a distance in bins (8e-6 where bins are told apart)
+constexpr double kSlack = 2.0 * kNear + 2.0e-5;
 
 struct MergeSmem {
-    double log_sum[RS_MAX_CANDIDATES];
-    double best[RS_MAX_CANDIDATES];      // a beam's best continuation
+    double sum[RS_MAX_CANDIDATES], log_sum[RS_MAX_CANDIDATES];
+    double top[RS_MAX_CANDIDATES];       // a beam's best continuation, by a 32-bit logarithm
     float max[RS_MAX_CANDIDATES], s[RS_MAX_CANDIDATES], T[RS_MAX_CANDIDATES];
-    float cut[RS_MAX_CANDIDATES];        // a row's logits that are listed
-    float below[RS_MAX_CANDIDATES], per_logit[RS_MAX_CANDIDATES];
     int32_t kind[RS_MAX_CANDIDATES];     // 0: no beam, 1: live, 2: ended
-    int32_t status, nchunks, nlist, kth_bin;
+    int32_t status[RS_MAX_CANDIDATES];
+    int32_t nchunks, nlist;
     uint32_t doubt[2];                   // beams to be summed in 64 bits
     double part[kMergeWaves];
+    int32_t bin[kBins];
     union {
-        int32_t bin[kBins];
         struct {
             double score[kList];
             float l[kList];
@@ -220,14 +221,29 @@ struct MergeSmem {
     int32_t chunks[kChunkList];          // those to read again: beam * chunks a row + chunk
 };
 
+// Inclusive prefix sum over the 64 lanes, as wave_incl_scan.
+template <int CTRL, int ROWMASK>
+__device__ __forceinline__ int dpp_or_zero(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWMASK, 0xF, true);
+}
+__device__ __forceinline__ int wave_incl_scan_i(int v) {
+    v += dpp_or_zero<kDppRowShr1, 0xF>(v);
+    v += dpp_or_zero<kDppRowShr2, 0xF>(v);
+    v += dpp_or_zero<kDppRowShr4, 0xF>(v);
+    v += dpp_or_zero<kDppRowShr8, 0xF>(v);
+    v += dpp_or_zero<kDppRowBcast15, 0xA>(v);
+    v += dpp_or_zero<kDppRowBcast31, 0xC>(v);
+    return v;
+}
+
 template <typename In, int VEC>
 struct Merge {
     using C = Chunk<In, VEC>;
-    using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
     const BeamParams& P;
     MergeSmem& sm;
     const int64_t b, r0;
     const int tid, lane, wave, nch;
+    const uint32_t by_nch;               // i / nch is the high half of i * by_nch for i < 2^18, nch <= 2^12
 
     __device__ __forceinline__ const In* row(int w) const {
         return reinterpret_cast<const In*>(P.logits) + (r0 + w) * P.stride;
@@ -235,10 +251,11 @@ struct Merge {
     __device__ __forceinline__ float chunk_max(int w, int c) const {
         return P.maxima[(r0 + w) * (int64_t)nch + c];
     }
-    __device__ __forceinline__ double score(int w, float l) const {
+    __device__ __forceinline__ double score(int w, float l, double log_sum) const {
         if (sm.kind[w] == 2) return (double)sm.s[w];
-        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - sm.log_sum[w]) + (double)sm.s[w];
+        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - log_sum) + (double)sm.s[w];
     }
+    __device__ __forceinline__ double score(int w, float l) const { return score(w, l, sm.log_sum[w]); }
 
     // Every beam's kind, maximum and sum, a wave a beam.
     __device__ __forceinline__ void sums() {
@@ -251,11 +268,12 @@ struct Merge {
             int st = RS_SEQ_OK;
             if (!(s < INFINITY) || (kind == 1 && !(T > 0.0f && T < INFINITY))) st = RS_SEQ_BAD_PARAM;
             float m = -INFINITY;
-            double sum = 0.0;
+            double sum = 1.0;
             if (kind == 1 && st == RS_SEQ_OK) {
                 m = x.max;
                 for (int u = lane + 64; u < P.units; u += 64) m = fmaxf(m, units[u].max);
                 m = wave_max(m);
+                sum = 0.0;
                 const double c2 = 1.4426950408889634 / (double)T;
                 auto add = [&](const UnitSum& y) {
                     if (y.sum != 0.0) sum += y.sum * exp2_64(((double)y.max - (double)m) * c2);
@@ -266,14 +284,13 @@ struct Merge {
                 if (!(m > -INFINITY && m < INFINITY && sum < INFINITY)) st = RS_SEQ_UNDERFLOW;
             }
             if (lane == 0) {
-                const double log_sum = kind == 1 && st == RS_SEQ_OK ? log(sum) : 0.0;
                 sm.kind[w] = kind;
                 sm.s[w] = s;
                 sm.T[w] = T;
                 sm.max[w] = m;
-                sm.log_sum[w] = log_sum;
-                sm.best[w] = (double)s - log_sum;
-                if (st != RS_SEQ_OK) atomicMax(&sm.status, st);
+                sm.sum[w] = sum;
+                sm.top[w] = (double)s - (double)(__builtin_amdgcn_logf((float)sum) * 0.693147181f);
+                sm.status[w] = st;
             }
         }
     }
@@ -282,8 +299,7 @@ struct Merge {
     __device__ __forceinline__ void sum_again(int w) {
         const double c2 = 1.4426950408889634 / (double)sm.T[w], md = (double)sm.max[w];
         double sum = 0.0;
-        for (int c = wave; c < nch; c += kMergeWaves) {
-            if (c * (int64_t)kChunk >= P.V) break;
+        for (int c = wave; c < nch && c * (int64_t)kChunk < P.V; c += kMergeWaves) {
             C chunk;
             chunk.template load<false>(row(w), c, P.V);
             chunk.settle(c, P.V);
@@ -303,77 +319,79 @@ struct Merge {
         }
     }
 
-    // How far a score is below the best, in bins.
-    __device__ __forceinline__ float depth(double best, double bins_per_unit, double s) const {
-        return (float)fmin((best - s) * bins_per_unit, (double)FLT_MAX);
-    }
-    __device__ __forceinline__ void count(float d) { atomicAdd(&sm.bin[(int)fminf(d, kBins - 1)], 1); }
+    // A distance from the reference, in bins, counted in its bin.
+    __device__ __forceinline__ void count(float d) { atomicAdd(&sm.bin[(int)fminf(fmaxf(d, 0.0f), kBins - 1)], 1); }
 
-    // The bin in which the k-th counted lies, or the last one if there are fewer.
-    __device__ __forceinline__ int bin_of_kth() {
-        __syncthreads();
-        if (wave == 0) {
-            constexpr int kLaneBins = kBins / 64;
-            int n[kLaneBins], mine = 0;
+    // The bin in which the k-th counted lies, or the last one if there are fewer.  Every wave
+    // looks for itself.
+    __device__ __forceinline__ int bin_of_kth() const {
+        constexpr int kLaneBins = kBins / 64;
+        int n[kLaneBins], mine = 0;
 #pragma unroll
-            for (int i = 0; i < kLaneBins; ++i) mine += n[i] = sm.bin[lane * kLaneBins + i];
-            int upto = mine;
+        for (int i = 0; i < kLaneBins; ++i) mine += n[i] = sm.bin[lane * kLaneBins + i];
+        int upto = wave_incl_scan_i(mine);
+        const uint64_t reached = __ballot(upto >= P.k);
+        int kth = kLaneBins - 1;
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int x = __shfl_up(upto, d);
-                if (lane >= d) upto += x;
-            }
-            const uint64_t reached = __ballot(upto >= P.k);
-            if (lane == (reached ? __builtin_ctzll(reached) : 63)) {
-                int kth = kLaneBins - 1;
-#pragma unroll
-                for (int i = kLaneBins - 1; i >= 0; --i) {
-                    if (upto >= P.k) kth = i;
-                    upto -= n[i];
-                }
-                sm.kth_bin = lane * kLaneBins + kth;
-            }
+        for (int i = kLaneBins - 1; i >= 0; --i) {
+            if (upto >= P.k) kth = i;
+            upto -= n[i];
         }
-        __syncthreads();
-        return sm.kth_bin;
+        const int at = reached ? __builtin_ctzll(reached) : 63;
+        return at * kLaneBins + __builtin_amdgcn_readlane(kth, at);
     }
 
-    // Rows' least logits whose scores may be within `far` of the best.
-    __device__ __forceinline__ void cut_at(double best, double far) {
-        if (tid < P.W && sm.kind[tid] == 1) {
-            const double l = (best - far - (double)sm.s[tid] + sm.log_sum[tid]) * (double)sm.T[tid] + (double)sm.max[tid];
-            sm.cut[tid] = fmaxf((float)(l - fabs(l) * 0x1p-23), -FLT_MAX);
-        }
-        __syncthreads();
-    }
-
-    // body(w, l, j) for what the listed chunks hold above the cuts.
+    // body(w, l, j, score) for what the listed chunks hold within `far` of the reference.
     template <typename Body>
-    __device__ __forceinline__ void each_listed(Body&& body) {
+    __device__ __forceinline__ void each_listed(double reference, double far, Body&& body) {
         const int n = sm.nchunks;
-        for (int i = wave; i < n; i += kMergeWaves) {
-            const int id = __builtin_amdgcn_readfirstlane(sm.chunks[i]), w = id / nch, c = id - w * nch;
-            if (sm.kind[w] == 2) {
-                if (lane == 0) body(w, 0.0f, P.end_token);
-                continue;
-            }
-            C chunk;
-            chunk.template load<false>(row(w), c, P.V);
-            chunk.settle(c, P.V);
-            float v[C::N];
-            chunk.unpack(v);
-            const float cut = sm.cut[w];
+        // two chunks a wave on their way at a time
+        for (int i0 = wave; i0 < n; i0 += 2 * kMergeWaves) {
+            C chunk[2];
+            int w[2], c[2];
 #pragma unroll
-            for (int e = 0; e < C::N; ++e)
-                if (v[e] >= cut) body(w, v[e], C::at(c, e));
+            for (int h = 0; h < 2; ++h) {
+                const int i = i0 + h * kMergeWaves;
+                const int id = __builtin_amdgcn_readfirstlane(sm.chunks[i < n ? i : i0]);
+                w[h] = id / nch;
+                c[h] = id - w[h] * nch;
+                if (i < n && sm.kind[w[h]] == 1) chunk[h].template load<false>(row(w[h]), c[h], P.V);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (i0 + h * kMergeWaves >= n) break;
+                if (sm.kind[w[h]] == 2) {
+                    if (lane == 0) body(w[h], 0.0f, P.end_token, (double)sm.s[w[h]]);
+                    continue;
+                }
+                const double log_sum = sm.log_sum[w[h]];
+                // the row's least logit within reach, or one below it
+                const double least = (reference - far - (double)sm.s[w[h]] + log_sum) * (double)sm.T[w[h]] + (double)sm.max[w[h]];
+                const float cut = fmaxf((float)(least - fabs(least) * 0x1p-23), -FLT_MAX);
+                chunk[h].settle(c[h], P.V);
+                float v[C::N];
+                chunk[h].unpack(v);
+                // few lanes have any: one after another, in little code
+                uint32_t hits = 0;
+#pragma unroll
+                for (int e = 0; e < C::N; ++e) hits |= (uint32_t)(v[e] >= cut) << e;
+                while (hits) {
+                    const int at = __builtin_ctz(hits);
+                    hits &= hits - 1;
+                    float l = v[0];
+#pragma unroll
+                    for (int e = 1; e < C::N; ++e) l = at == e ? v[e] : l;
+                    body(w[h], l, C::at(c[h], at), score(w[h], l, log_sum));
+                }
+            }
         }
         __syncthreads();
     }
-    __device__ __forceinline__ void list_listed() {
-        each_listed([&](int w, float l, int j) {
+    __device__ __forceinline__ void list_listed(double reference, double far) {
+        each_listed(reference, far, [&](int w, float l, int j, double s) {
             const int at = atomicAdd(&sm.nlist, 1);
             if (at < kList) {
-                sm.score[at] = score(w, l);
+                sm.score[at] = s;
                 sm.l[at] = l;
                 sm.w[at] = w;
                 sm.j[at] = j;
@@ -386,24 +404,17 @@ struct Merge {
     // maxima: those of the chunks tid, tid + kMergeBlock ..
     __device__ __forceinline__ bool list(const float (&maxima)[kHeld]) {
         const int n = P.W * nch;
-        double best = -INFINITY;
-        for (int w = 0; w < P.W; ++w)
-            if (sm.kind[w]) best = fmax(best, sm.best[w]);
-        // a row's best is this far below the best, and a unit of logits so many of scores
-        if (tid < P.W) {
-            sm.below[tid] = (float)(best - sm.best[tid]);
-            sm.per_logit[tid] = (float)(1.0 / (double)sm.T[tid]);
-        }
-        for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
-        __syncthreads();
-        // how far the score of chunk i's first element is below the best, in bins, in 32 bits:
-        // 2^-22 of it off, 2e-4 bins at most where bins are told apart
+        // a score near the best: distances are from here
+        const float high = wave_max(lane < P.W ? (float)sm.top[lane] : -INFINITY);
+        const double reference = high > -INFINITY ? (double)high : 0.0;
+        // how far the score of chunk i's first element is below it, in bins
         auto key = [&](int i, float l) {
-            const int w = i / nch, kind = sm.kind[w];
+            const int w = (int)__umulhi((uint32_t)i, by_nch), kind = sm.kind[w];
             if (kind == 0 || (kind == 2 && i != w * nch)) return INFINITY;
-            if (kind == 2) return sm.below[w] * (float)kBinsPerUnit;
+            const float below = (float)(reference - sm.top[w]);
+            if (kind == 2) return below * (float)kBinsPerUnit;
             if (l == -INFINITY) return INFINITY;
-            return fminf((sm.below[w] + (sm.max[w] - l) * sm.per_logit[w]) * (float)kBinsPerUnit, FLT_MAX);
+            return fminf((below + (sm.max[w] - l) / sm.T[w]) * (float)kBinsPerUnit, FLT_MAX);
         };
         float held[kHeld];
 #pragma unroll
@@ -419,6 +430,7 @@ struct Merge {
             }
         };
         later([&](int, float d) { count(d); });
+        __syncthreads();
         int bin = bin_of_kth();
         // the last bin has no end, so all chunks are listed
         const bool all = bin == kBins - 1;
@@ -432,10 +444,10 @@ struct Merge {
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) pick(tid + h * kMergeBlock, held[h]);
         later(pick);
-        cut_at(best, far);
+        __syncthreads();
         if (sm.nchunks > kChunkList) return false;
         if (!all) {
-            list_listed();
+            list_listed(reference, far);
             if (sm.nlist <= kList) return true;
         }
         // finer, by the elements themselves
@@ -444,10 +456,11 @@ struct Merge {
         for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
         if (tid == 0) sm.nlist = 0;
         __syncthreads();
-        each_listed([&](int w, float l, int) { count(depth(best, bins_per_unit, score(w, l))); });
+        each_listed(reference, far, [&](int, float, int, double s) {
+            count((float)fmin((reference - s) * bins_per_unit, (double)FLT_MAX));
+        });
         bin = bin_of_kth();
-        if (bin < kBins - 1) cut_at(best, (bin + 1) / bins_per_unit + kSlack);
-        list_listed();
+        list_listed(reference, bin < kBins - 1 ? (bin + 1) / bins_per_unit + kSlack : far);
         return sm.nlist <= kList;
     }
 
@@ -567,21 +580,25 @@ struct Merge {
     }
 
     __device__ __forceinline__ void run() {
-        if (tid == 0) {
-            sm.status = RS_SEQ_OK;
-            sm.nchunks = sm.nlist = 0;
-            sm.doubt[0] = sm.doubt[1] = 0;
-        }
         float maxima[kHeld];
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
             const int i = tid + h * kMergeBlock;
             maxima[h] = i < P.W * nch ? P.maxima[r0 * nch + i] : -INFINITY;
         }
-        __syncthreads();
+        for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
+        if (tid == 0) {
+            sm.nchunks = sm.nlist = 0;
+            sm.doubt[0] = sm.doubt[1] = 0;
+        }
         sums();
         __syncthreads();
-        const int status = sm.status;
+        const int st = lane < P.W ? sm.status[lane] : RS_SEQ_OK;
+        const int status = __ballot(st == RS_SEQ_BAD_PARAM) ? RS_SEQ_BAD_PARAM
+                           : __ballot(st != RS_SEQ_OK)      ? RS_SEQ_UNDERFLOW
+                                                            : RS_SEQ_OK;
+        // the sums' logarithms, by one wave while the others look for what to read
+        if (wave == kMergeWaves - 1 && lane < P.W) sm.log_sum[lane] = log(sm.sum[lane]);
         int found = 0;
         if (status == RS_SEQ_OK) {
             if (list(maxima)) {
@@ -615,7 +632,7 @@ __global__ void __launch_bounds__(kMergeBlock) rs_beam_merge_kernel(const BeamPa
     __shared__ MergeSmem sm;
     const int tid = threadIdx.x;
     Merge<In, VEC> m{P, sm, (int64_t)blockIdx.x, (int64_t)blockIdx.x * P.W, tid, tid & 63,
-                     __builtin_amdgcn_readfirstlane(tid >> 6), P.units * kUnitChunks};
+                     __builtin_amdgcn_readfirstlane(tid >> 6), P.units * kUnitChunks, P.by_nch};
     m.run();
 }
 
@@ -668,6 +685,7 @@ rs_status resispec_beam_select(const void* logits, int64_t row_stride, const flo
     P.temperature = filter->temperature;
     P.temperatures = filter->temperatures;
     P.units = units_of(V);
+    P.by_nch = (uint32_t)(((uint64_t)1 << 32) / (P.units * kUnitChunks)) + 1;
     P.sums = static_cast<UnitSum*>(workspace);
     P.maxima = reinterpret_cast<float*>(P.sums + (int64_t)B * W * P.units);
     P.parent = out_parent;
