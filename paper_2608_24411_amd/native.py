@@ -845,6 +845,31 @@ def _row_call(logits, stream, call):
         return call(_stream(stream))
 
 
+def _handle(like, stream):
+    """The current stream's handle where the tensors' device is the current one and no stream is
+    given, the usual case; else None, and the call is to be made again by _elsewhere."""
+    if stream is None:
+        device, raw = _runtime()
+        d = like.get_device()
+        if device() == d:
+            return raw(d)
+    return None
+
+
+def _elsewhere(like, stream, call, *args, **kw):
+    """call(*args, **kw) with the tensors' device, and `stream` if given, the current ones."""
+    import torch
+    if not like.is_cuda:
+        raise ValueError("device tensors are required, got %s" % like.device)
+    if stream is None:
+        with torch.cuda.device(like.device):
+            return call(*args, **kw)
+    if stream.device != like.device:
+        raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, like.device))
+    with torch.cuda.stream(stream):
+        return call(*args, **kw)
+
+
 def resispec_sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out_token=None,
                     out_logprob=None, out_kept=None, out_status=None, stream=None):
     """Draws from rows of logits under temperature, top-k, top-p and min-p, one for each of the
@@ -973,23 +998,30 @@ def resispec_beam_select(logits, scores, *, k=None, temperature=1.0, ended=None,
     ep = None
     if ended is not None:
         ep = _given(ended, shape, torch.bool if ended.dtype is torch.bool else torch.uint8, logits, "ended")
-    dev, to = logits.device, (B, k)
-    need = lib.resispec_beam_workspace_bytes(B, W, V)
-
-    def call(handle):
-        parent = torch.empty(to, dtype=torch.int32, device=dev) if out_parent is None else out_parent
-        token = torch.empty(to, dtype=torch.int32, device=dev) if out_token is None else out_token
-        score = torch.empty(to, dtype=torch.float32, device=dev) if out_score is None else out_score
-        st = torch.empty(B, dtype=torch.int32, device=dev) if out_status is None else out_status
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev) if workspace is None else workspace
-        _check(lib.resispec_beam_select(ptr, step, sp, ep, end_token, B, W, V, k, ctypes.byref(f),
-                                        _given(parent, to, torch.int32, logits, "out_parent"),
-                                        _given(token, to, torch.int32, logits, "out_token"),
-                                        _given(score, to, torch.float32, logits, "out_score"),
-                                        _given(st, (B,), torch.int32, logits, "out_status"),
-                                        _given(ws, ws.shape, torch.uint8, logits, "workspace"), ws.numel(), handle))
-        return parent, token, score, st
-    return _row_call(logits, stream, call)
+    handle = _handle(logits, stream)
+    if handle is None:
+        return _elsewhere(logits, stream, resispec_beam_select, logits, scores, k=k, temperature=temperature, ended=ended,
+                          end_token=end_token, out_parent=out_parent, out_token=out_token, out_score=out_score,
+                          out_status=out_status, workspace=workspace)
+    i32, to = torch.int32, (B, k)
+    if out_parent is None:
+        out_parent = torch.empty(to, dtype=i32, device=logits.device)
+    if out_token is None:
+        out_token = torch.empty(to, dtype=i32, device=logits.device)
+    if out_score is None:
+        out_score = torch.empty(to, dtype=torch.float32, device=logits.device)
+    if out_status is None:
+        out_status = torch.empty(B, dtype=i32, device=logits.device)
+    if workspace is None:
+        workspace = torch.empty(max(1, lib.resispec_beam_workspace_bytes(B, W, V)), dtype=torch.uint8, device=logits.device)
+    _check(lib.resispec_beam_select(ptr, step, sp, ep, end_token, B, W, V, k, f,
+                                    _given(out_parent, to, i32, logits, "out_parent"),
+                                    _given(out_token, to, i32, logits, "out_token"),
+                                    _given(out_score, to, torch.float32, logits, "out_score"),
+                                    _given(out_status, (B,), i32, logits, "out_status"),
+                                    _given(workspace, workspace.shape, torch.uint8, logits, "workspace"),
+                                    workspace.numel(), handle))
+    return out_parent, out_token, out_score, out_status
 
 
 @functools.lru_cache(maxsize=256)
@@ -1110,13 +1142,15 @@ def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengt
     if dst.pages != B * K:
         raise ValueError("out has %d beams, expected %d" % (dst.pages, B * K))
     lp = None if lengths is None else _given(lengths, (B,), torch.int32, state, "lengths")
-
-    def call(handle):
-        st = torch.empty(B, dtype=torch.int32, device=state.device) if out_status is None else out_status
-        _check(lib.resispec_beam_reorder(state.data_ptr(), src, to, dst, pp, lp, B, W, K,
-                                         _given(st, (B,), torch.int32, state, "out_status"), handle))
-        return (state if out is None else out), st
-    return _row_call(state, stream, call)
+    handle = _handle(state, stream)
+    if handle is None:
+        return _elsewhere(state, stream, resispec_beam_reorder, state, parent, beam_dim=beam_dim, position_dim=position_dim,
+                          lengths=lengths, out=out, out_status=out_status)
+    if out_status is None:
+        out_status = torch.empty(B, dtype=torch.int32, device=state.device)
+    _check(lib.resispec_beam_reorder(state.data_ptr(), src, to, dst, pp, lp, B, W, K,
+                                     _given(out_status, (B,), torch.int32, state, "out_status"), handle))
+    return (state if out is None else out), out_status
 
 
 def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim=0, position_dim=1, out_table=None,
@@ -1143,13 +1177,15 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
         raise ValueError("a move within the cache needs as many beams as there are, %d, got %d" % (W, K))
     to, dst = _moved_to(cache, src, span, out, "out", page_dim, position_dim)
     lp = _given(lengths, (B,), torch.int32, cache, "lengths")
-
-    def call(handle):
-        st = torch.empty(B, dtype=torch.int32, device=cache.device) if out_status is None else out_status
-        _check(lib.resispec_beam_reorder_paged(cache.data_ptr(), src, tp, tstep, to, dst, op, ostep, n, pp, lp, B, W, K,
-                                               _given(st, (B,), torch.int32, cache, "out_status"), handle))
-        return (cache if out is None else out), st
-    return _row_call(cache, stream, call)
+    handle = _handle(cache, stream)
+    if handle is None:
+        return _elsewhere(cache, stream, resispec_beam_reorder_paged, cache, block_table, parent, lengths,
+                          page_dim=page_dim, position_dim=position_dim, out_table=out_table, out=out, out_status=out_status)
+    if out_status is None:
+        out_status = torch.empty(B, dtype=torch.int32, device=cache.device)
+    _check(lib.resispec_beam_reorder_paged(cache.data_ptr(), src, tp, tstep, to, dst, op, ostep, n, pp, lp, B, W, K,
+                                           _given(out_status, (B,), torch.int32, cache, "out_status"), handle))
+    return (cache if out is None else out), out_status
 
 
 # ------------------------------------------------------------------- cache --
@@ -1168,8 +1204,9 @@ def resispec_plan_cache(kept, added, held, block_table, free_pages, free_count, 
     import torch
     if not isinstance(kept, torch.Tensor) or kept.dim() != 1:
         raise ValueError("kept must be a [R] tensor")
-    R, like = kept.shape[0], kept
-    kp, ap, hp = (_given(t, (R,), torch.int32, like, n) for t, n in ((kept, "kept"), (added, "added"), (held, "held")))
+    R, like, shape = kept.shape[0], kept, kept.shape
+    kp, ap = _given(kept, shape, torch.int32, like, "kept"), _given(added, shape, torch.int32, like, "added")
+    hp = _given(held, shape, torch.int32, like, "held")
     tp, step, n = _table(block_table, R, like, "block_table")
     if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
         raise ValueError("free_pages must be a [pages] tensor")
@@ -1185,22 +1222,37 @@ def resispec_plan_cache(kept, added, held, block_table, free_pages, free_count, 
     if T < 0:
         raise ValueError("out_slots must be a [T] tensor, max_slots >= 0")
     page_size = _int32(page_size, "page_size")
-
-    def call(handle):
-        e = lambda given, m: torch.empty(m, dtype=torch.int32, device=kept.device) if given is None else given  # noqa: E731
-        slots, positions, requests = e(out_slots, T), e(out_positions, T), e(out_requests, T)
-        starts, got, count, st = e(out_starts, R + 1), e(out_held, R), e(out_free_count, 1), e(out_status, R)
-        i32 = torch.int32
-        _check(lib.resispec_plan_cache(kp, ap, hp, R, page_size, tp, step, n, fp, cp, pages,
-                                       _given(got, (R,), i32, like, "out_held"),
-                                       _given(count, (1,), i32, like, "out_free_count"),
-                                       _given(starts, (R + 1,), i32, like, "out_starts"), T,
-                                       _given(slots, (T,), i32, like, "out_slots"),
-                                       _given(positions, (T,), i32, like, "out_positions"),
-                                       _given(requests, (T,), i32, like, "out_requests"),
-                                       _given(st, (R,), i32, like, "out_status"), handle))
-        return slots, positions, requests, starts, got, count, st
-    return _row_call(like, stream, call)
+    handle = _handle(like, stream)
+    if handle is None:
+        return _elsewhere(like, stream, resispec_plan_cache, kept, added, held, block_table, free_pages, free_count,
+                          page_size=page_size, max_slots=T, out_slots=out_slots, out_positions=out_positions,
+                          out_requests=out_requests, out_starts=out_starts, out_held=out_held,
+                          out_free_count=out_free_count, out_status=out_status)
+    i32, dev = torch.int32, kept.device
+    if out_slots is None:
+        out_slots = torch.empty(T, dtype=i32, device=dev)
+    if out_positions is None:
+        out_positions = torch.empty(T, dtype=i32, device=dev)
+    if out_requests is None:
+        out_requests = torch.empty(T, dtype=i32, device=dev)
+    if out_starts is None:
+        out_starts = torch.empty(R + 1, dtype=i32, device=dev)
+    if out_held is None:
+        out_held = torch.empty(R, dtype=i32, device=dev)
+    if out_free_count is None:
+        out_free_count = torch.empty(1, dtype=i32, device=dev)
+    if out_status is None:
+        out_status = torch.empty(R, dtype=i32, device=dev)
+    requests, rows = (R,), (T,)
+    _check(lib.resispec_plan_cache(kp, ap, hp, R, page_size, tp, step, n, fp, cp, pages,
+                                   _given(out_held, requests, i32, like, "out_held"),
+                                   _given(out_free_count, (1,), i32, like, "out_free_count"),
+                                   _given(out_starts, (R + 1,), i32, like, "out_starts"), T,
+                                   _given(out_slots, rows, i32, like, "out_slots"),
+                                   _given(out_positions, rows, i32, like, "out_positions"),
+                                   _given(out_requests, rows, i32, like, "out_requests"),
+                                   _given(out_status, requests, i32, like, "out_status"), handle))
+    return out_slots, out_positions, out_requests, out_starts, out_held, out_free_count, out_status
 
 
 def resispec_accepted_path(parent, node_token, tokens, accepted_len, *, out_path=None, out_status=None, stream=None):
@@ -1215,15 +1267,17 @@ def resispec_accepted_path(parent, node_token, tokens, accepted_len, *, out_path
     i32, like = torch.int32, parent
     pp, np_ = _given(parent, (B, N), i32, like, "parent"), _given(node_token, (B, N), i32, like, "node_token")
     tp, lp = _given(tokens, shape, i32, like, "tokens"), _given(accepted_len, (B,), i32, like, "accepted_len")
-
-    def call(handle):
-        path = torch.empty(shape, dtype=i32, device=parent.device) if out_path is None else out_path
-        st = torch.empty(B, dtype=i32, device=parent.device) if out_status is None else out_status
-        _check(lib.resispec_accepted_path(pp, np_, tp, lp, B, N, shape[1] - 1,
-                                          _given(path, shape, i32, like, "out_path"),
-                                          _given(st, (B,), i32, like, "out_status"), handle))
-        return path, st
-    return _row_call(like, stream, call)
+    handle = _handle(like, stream)
+    if handle is None:
+        return _elsewhere(like, stream, resispec_accepted_path, parent, node_token, tokens, accepted_len, out_path=out_path,
+                          out_status=out_status)
+    if out_path is None:
+        out_path = torch.empty(shape, dtype=i32, device=parent.device)
+    if out_status is None:
+        out_status = torch.empty(B, dtype=i32, device=parent.device)
+    _check(lib.resispec_accepted_path(pp, np_, tp, lp, B, N, shape[1] - 1, _given(out_path, shape, i32, like, "out_path"),
+                                      _given(out_status, (B,), i32, like, "out_status"), handle))
+    return out_path, out_status
 
 
 def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, position_dim=1, out_status=None, stream=None):
@@ -1250,10 +1304,12 @@ def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, positio
             raise ValueError("source must be apart from the cache")
         if rows_of.pages != B or rows_of.positions != N:
             raise ValueError("source has %d trees of %d nodes, expected %d of %d" % (rows_of.pages, rows_of.positions, B, N))
-
-    def call(handle):
-        st = torch.empty(B, dtype=i32, device=cache.device) if out_status is None else out_status
-        _check(lib.resispec_commit_path(cache.data_ptr(), rows, sp, pp, at, rows_of, B, N, path.shape[1],
-                                        _given(st, (B,), i32, cache, "out_status"), handle))
-        return cache, st
-    return _row_call(cache, stream, call)
+    handle = _handle(cache, stream)
+    if handle is None:
+        return _elsewhere(cache, stream, resispec_commit_path, cache, slots, path, source=source, page_dim=page_dim,
+                          position_dim=position_dim, out_status=out_status)
+    if out_status is None:
+        out_status = torch.empty(B, dtype=i32, device=cache.device)
+    _check(lib.resispec_commit_path(cache.data_ptr(), rows, sp, pp, at, rows_of, B, N, path.shape[1],
+                                    _given(out_status, (B,), i32, cache, "out_status"), handle))
+    return cache, out_status
