@@ -629,7 +629,7 @@ size_t resispec_beam_workspace_bytes(int32_t B, int32_t W, int32_t V);
  *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_PARAM: a parent or a length
  *                 out of its range; nothing of that sequence is moved.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, W or K <= 0, or layouts that do not fit;
- * RS_ERR_UNSUPPORTED for W or K > RS_MAX_CANDIDATES, or 2^31 rows of one beam and layer or
+ * RS_ERR_UNSUPPORTED for W or K > RS_MAX_CANDIDATES, or states of 2^31 rows a sequence's beam or
  * more.  B = 0 is a no-op.
  */
 rs_status resispec_beam_reorder(const void* src, const rs_rows* src_rows, void* dst,
@@ -733,8 +733,8 @@ rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_toke
  *                 ascend or has a node outside [0, N); RS_SEQ_BAD_PAGE: a slot of it outside
  *                 the cache.  Nothing of that sequence is moved.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, N or depth <= 0, or layouts that do not fit;
- * RS_ERR_UNSUPPORTED for N or depth > RS_MAX_PATH_NODES or pages * positions >= 2^31.  B = 0 is a
- * no-op.
+ * RS_ERR_UNSUPPORTED for N or depth > RS_MAX_PATH_NODES, pages * positions >= 2^31 or rows of
+ * 2^31 bytes or more.  B = 0 is a no-op.
  */
 rs_status resispec_commit_path(void* cache, const rs_rows* cache_rows, const int32_t* slots,
                                const int32_t* path, const void* source,

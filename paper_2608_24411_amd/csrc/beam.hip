@@ -28,7 +28,8 @@ constexpr int kUnitChunks = 4;           // chunks of a unit
 constexpr int kUnit = kChunk * kUnitChunks;
 constexpr int kRowsBlock = 256, kRowsWaves = kRowsBlock / 64;
 constexpr int kMergeBlock = 1024, kMergeWaves = kMergeBlock / 64;
-constexpr double kNear = 3.0e-6;         // scores this close are told apart in 64 bits
+// Scores this close are told apart by sums in 64 bits; besides, a score has its own rounding.
+constexpr double kNear = 3.0e-6, kNearOf = 0x1p-50;
 
 struct UnitSum {
     double sum;                          // of 2^((l - max) c)
@@ -406,13 +407,13 @@ struct Merge {
         const int n = P.W * nch;
         // a score near the best: distances are from here
         const float high = wave_max(lane < P.W ? (float)sm.top[lane] : -INFINITY);
-        const double reference = high > -INFINITY ? (double)high : 0.0;
+        const double reference = high > -INFINITY ? (double)high : 0.0, slack = kSlack + 4.0 * fabs(reference) * kNearOf;
         // how far the score of chunk i's first element is below it, in bins
         auto key = [&](int i, float l) {
             const int w = (int)__umulhi((uint32_t)i, by_nch), kind = sm.kind[w];
             if (kind == 0 || (kind == 2 && i != w * nch)) return INFINITY;
             const float below = (float)(reference - sm.top[w]);
-            if (kind == 2) return below * (float)kBinsPerUnit;
+            if (kind == 2) return fminf(below * (float)kBinsPerUnit, FLT_MAX);
             if (l == -INFINITY) return INFINITY;
             return fminf((below + (sm.max[w] - l) / sm.T[w]) * (float)kBinsPerUnit, FLT_MAX);
         };
@@ -434,8 +435,8 @@ struct Merge {
         int bin = bin_of_kth();
         // the last bin has no end, so all chunks are listed
         const bool all = bin == kBins - 1;
-        const double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + kSlack;
-        const float limit = all ? FLT_MAX : (float)((far + kSlack) * kBinsPerUnit);
+        const double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + slack;
+        const float limit = all ? FLT_MAX : (float)((far + slack) * kBinsPerUnit);
         auto pick = [&](int i, float d) {
             if (!(d <= limit)) return;
             const int at = atomicAdd(&sm.nchunks, 1);
@@ -460,7 +461,7 @@ struct Merge {
             count((float)fmin((reference - s) * bins_per_unit, (double)FLT_MAX));
         });
         bin = bin_of_kth();
-        list_listed(reference, bin < kBins - 1 ? (bin + 1) / bins_per_unit + kSlack : far);
+        list_listed(reference, bin < kBins - 1 ? (bin + 1) / bins_per_unit + slack : far);
         return sm.nlist <= kList;
     }
 
@@ -481,7 +482,8 @@ struct Merge {
             for (int x = sub; x < n; x += 16) {
                 const Place other = {sm.score[x], sm.w[x], sm.l[x], sm.j[x]};
                 ahead += before(other, mine);
-                if (other.w != mine.w && fabs(other.score - mine.score) <= kNear) close |= 1ull << other.w;
+                if (other.w != mine.w && fabs(other.score - mine.score) <= kNear + fabs(mine.score) * kNearOf)
+                    close |= 1ull << other.w;
             }
             ahead += dpp_i<kDppXor1>(ahead);
             ahead += dpp_i<kDppXor2>(ahead);

@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(BLOCK) rs_plan_step_kernel(const PlanParams P)
         if (alone) from = 0, groups = 1;
         const int g = (int)blockIdx.x - from;
         if (g < 0 || g >= groups) return;
-        for (int x = g * BLOCK + tid; x < n; x += groups * BLOCK) body(x);
+        for (uint32_t x = g * BLOCK + tid; x < (uint32_t)n; x += groups * BLOCK) body((int)x);
     };
     job(nrows + kTakers, kGivers, F, [&](int x) { P.free_pages[count + x] = given_page(x); });
     job(nrows, kTakers, A, [&](int x) {
@@ -597,6 +597,7 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
     // the rows of entries first .. first + 63: how many, and whether they can be moved
     int64_t from = 0, to = 0;
     int before = -1;                     // the entry before these
+    int start = 0;                       // the first row that moves
     bool wrong = false, outside = false;
     auto look = [&](int first) {
         const int i = first + lane;
@@ -622,6 +623,8 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
         wrong |= __ballot(order) != 0;
         outside |= __ballot(out) != 0;
         before = n == 64 ? __builtin_amdgcn_readlane(x, 63) : before;
+        // rows that are where they belong are the path's first
+        start = P.source ? 0 : __popcll(__ballot(on && x == i));
         return n;
     };
     int n = look(0);
@@ -645,7 +648,7 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
             uint8_t* y = P.cache + o * P.c.outer_stride + i * P.c.inner_stride;
             auto move = [&](auto zero, uint32_t c) {
                 using T = decltype(zero);
-                for (int r = 0; r < n; r += 8) {
+                for (int r = start; r < n; r += 8) {
                     T v[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -755,7 +758,7 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
         const integral_constant<int, 1> one;
         const integral_constant<int, 2> two;
         // few bytes: every column a lane of its own
-        const bool few = src_rows->outer * src_rows->inner * longest * row <= kFewBytes / B;
+        const bool few = (double)src_rows->outer * src_rows->inner * longest * row <= (double)kFewBytes / B;
         if (K <= 4) return few ? launch(integral_constant<int, 4>(), u32x4{}, one, pages)
                                : launch(integral_constant<int, 4>(), u32x4{}, integral_constant<int, 4>(), pages);
         if (K <= 8) return few ? launch(integral_constant<int, 8>(), u32x4{}, one, pages)

@@ -997,6 +997,8 @@ def resispec_beam_select(logits, scores, *, k=None, temperature=1.0, ended=None,
     sp = _given(scores, shape, torch.float32, logits, "scores")
     ep = None
     if ended is not None:
+        if not isinstance(ended, torch.Tensor):
+            raise ValueError("ended must be a device tensor")
         ep = _given(ended, shape, torch.bool if ended.dtype is torch.bool else torch.uint8, logits, "ended")
     handle = _handle(logits, stream)
     if handle is None:
@@ -1115,12 +1117,23 @@ def _moved_to(src, layout, span, dst, name, *dims):
     return b, to
 
 
+def _none(of, rows):
+    """Whether there are no sequences, and so nothing to move."""
+    import torch
+    return isinstance(of, torch.Tensor) and of.is_cuda and of.dim() == 2 and of.shape[0] == 0 and rows.is_cuda
+
+
+def _empty(status, like):
+    import torch
+    return torch.empty(0, dtype=torch.int32, device=like.device) if status is None else status
+
+
 def _beams(parent, n, like, name):
     import torch
     if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
         raise ValueError("parent must be a [B, K] tensor")
     B, K = parent.shape
-    if B < 1 or n % B:
+    if n % B or n < B:
         raise ValueError("%s has %d beams, parent %d sequences" % (name, n, B))
     return B, n // B, K, _given(parent, parent.shape, torch.int32, like, "parent")
 
@@ -1132,6 +1145,8 @@ def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengt
     with B * K, or None for a move in place (K = W).  lengths (int32 [B], with position_dim):
     only so many positions are moved.  Returns (out, status)."""
     import torch
+    if _none(parent, state):
+        return (state if out is None else out), _empty(out_status, parent)
     src, span = _row_layout(state, beam_dim, position_dim, "state")
     B, W, K, pp = _beams(parent, src.pages, state, "state")
     if lengths is not None and position_dim is None:
@@ -1160,6 +1175,8 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
     block_table) says where the chosen beams' positions go, in `out` (default: the cache
     itself).  Returns (out, status)."""
     import torch
+    if _none(parent, cache):
+        return (cache if out is None else out), _empty(out_status, parent)
     src, span = _row_layout(cache, page_dim, position_dim, "cache")
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be a [B * W, pages] tensor")
@@ -1286,6 +1303,8 @@ def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, positio
     (int32 [B, N]).  It comes from `source`, laid out as the cache with trees for pages and nodes
     for positions, or, without one, from the node's own slot.  Returns (cache, status)."""
     import torch
+    if _none(slots, cache):
+        return cache, _empty(out_status, slots)
     rows, span = _row_layout(cache, page_dim, position_dim, "cache")
     if not isinstance(slots, torch.Tensor) or slots.dim() != 2 or not isinstance(path, torch.Tensor) or path.dim() != 2:
         raise ValueError("slots must be [B, N], path [B, depth]")

@@ -234,3 +234,49 @@ def test_graph_and_streams(gpu_lib):
         for out in outs:
             assert all(torch.equal(x, y) for x, y in zip(out, ref[i]))
         assert all(torch.equal(x, y) for x, y in zip(other, ref[(i + 1) % 4]))
+
+
+def test_scores_far_apart_and_far_from_zero(gpu_lib):
+    """Scores so large that a logit's difference is below their last bit, and beams farther apart
+    than 32 bits hold in steps of 1/16."""
+    logits = make_rows(8, 900, torch.float32, 15).view(2, 4, 900)
+    for scores in ([-1e6, -1e6, -1e6 - 1, -1e6 + 2], [-1e12, -1e12, -1e12, -2e12], [-1e30, -1e30, -3e38, 0.0],
+                   [3e38, -3e38, 0.0, 1.0]):
+        s = torch.tensor([scores, scores[::-1]], device="cuda")
+        check(gpu_lib, logits, s, 9)
+        check(gpu_lib, logits, s, 9, ended=torch.tensor([[0, 1, 1, 0]] * 2, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
+def test_many_alike(gpu_lib, dtype):
+    """More equal elements, and more chunks with the same maximum, than the lists hold, beside
+    beams whose rows have an order."""
+    V = 1 << 20
+    rows = torch.zeros((3, V), dtype=dtype, device="cuda")
+    rows[1, 700000:] = 1.0
+    rows[2] = make_rows(1, V, dtype, 2)[0]
+    check(gpu_lib, rows.view(1, 3, V), torch.tensor([[-3.0, -4.0, -14.0]], device="cuda"), 40)
+    check(gpu_lib, rows.view(1, 3, V), torch.tensor([[-3.0, -3.0, -3.0]], device="cuda"), 64)
+
+
+def test_fewer_chunks_than_chosen(gpu_lib):
+    """One beam of a vocabulary with fewer chunks than continuations are asked for."""
+    for V in (700, 5000, 33000):
+        for dtype in DTYPES:
+            check(gpu_lib, make_rows(2, V, dtype, V).view(2, 1, V), scores_for(2, 1), 64)
+
+
+def test_binding_refusals(gpu_lib):
+    l, s = torch.zeros((2, 3, 10), device="cuda"), torch.zeros((2, 3), device="cuda")
+    i = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    for kw in (dict(k=0), dict(k=31), dict(k=1 << 33), dict(temperature=0.0), dict(temperature=float("nan")),
+               dict(ended=i(2, 3)), dict(ended=[1]), dict(ended=torch.zeros((3, 2), dtype=torch.uint8, device="cuda")),
+               dict(end_token=1 << 31), dict(out_parent=i(2, 4)), dict(out_score=i(2, 3)), dict(out_status=i(3)),
+               dict(workspace=torch.empty(8, dtype=torch.uint8, device="cuda")), dict(workspace=i(4096)),
+               dict(temperature=torch.ones(3, device="cuda"))):
+        with pytest.raises((ValueError, TypeError, gpu_lib.ResiSpecError)):
+            gpu_lib.resispec_beam_select(l, s, **kw)
+    for a, b in ((l, s[:, :2].contiguous()), (l, s.view(6)), (l.half(), s), (l, s.double()), (l.transpose(1, 2), s),
+                 (l[:, :1].expand(2, 3, 10), s), (l, s.t().contiguous().t()), (l.view(6, 10)[:5], s)):
+        with pytest.raises((ValueError, TypeError)):
+            gpu_lib.resispec_beam_select(a, b)

@@ -396,3 +396,107 @@ def test_commit_faults(gpu_lib):
     out, st = gpu_lib.resispec_commit_path(state, slots, path, source=source, page_dim=1, position_dim=3)
     torch.cuda.synchronize()
     assert st.tolist() == [0, 4, 4, 4, 0, 11, 4]
+
+
+def test_no_sequences(gpu_lib):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    state = torch.zeros((2, 0, 3, 5), device="cuda")
+    out, st = gpu_lib.resispec_beam_reorder(state, torch.zeros((0, 4), **i32), beam_dim=1, position_dim=2)
+    assert out is state and st.shape == (0,)
+    cache = torch.ones((6, 4, 8), device="cuda")
+    out, st = gpu_lib.resispec_beam_reorder_paged(cache, torch.zeros((0, 3), **i32), torch.zeros((0, 4), **i32),
+                                                  torch.zeros(0, **i32))
+    assert out is cache and st.shape == (0,)
+    out, st = gpu_lib.resispec_commit_path(cache, torch.zeros((0, 5), **i32), torch.zeros((0, 2), **i32))
+    assert out is cache and st.shape == (0,)
+    path, st = gpu_lib.resispec_accepted_path(torch.zeros((0, 5), **i32), torch.zeros((0, 5), **i32), torch.zeros((0, 2), **i32),
+                                              torch.zeros(0, **i32))
+    assert path.shape == (0, 2) and st.shape == (0,)
+
+
+def test_places_past_32_bits(gpu_lib):
+    """Beams of 3 GiB, and pages that lie more than 4 GiB into a cache."""
+    n = 3 << 30
+    state = torch.empty((2, n), dtype=torch.uint8, device="cuda")
+    state[0].random_(generator=torch.Generator(device="cuda").manual_seed(1))
+    state[1].fill_(7)
+    first = state[0].clone()
+    out, st = gpu_lib.resispec_beam_reorder(state, torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(st) == 0 and bool((state[0] == 7).all()) and torch.equal(state[1], first)
+    del first, out
+    # 96 pages of 16 positions of 4 MiB: 6 GiB
+    cache = state.view(-1).view(96, 16, 1 << 22)
+    cache.random_(generator=torch.Generator(device="cuda").manual_seed(2))
+    before = {(p, t): cache[p, t].clone() for p, t in ((95, 3), (95, 9), (94, 15), (2, 0), (93, 1))}
+    slots = torch.tensor([[2 * 16, 95 * 16 + 3, 94 * 16 + 15, 95 * 16 + 9, 93 * 16 + 1]], dtype=torch.int32, device="cuda")
+    path = torch.tensor([[0, 2, 3, 4]], dtype=torch.int32, device="cuda")
+    gpu_lib.resispec_commit_path(cache, slots, path)
+    torch.cuda.synchronize()
+    for to, of in (((2, 0), (2, 0)), ((95, 3), (94, 15)), ((94, 15), (95, 9)), ((95, 9), (93, 1)), ((93, 1), (93, 1))):
+        assert torch.equal(cache[to], before[of])
+    table = torch.tensor([[95], [1]], dtype=torch.int32, device="cuda")
+    a, b = cache[95, :2].clone(), cache[1, :2].clone()
+    gpu_lib.resispec_beam_reorder_paged(cache, table, torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"),
+                                        torch.tensor([2], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert torch.equal(cache[95, :2], b) and torch.equal(cache[1, :2], a)
+
+
+def test_streams_and_places_of_outputs(gpu_lib):
+    """A stream given by the caller, and outputs that are the caller's."""
+    side = torch.cuda.Stream()
+    state = fill((4, 6, 5), torch.float32)
+    parent = torch.tensor([[1, 0], [0, 0]], dtype=torch.int32, device="cuda")
+    old = state.view(4, 6, 5).clone()
+    st = torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    out, got = gpu_lib.resispec_beam_reorder(state, parent, beam_dim=0, position_dim=1, out_status=st, stream=side)
+    side.synchronize()
+    assert got is st and (st == 0).all()
+    assert same(out, old[[1, 0, 2, 2]])         # any bits, NaNs among them
+    args = batch(20, 8, 60, 20, 3)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    want = plan(*(list(x) if not isinstance(x[0], list) else [list(y) for y in x] for x in args[:4]), list(args[4]), args[5], 8, 300)
+    t, f = torch.tensor(args[3], **i32), torch.tensor(args[4], **i32)
+    rest = [torch.tensor(x, **i32) for x in (args[0], args[1], args[2])]
+    outs = dict(out_slots=torch.empty(300, **i32), out_positions=torch.empty(300, **i32), out_requests=torch.empty(300, **i32))
+    side.wait_stream(torch.cuda.current_stream())
+    res = gpu_lib.resispec_plan_cache(*rest, t, f, torch.tensor([args[5]], **i32), page_size=8, stream=side, **outs)
+    side.synchronize()
+    assert res[0] is outs["out_slots"] and res[0].tolist() == want[0] and res[6].tolist() == want[6]
+
+
+def test_binding_refusals(gpu_lib):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    state, parent = torch.zeros((2, 6, 5), device="cuda"), torch.zeros((2, 3), **i32)
+    for kw in (dict(lengths=torch.zeros(2, **i32), beam_dim=1),                       # lengths of what
+               dict(beam_dim=0), dict(beam_dim=1, out=state[:, 1:]), dict(beam_dim=1, out=state.double()),
+               dict(beam_dim=1, out=torch.zeros((2, 5, 5), device="cuda")), dict(beam_dim=1, position_dim=0),
+               dict(beam_dim=1, out=torch.zeros((2, 6, 6), device="cuda")), dict(beam_dim=1, out_status=torch.zeros(3, **i32))):
+        with pytest.raises((ValueError, TypeError, gpu_lib.ResiSpecError)):
+            gpu_lib.resispec_beam_reorder(state, parent, **kw)
+    with pytest.raises(ValueError):
+        gpu_lib.resispec_beam_reorder(state, torch.zeros((2, 4), **i32), beam_dim=1)       # in place, more than there are
+    big = torch.zeros((2, 12, 5), device="cuda")
+    with pytest.raises(ValueError):
+        gpu_lib.resispec_beam_reorder(big[:, :6], parent, beam_dim=1, out=big[:, 3:9])     # partly the same rows
+    cache, table = torch.zeros((9, 4, 5), device="cuda"), torch.zeros((6, 2), **i32)
+    lengths = torch.zeros(2, **i32)
+    for kw in (dict(out_table=torch.zeros((6, 3), **i32)), dict(out_table=torch.zeros((5, 2), **i32)), dict(out=cache[1:])):
+        with pytest.raises((ValueError, gpu_lib.ResiSpecError)):
+            gpu_lib.resispec_beam_reorder_paged(cache, table, parent, lengths, **kw)
+    slots, path = torch.zeros((2, 4), **i32), torch.zeros((2, 3), **i32)
+    for kw in (dict(source=torch.zeros((2, 5, 5), device="cuda")), dict(source=torch.zeros((2, 4, 6), device="cuda")),
+               dict(source=torch.zeros((2, 4, 5), device="cuda", dtype=torch.float64)), dict(source=cache[:2])):
+        with pytest.raises((ValueError, TypeError, gpu_lib.ResiSpecError)):
+            gpu_lib.resispec_commit_path(cache, slots, path, **kw)
+    ones = [torch.zeros(3, **i32) for _ in range(3)]
+    with pytest.raises(ValueError):
+        gpu_lib.resispec_plan_cache(*ones, torch.zeros((3, 2), **i32), torch.zeros(4, **i32), torch.zeros(1, **i32), page_size=4)
+    with pytest.raises(ValueError):
+        gpu_lib.resispec_plan_cache(*ones, torch.zeros((2, 3), **i32).t(), torch.zeros(4, **i32), torch.zeros(1, **i32),
+                                    page_size=4, max_slots=4)
+    with pytest.raises(gpu_lib.ResiSpecError):
+        gpu_lib.resispec_plan_cache(*ones, torch.zeros((3, 2), **i32), torch.zeros(4, **i32), torch.zeros(1, **i32), page_size=0,
+                                    max_slots=4)
