@@ -1,7 +1,7 @@
 // beam.hip -- beam search's choice of the next beams from rows of logits on gfx950
 // (resispec_beam_select).  Declared in resispec.h.
 
-#include "common.h"
+#include "mass64.h"
 
 #include <climits>
 
@@ -15,8 +15,8 @@ namespace {
 // chunks are k elements, so whatever is chosen is not below the last of them, and only chunks
 // that reach so far, about k of a sequence's hundreds, are read again.
 //
-// Sums are of 32-bit masses: a 64-bit exponential takes twice the vector ALU's time.  A sum is
-// off by 1.3e-6 of itself at most: an exponent x by 3 * 2^-24 of itself (difference, scale and
+// Sums are of 32-bit masses (1024 rows of 151,936 bf16 48 us, at 6.5 TB/s; with exponentials in
+// fp64 122).  A sum is off by 1.3e-6 of itself at most: an exponent x by 3 * 2^-24 of itself (difference, scale and
 // product are rounded), so a mass by 0.693 of that and 2^-23, the mean of |x| by mass over a
 // unit of 4096 elements whose maximum is at 0 is 8.1 at most, and three additions are in 32
 // bits.  That is enough for a score, and for an order too unless two beams' scores are closer
@@ -99,10 +99,11 @@ struct Chunk {
             for (int e = 0; e < VEC; ++e) v[u * VEC + e] = x[e];
         }
     }
-    // the place of value i of this lane in the row
-    static __device__ __forceinline__ int at(int c, int i) {
-        return c * kChunk + (i / VEC) * 64 * VEC + (threadIdx.x & 63) * VEC + i % VEC;
+    // the place of a lane's value i in the row
+    static __device__ __forceinline__ int place(int c, int lane, int i) {
+        return c * kChunk + (i / VEC) * 64 * VEC + lane * VEC + i % VEC;
     }
+    static __device__ __forceinline__ int at(int c, int i) { return place(c, threadIdx.x & 63, i); }
 };
 
 // The maxima over the wave of four values a lane: lanes q, q + 4, q + 8 .. get that of value q.
@@ -193,7 +194,7 @@ __device__ __forceinline__ Place wave_first(Place a) {
 constexpr int kBins = 512;               // of scores of chunks, from the best downwards
 constexpr double kBinsPerUnit = 16.0;
 constexpr int kChunkList = 512, kList = 1024;
-constexpr int kHeld = 2;                 // maxima of chunks a thread holds
+constexpr int kHeld = 5;                 // maxima of chunks a thread holds
 // what is listed besides: the errors of two sums and of their logarithms in 32 bits (2e-6 each),
 // and the rounding of a distance in bins (8e-6 where bins are told apart)
 constexpr double kSlack = 2.0 * kNear + 2.0e-5;
@@ -209,11 +210,7 @@ struct MergeSmem {
     double part[kMergeWaves];
     int32_t bin[kBins];
     union {
-        struct {
-            double score[kList];
-            float l[kList];
-            int32_t w[kList], j[kList];
-        };
+        Place list[kList];
         struct {
             Place place[2][kMergeWaves];
             Place chosen[RS_MAX_CANDIDATES];
@@ -240,6 +237,7 @@ __device__ __forceinline__ int wave_incl_scan_i(int v) {
 template <typename In, int VEC>
 struct Merge {
     using C = Chunk<In, VEC>;
+    using E = std::conditional_t<sizeof(In) == 2, uint16_t, float>;
     const BeamParams& P;
     MergeSmem& sm;
     const int64_t b, r0;
@@ -252,11 +250,10 @@ struct Merge {
     __device__ __forceinline__ float chunk_max(int w, int c) const {
         return P.maxima[(r0 + w) * (int64_t)nch + c];
     }
-    __device__ __forceinline__ double score(int w, float l, double log_sum) const {
+    __device__ __forceinline__ double score(int w, float l) const {
         if (sm.kind[w] == 2) return (double)sm.s[w];
-        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - log_sum) + (double)sm.s[w];
+        return (((double)l - (double)sm.max[w]) / (double)sm.T[w] - sm.log_sum[w]) + (double)sm.s[w];
     }
-    __device__ __forceinline__ double score(int w, float l) const { return score(w, l, sm.log_sum[w]); }
 
     // Every beam's kind, maximum and sum, a wave a beam.
     __device__ __forceinline__ void sums() {
@@ -342,61 +339,45 @@ struct Merge {
         return at * kLaneBins + __builtin_amdgcn_readlane(kth, at);
     }
 
-    // body(w, l, j, score) for what the listed chunks hold within `far` of the reference.
+    // body(w, l, j) for what the listed chunks hold within `far` of the reference.
     template <typename Body>
     __device__ __forceinline__ void each_listed(double reference, double far, Body&& body) {
         const int n = sm.nchunks;
-        // two chunks a wave on their way at a time
-        for (int i0 = wave; i0 < n; i0 += 2 * kMergeWaves) {
-            C chunk[2];
-            int w[2], c[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = i0 + h * kMergeWaves;
-                const int id = __builtin_amdgcn_readfirstlane(sm.chunks[i < n ? i : i0]);
-                w[h] = id / nch;
-                c[h] = id - w[h] * nch;
-                if (i < n && sm.kind[w[h]] == 1) chunk[h].template load<false>(row(w[h]), c[h], P.V);
+        for (int i = wave; i < n; i += kMergeWaves) {
+            const int id = __builtin_amdgcn_readfirstlane(sm.chunks[i]), w = id / nch, c = id - w * nch;
+            if (sm.kind[w] == 2) {
+                if (lane == 0) body(w, 0.0f, P.end_token);
+                continue;
             }
+            C chunk;
+            chunk.template load<false>(row(w), c, P.V);
+            // the row's least logit within reach, or one below it
+            const double least = (reference - far - (double)sm.s[w] + sm.log_sum[w]) * (double)sm.T[w] + (double)sm.max[w];
+            const float cut = fmaxf((float)(least - fabs(least) * 0x1p-23), -FLT_MAX);
+            chunk.settle(c, P.V);
+            float v[C::N];
+            chunk.unpack(v);
+            float top = v[0];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (i0 + h * kMergeWaves >= n) break;
-                if (sm.kind[w[h]] == 2) {
-                    if (lane == 0) body(w[h], 0.0f, P.end_token, (double)sm.s[w[h]]);
-                    continue;
-                }
-                const double log_sum = sm.log_sum[w[h]];
-                // the row's least logit within reach, or one below it
-                const double least = (reference - far - (double)sm.s[w[h]] + log_sum) * (double)sm.T[w[h]] + (double)sm.max[w[h]];
-                const float cut = fmaxf((float)(least - fabs(least) * 0x1p-23), -FLT_MAX);
-                chunk[h].settle(c[h], P.V);
-                float v[C::N];
-                chunk[h].unpack(v);
-                // few lanes have any: one after another, in little code
-                uint32_t hits = 0;
-#pragma unroll
-                for (int e = 0; e < C::N; ++e) hits |= (uint32_t)(v[e] >= cut) << e;
-                while (hits) {
-                    const int at = __builtin_ctz(hits);
-                    hits &= hits - 1;
-                    float l = v[0];
-#pragma unroll
-                    for (int e = 1; e < C::N; ++e) l = at == e ? v[e] : l;
-                    body(w[h], l, C::at(c[h], at), score(w[h], l, log_sum));
+            for (int e = 1; e < C::N; ++e) top = fmaxf(top, v[e]);
+            // few lanes have any: the wave takes one lane's elements after another's, from memory
+            // again (in registers each is a place of its own, and much code: the choice of 64 of
+            // 32 beams 15.2 us where this takes 13.6)
+            for (uint64_t hits = __ballot(top >= cut); hits; hits &= hits - 1) {
+                const int j = C::place(c, __builtin_ctzll(hits), lane);
+                if (lane < C::N && j < P.V) {
+                    float l[1];
+                    load_vec<E, 1>(reinterpret_cast<const E*>(row(w)), j, P.V, l);
+                    if (l[0] >= cut) body(w, l[0], j);
                 }
             }
         }
         __syncthreads();
     }
     __device__ __forceinline__ void list_listed(double reference, double far) {
-        each_listed(reference, far, [&](int w, float l, int j, double s) {
+        each_listed(reference, far, [&](int w, float l, int j) {
             const int at = atomicAdd(&sm.nlist, 1);
-            if (at < kList) {
-                sm.score[at] = s;
-                sm.l[at] = l;
-                sm.w[at] = w;
-                sm.j[at] = j;
-            }
+            if (at < kList) sm.list[at] = {0.0, w, l, j};
         });
     }
 
@@ -457,9 +438,10 @@ struct Merge {
         for (int i = tid; i < kBins; i += kMergeBlock) sm.bin[i] = 0;
         if (tid == 0) sm.nlist = 0;
         __syncthreads();
-        each_listed(reference, far, [&](int, float, int, double s) {
-            count((float)fmin((reference - s) * bins_per_unit, (double)FLT_MAX));
+        each_listed(reference, far, [&](int w, float l, int) {
+            count((float)fmin((reference - score(w, l)) * bins_per_unit, (double)FLT_MAX));
         });
+        __syncthreads();
         bin = bin_of_kth();
         list_listed(reference, bin < kBins - 1 ? (bin + 1) / bins_per_unit + slack : far);
         return sm.nlist <= kList;
@@ -475,12 +457,14 @@ struct Merge {
     // one.  Beams are marked whose scores are too close to call.
     __device__ __forceinline__ void rank() {
         const int n = sm.nlist, sub = lane & 15;
+        for (int i = tid; i < n; i += kMergeBlock) sm.list[i].score = score(sm.list[i].w, sm.list[i].l);
+        __syncthreads();
         for (int i = tid >> 4; i < n; i += kMergeBlock / 16) {
-            const Place mine = {sm.score[i], sm.w[i], sm.l[i], sm.j[i]};
+            const Place mine = sm.list[i];
             int ahead = 0;
             uint64_t close = 0;
             for (int x = sub; x < n; x += 16) {
-                const Place other = {sm.score[x], sm.w[x], sm.l[x], sm.j[x]};
+                const Place other = sm.list[x];
                 ahead += before(other, mine);
                 if (other.w != mine.w && fabs(other.score - mine.score) <= kNear + fabs(mine.score) * kNearOf)
                     close |= 1ull << other.w;
@@ -611,8 +595,6 @@ struct Merge {
                 if (doubt) {
                     for (int w = 0; w < P.W; ++w)
                         if ((doubt >> w & 1) && sm.kind[w] == 1) sum_again(w);
-                    __syncthreads();
-                    for (int i = tid; i < sm.nlist; i += kMergeBlock) sm.score[i] = score(sm.w[i], sm.l[i]);
                     __syncthreads();
                     rank();
                 }

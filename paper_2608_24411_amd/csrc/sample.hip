@@ -3,7 +3,7 @@
 // (resispec_filter_logits), and log-probabilities and ranks of given tokens
 // (resispec_token_logprobs).  Declared in resispec.h.
 
-#include "common.h"
+#include "mass64.h"
 
 #include <climits>
 
