@@ -73,10 +73,12 @@ struct ReorderParams {
 
 constexpr int kReorderBlock = 256, kReorderWaves = kReorderBlock / 64;
 
-// U: columns a lane and beam in a piece.
-template <int KMAX, typename T, int U, bool PAGED>
+// A piece is a column a lane.  (With two or four 1 x 4 states of 32 KB 5.8 us instead of 3.8, 32 x
+// 4 of 2 MB 114 and 88, the largest alike.)  40 states of 492 KB: 25 us, 5.3 TB/s; 256 of 2.1 MB in
+// pages of 16 rows: 186 us, 4.8 TB/s, a copy's rate: HBM bounds it.
+template <int KMAX, typename T, bool PAGED>
 __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const ReorderParams P) {
-    constexpr int64_t kPiece = 64 * U * sizeof(T);
+    constexpr int64_t kPiece = 64 * sizeof(T);
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
     const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
     const int32_t* parent = P.parent + (int64_t)b * P.K;
@@ -149,12 +151,8 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
                 if (on >> k & 1) store_at<E>(reinterpret_cast<uint8_t*>(readlane_i64(to, k)) + c, v[k]);
         };
         // columns, and bytes at a run's end
-        const uint32_t whole = (uint32_t)bytes / sizeof(T) * sizeof(T);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t c = (u * 64 + lane) * sizeof(T);
-            if (c < whole) move(T{}, c);
-        }
+        const uint32_t whole = (uint32_t)bytes / sizeof(T) * sizeof(T), c = lane * sizeof(T);
+        if (c < whole) move(T{}, c);
         if (whole + lane < bytes) move(uint8_t{}, whole + lane);
     }
 }
@@ -173,6 +171,7 @@ struct PlanParams {
     int32_t *out_held, *out_free_count, *out_starts;
     int32_t T;
     int32_t *slots, *positions, *requests, *status;
+    int32_t later;                   // out_held and out_free_count are left to rs_plan_tell_kernel
 };
 
 // The sum over a workgroup's threads up to each, in order, and the whole sum.  Whole numbers in
@@ -280,10 +279,7 @@ struct Plan {
             q.need = 0;
         }
     }
-    __device__ __forceinline__ void put(int r, const Request& q) const {
-        P.out_held[r] = q.status == RS_SEQ_OK ? q.want : q.held;
-        P.out_starts[r] = (int32_t)min(q.first, (int64_t)INT_MAX);
-    }
+    static __device__ __forceinline__ int holds(const Request& q) { return q.status == RS_SEQ_OK ? q.want : q.held; }
 };
 
 // A step of up to BLOCK requests in one launch.  Every workgroup works out the running sums for
@@ -384,16 +380,39 @@ __global__ void __launch_bounds__(BLOCK) rs_plan_step_kernel(const PlanParams P)
         __syncthreads();
         if (mine) P.status[tid] = granted && wrong[tid] ? RS_SEQ_BAD_PAGE : q.status;
     }
-    if (mine) plan.put(tid, q);
+    if (mine) P.out_starts[tid] = (int32_t)min(q.first, (int64_t)INT_MAX);
+    if (mine && !P.later) P.out_held[tid] = plan.holds(q);
     if (teller == 0 && tid == 0) {
         P.out_starts[P.R] = (int32_t)min(rows, (int64_t)INT_MAX);
-        P.out_free_count[0] = avail - A;
+        if (!P.later) P.out_free_count[0] = avail - A;
     }
 }
 
-// Any number of requests, and outputs that are inputs: one workgroup, 1024 requests at a time,
-// in two passes (the first gives pages back, the second takes them), and the new rows in a
-// launch of their own.
+// What the requests hold then, and how many pages are free, where these are inputs of the step:
+// they may change only when every workgroup has read them.
+template <int BLOCK>
+__global__ void __launch_bounds__(BLOCK) rs_plan_tell_kernel(const PlanParams P) {
+    __shared__ double part[3][BLOCK / 64];
+    __shared__ int32_t released, taken;
+    const int tid = threadIdx.x, count = P.free_count[0];
+    if (tid == 0) released = taken = 0;
+    __syncthreads();
+    Plan<BLOCK> plan{P, part, count};
+    Request q;
+    plan.look(tid, q);
+    if (q.give) atomicAdd(&released, q.give);
+    __syncthreads();
+    const int avail = count + released;
+    plan.take(q, avail);
+    if (q.need) atomicAdd(&taken, q.need);
+    __syncthreads();
+    if (tid < P.R) P.out_held[tid] = plan.holds(q);
+    if (tid == 0) P.out_free_count[0] = avail - taken;
+}
+
+// More than 1024 requests: one workgroup, 1024 at a time, in two passes (the first gives pages
+// back, the second takes them), and the new rows in a launch of their own.  3000 requests of 33
+// rows: 35 and 7 us.
 constexpr int kPlanBlock = 1024;
 __global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P) {
     __shared__ double part[3][kPlanBlock / 64];
@@ -445,7 +464,8 @@ __global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P)
             P.table[r * P.table_stride + e] = P.free_pages[avail - 1 - (base + x)];
         });
         if (r < P.R) {
-            plan.put(r, q);
+            P.out_held[r] = plan.holds(q);
+            P.out_starts[r] = (int32_t)min(q.first, (int64_t)INT_MAX);
             if (P.status) P.status[r] = q.status;
         }
         __syncthreads();
@@ -487,7 +507,8 @@ __global__ void __launch_bounds__(256) rs_plan_rows_kernel(const PlanParams P) {
 // ------------------------------------------------------------------- path ----
 
 // Trees of up to 64 nodes, a wave a sequence: lane n has node n, and the nodes of a level that
-// carry the tokens are bits of a mask.
+// carry the tokens are bits of a mask.  All loads are on their way at once, so a call is a launch
+// and one latency: 1 tree of 26 nodes 1.8 us, 1024 of 60 nodes 4.7 (6.2 by the kernel below).
 constexpr int kPathWaves = 4;
 __global__ void __launch_bounds__(kPathWaves * 64) rs_path_wave_kernel(
     const int32_t* __restrict__ parent, const int32_t* __restrict__ node_token, const int32_t* __restrict__ tokens,
@@ -587,7 +608,8 @@ constexpr int kCommitBlock = 256, kCommitWaves = kCommitBlock / 64;
 // A lane owns a column of 16 bytes (or one) of all rows of a path, as in the reorder.  Paths
 // ascend, so path[j] >= j: the slot that row i goes to, slots[i], is the source of none after
 // it, and the rows are moved in order, eight loaded before they are stored.  Lane i has row i's
-// places, 64 at a time; no wave waits for another.
+// places, 64 at a time; no wave waits for another.  1024 paths of four rows of 16 x 1000 bytes:
+// 26 us, 131 MB, 5.0 TB/s, a copy's rate: HBM bounds it.
 __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitParams P) {
     const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
@@ -699,8 +721,6 @@ int32_t groups_for(int64_t pieces, int32_t B, int waves) {
     return (int32_t)(most < share ? most : share);
 }
 
-constexpr int64_t kFewBytes = 4 << 20;    // of one beam of every sequence
-
 rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_table, int64_t src_table_stride,
                   void* dst, const rs_rows* dst_rows, const int32_t* dst_table, int64_t dst_table_stride,
                   int32_t max_pages, const int32_t* parent, const int32_t* lengths, int32_t B, int32_t W, int32_t K,
@@ -741,31 +761,26 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
     // positions that lie one after another in both are one run
     const int64_t row = src_rows->row_bytes, S = src_rows->positions;
     P.together = src_rows->position_stride == row && dst_rows->position_stride == row;
-    auto launch = [&](auto kmax, auto zero, auto u, auto pages) -> rs_status {
-        constexpr int64_t piece = 64 * u() * sizeof(zero);
+    auto launch = [&](auto kmax, auto zero, auto pages) -> rs_status {
+        constexpr int64_t piece = 64 * sizeof(zero);
         const int64_t run = P.together ? S * row : row, runs = (P.together ? 1 : S) * (paged ? max_pages : 1);
         const int64_t each = (run + piece - 1) / piece;
         if (each > INT_MAX || runs > INT_MAX || !counts_fit(*src_rows, each * runs)) return RS_ERR_UNSUPPORTED;
         P.pieces = (int32_t)each;
         P.G = groups_for(src_rows->outer * src_rows->inner * each * runs, B, kReorderWaves);
         if ((int64_t)P.G * B > INT_MAX / kReorderBlock) return RS_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((rs_reorder_kernel<kmax(), decltype(zero), u(), pages()>), dim3((unsigned)P.G * B),
+        hipLaunchKernelGGL((rs_reorder_kernel<kmax(), decltype(zero), pages()>), dim3((unsigned)P.G * B),
                            dim3(kReorderBlock), 0, (hipStream_t)stream, P);
         return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
     };
     auto by_beams = [&](auto pages) {
+        // columns of 8 bytes where the new values of so many beams would not fit the registers
         using std::integral_constant;
-        const integral_constant<int, 1> one;
-        const integral_constant<int, 2> two;
-        // few bytes: every column a lane of its own
-        const bool few = (double)src_rows->outer * src_rows->inner * longest * row <= (double)kFewBytes / B;
-        if (K <= 4) return few ? launch(integral_constant<int, 4>(), u32x4{}, one, pages)
-                               : launch(integral_constant<int, 4>(), u32x4{}, integral_constant<int, 4>(), pages);
-        if (K <= 8) return few ? launch(integral_constant<int, 8>(), u32x4{}, one, pages)
-                               : launch(integral_constant<int, 8>(), u32x4{}, two, pages);
-        if (K <= 16) return launch(integral_constant<int, 16>(), u32x4{}, one, pages);
-        if (K <= 32) return launch(integral_constant<int, 32>(), u32x2{}, one, pages);
-        return launch(integral_constant<int, 64>(), u32x2{}, one, pages);
+        if (K <= 4) return launch(integral_constant<int, 4>(), u32x4{}, pages);
+        if (K <= 8) return launch(integral_constant<int, 8>(), u32x4{}, pages);
+        if (K <= 16) return launch(integral_constant<int, 16>(), u32x4{}, pages);
+        if (K <= 32) return launch(integral_constant<int, 32>(), u32x2{}, pages);
+        return launch(integral_constant<int, 64>(), u32x2{}, pages);
     };
     return paged ? by_beams(std::true_type()) : by_beams(std::false_type());
 }
@@ -801,17 +816,31 @@ rs_status resispec_plan_cache(const int32_t* kept, const int32_t* added, const i
     if (R > 0 && (!kept || !added || !held || !block_table || !out_held)) return RS_ERR_INVALID_ARG;
     if ((int64_t)num_pages * page_size > INT_MAX || (int64_t)max_pages * page_size > INT_MAX) return RS_ERR_UNSUPPORTED;
     PlanParams P{kept, added, held, R, page_size, block_table, table_stride, max_pages, free_pages, free_count, num_pages,
-                 out_held, out_free_count, out_starts, T, out_slots, out_positions, out_requests, out_status};
+                 out_held, out_free_count, out_starts, T, out_slots, out_positions, out_requests, out_status, 0};
+    // One workgroup for the smallest steps (1 request of 26 rows 3.6 us), and for small ones whose
+    // outputs are inputs, which need a second launch otherwise.  Jobs side by side are quicker
+    // elsewhere: 64 requests of 4 rows 7.7 us in one, 200 of 2 rows 10.2 and 5.9, 16 of 33 rows
+    // 7.3 and 5.5, 256 of 33 rows 6.4, 1024 of 2 rows 16.7 and 9.6, 1024 with prompts and 93,000
+    // rows 11.4, of which each is a chain of latencies: numbers, sums, a search, a page, a row.
+    const bool in_place = out_held == held || out_free_count == free_count;
     auto step = [&](auto block, unsigned groups) {
+        P.later = groups > 1 && in_place;
         hipLaunchKernelGGL(rs_plan_step_kernel<block()>, dim3(groups), dim3(block()), 0, (hipStream_t)stream, P);
-        return hipGetLastError() == hipSuccess ? RS_OK : RS_ERR_HIP;
+        if (hipGetLastError() != hipSuccess) return RS_ERR_HIP;
+        if constexpr (block() > 64) {
+            if (!P.later) return RS_OK;
+            hipLaunchKernelGGL(rs_plan_tell_kernel<block()>, dim3(1), dim3(block()), 0, (hipStream_t)stream, P);
+            if (hipGetLastError() != hipSuccess) return RS_ERR_HIP;
+        }
+        return RS_OK;
     };
     using std::integral_constant;
-    if (R <= 64 && T <= 256) return step(integral_constant<int, 64>(), 1);
-    if (R <= 256 && T <= 1024) return step(integral_constant<int, 256>(), 1);
-    const unsigned groups = T <= 2048 ? 1 : std::min(((unsigned)T + 1023) / 1024, 224u) + kTakers + kGivers + kTellers;
-    if (R <= 1024 && (groups == 1 || (out_held != held && out_free_count != free_count)))
-        return step(integral_constant<int, 1024>(), groups);
+    constexpr unsigned kPageGroups = kTakers + kGivers + kTellers;
+    if (R <= 64 && T <= 64) return step(integral_constant<int, 64>(), 1);
+    if (R <= 256 && T <= 512 && in_place) return step(integral_constant<int, 256>(), 1);
+    if (R <= 256) return step(integral_constant<int, 256>(), std::min(((unsigned)T + 255) / 256, 1024u) + kPageGroups);
+    if (R <= 1024)
+        return step(integral_constant<int, 1024>(), std::max(1u, std::min(((unsigned)T + 1023) / 1024, 256u)) + kPageGroups);
     hipLaunchKernelGGL(rs_plan_kernel, dim3(1), dim3(kPlanBlock), 0, (hipStream_t)stream, P);
     if (hipGetLastError() != hipSuccess) return RS_ERR_HIP;
     if (T == 0) return RS_OK;
