@@ -14,6 +14,8 @@
  *   and the inverse-CDF draw from the final residual when every candidate is
  *   rejected; then a walk from each root that follows accepted children and
  *   returns the accepted tokens (Preliminary, tree-structured verification).
+ * Around it: the draft step, sampling from rows of logits, beam search's step, and the pages,
+ * slots and rows of a paged cache under a draft tree.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller unless stated
@@ -605,7 +607,7 @@ typedef struct {
  *                 workspace race.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, V, W or k <= 0, k > W * V, row_stride < V, or a
  * number in `filter` out of its range; RS_ERR_UNSUPPORTED for V > RS_MAX_VOCAB, W or k >
- * RS_MAX_CANDIDATES or B * W >= 2^23; RS_ERR_WORKSPACE.  B = 0 is a no-op.  A sequence's
+ * RS_MAX_CANDIDATES, B * W >= 2^23 or B >= 2^22; RS_ERR_WORKSPACE.  B = 0 is a no-op.  A sequence's
  * outputs depend on its rows, scores and ends alone, not on the batch.
  */
 rs_status resispec_beam_select(const void* logits, int64_t row_stride, const float* scores,
@@ -629,8 +631,8 @@ size_t resispec_beam_workspace_bytes(int32_t B, int32_t W, int32_t V);
  *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_BAD_PARAM: a parent or a length
  *                 out of its range; nothing of that sequence is moved.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, W or K <= 0, or layouts that do not fit;
- * RS_ERR_UNSUPPORTED for W or K > RS_MAX_CANDIDATES, or states of 2^31 rows a sequence's beam or
- * more.  B = 0 is a no-op.
+ * RS_ERR_UNSUPPORTED for W or K > RS_MAX_CANDIDATES, B >= 2^23, or a beam's state of 2^31 rows, or
+ * pieces of 512 bytes, or more.  B = 0 is a no-op.
  */
 rs_status resispec_beam_reorder(const void* src, const rs_rows* src_rows, void* dst,
                                 const rs_rows* dst_rows, const int32_t* parent,
@@ -710,7 +712,7 @@ rs_status resispec_plan_cache(const int32_t* kept, const int32_t* added, const i
  *                 array, or no way carries the tokens; RS_SEQ_DEPTH_EXCEEDED: accepted_len
  *                 outside [-1, max_depth].  Such a sequence has no path.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, N <= 0 or max_depth < 0; RS_ERR_UNSUPPORTED for
- * N > RS_MAX_PATH_NODES.  B = 0 is a no-op.
+ * N > RS_MAX_PATH_NODES or B >= 2^22.  B = 0 is a no-op.
  */
 #define RS_MAX_PATH_NODES 8192
 rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_token,
@@ -733,8 +735,8 @@ rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_toke
  *                 ascend or has a node outside [0, N); RS_SEQ_BAD_PAGE: a slot of it outside
  *                 the cache.  Nothing of that sequence is moved.
  * RS_ERR_INVALID_ARG for a NULL pointer, B < 0, N or depth <= 0, or layouts that do not fit;
- * RS_ERR_UNSUPPORTED for N or depth > RS_MAX_PATH_NODES, pages * positions >= 2^31 or rows of
- * 2^31 bytes or more.  B = 0 is a no-op.
+ * RS_ERR_UNSUPPORTED for N or depth > RS_MAX_PATH_NODES, B >= 2^23, pages * positions or outer *
+ * inner >= 2^31, or rows of 2^31 bytes or more.  B = 0 is a no-op.
  */
 rs_status resispec_commit_path(void* cache, const rs_rows* cache_rows, const int32_t* slots,
                                const int32_t* path, const void* source,

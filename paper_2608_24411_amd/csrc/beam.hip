@@ -624,7 +624,8 @@ __global__ void __launch_bounds__(kMergeBlock) rs_beam_merge_kernel(const BeamPa
 
 int32_t units_of(int32_t V) { return (V + kUnit - 1) / kUnit; }
 
-constexpr int32_t kMostRows = (1 << 23) - 1;
+// less than 2^32 threads a launch: of the rows' pass, and of the merge
+constexpr int32_t kMostRows = (1 << 23) - 1, kMostSequences = (1 << 22) - 1;
 
 }  // namespace
 
@@ -632,7 +633,7 @@ extern "C" {
 
 size_t resispec_beam_workspace_bytes(int32_t B, int32_t W, int32_t V) {
     if (B <= 0 || W <= 0 || V <= 0 || W > RS_MAX_CANDIDATES || V > RS_MAX_VOCAB) return 0;
-    if ((int64_t)B * W > kMostRows) return 0;
+    if ((int64_t)B * W > kMostRows || B > kMostSequences) return 0;
     return (size_t)B * W * units_of(V) * (sizeof(UnitSum) + kUnitChunks * sizeof(float));
 }
 
@@ -648,7 +649,8 @@ rs_status resispec_beam_select(const void* logits, int64_t row_stride, const flo
         filter->min_p != 0.0f)
         return RS_ERR_INVALID_ARG;
     if (B < 0 || W <= 0 || V <= 0 || k <= 0 || (int64_t)W * V < k || row_stride < V) return RS_ERR_INVALID_ARG;
-    if (V > RS_MAX_VOCAB || W > RS_MAX_CANDIDATES || k > RS_MAX_CANDIDATES || (int64_t)B * W > kMostRows)
+    if (V > RS_MAX_VOCAB || W > RS_MAX_CANDIDATES || k > RS_MAX_CANDIDATES || (int64_t)B * W > kMostRows ||
+        B > kMostSequences)
         return RS_ERR_UNSUPPORTED;
     if (B == 0) return RS_OK;
     if (!logits || !scores || !out_parent || !out_token || !out_score) return RS_ERR_INVALID_ARG;

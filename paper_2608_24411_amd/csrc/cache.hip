@@ -740,7 +740,7 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
         if (src_rows->pages != (int64_t)B * W || dst_rows->pages != (int64_t)B * K) return RS_ERR_INVALID_ARG;
     }
     if (src == dst && (W != K || !same_layout(*src_rows, *dst_rows))) return RS_ERR_INVALID_ARG;
-    if (src_rows->positions > INT_MAX) return RS_ERR_UNSUPPORTED;
+    if (src_rows->positions > INT_MAX || src_rows->row_bytes > LLONG_MAX / src_rows->positions) return RS_ERR_UNSUPPORTED;
     const int64_t longest = src_rows->positions * (paged ? max_pages : 1);
     if ((paged && src_rows->positions > INT_MAX / max_pages) || !counts_fit(*src_rows, longest)) return RS_ERR_UNSUPPORTED;
     ReorderParams P{};
@@ -853,7 +853,7 @@ rs_status resispec_accepted_path(const int32_t* parent, const int32_t* node_toke
                                  const int32_t* accepted_len, int32_t B, int32_t N, int32_t max_depth,
                                  int32_t* out_path, int32_t* out_status, void* stream) {
     if (B < 0 || N <= 0 || max_depth < 0 || max_depth == INT_MAX) return RS_ERR_INVALID_ARG;
-    if (N > RS_MAX_PATH_NODES) return RS_ERR_UNSUPPORTED;
+    if (N > RS_MAX_PATH_NODES || B >= 1 << 22) return RS_ERR_UNSUPPORTED;     // less than 2^32 threads
     if (B == 0) return RS_OK;
     if (!parent || !node_token || !tokens || !accepted_len || !out_path) return RS_ERR_INVALID_ARG;
     if (N <= 64) {

@@ -38,7 +38,7 @@ def test_beam_select_refusals():
     for kw in (dict(B=-1), dict(W=0), dict(V=0), dict(k=0), dict(stride=99), dict(W=2, V=3, stride=3, k=7), dict(logits=None),
                dict(scores=None), dict(parent=None), dict(token=None), dict(score=None)):
         assert beam(**kw) == INVALID, kw
-    for kw in (dict(W=65), dict(k=65), dict(V=(1 << 22) + 1, stride=1 << 23), dict(B=1 << 21, W=4)):
+    for kw in (dict(W=65), dict(k=65), dict(V=(1 << 22) + 1, stride=1 << 23), dict(B=1 << 21, W=4), dict(B=1 << 22, W=1)):
         assert beam(**kw) == UNSUPPORTED, kw
     need = native.resispec_beam_workspace_bytes(2, 4, 100)
     assert need > 0
@@ -85,6 +85,9 @@ def test_reorder_refusals(call):
     big = dict(outer=1 << 16, inner=1 << 16)
     assert call(s=rows(**big), d=rows(**big)) == UNSUPPORTED
     assert call(s=rows(positions=1 << 40), d=rows(positions=1 << 40)) == UNSUPPORTED
+    assert call(s=rows(row_bytes=1 << 62), d=rows(row_bytes=1 << 62)) == UNSUPPORTED
+    wide = rows(pages=1 << 26)
+    assert call(s=wide, d=wide, B=1 << 24) == UNSUPPORTED
     assert call(B=0, src=None) == native.RS_OK
 
 
@@ -126,7 +129,7 @@ def test_path_and_commit_refusals():
     for kw in (dict(B=-1), dict(N=0), dict(D=-1), dict(D=(1 << 31) - 1), dict(parent=None), dict(token=None),
                dict(tokens=None), dict(length=None), dict(out=None)):
         assert path_call(**kw) == INVALID, kw
-    assert path_call(N=native.RS_MAX_PATH_NODES + 1) == UNSUPPORTED
+    assert path_call(N=native.RS_MAX_PATH_NODES + 1) == UNSUPPORTED and path_call(B=1 << 22) == UNSUPPORTED
     assert path_call(B=0, parent=None) == native.RS_OK
     for kw in (dict(B=-1), dict(N=0), dict(depth=0), dict(cache=None), dict(slots=None), dict(path=None),
                dict(c=rows(row_bytes=0)), dict(source=FAKE), dict(source=FAKE, s=rows(pages=7)),
@@ -134,7 +137,8 @@ def test_path_and_commit_refusals():
                dict(source=FAKE, s=rows(outer=1)), dict(source=FAKE, s=rows(inner=1))):
         assert commit_call(**kw) == INVALID, kw
     for kw in (dict(N=native.RS_MAX_PATH_NODES + 1), dict(depth=native.RS_MAX_PATH_NODES + 1),
-               dict(c=rows(pages=1 << 30)), dict(c=rows(outer=1 << 20, inner=1 << 20))):
+               dict(c=rows(pages=1 << 30)), dict(c=rows(outer=1 << 20, inner=1 << 20)), dict(c=rows(row_bytes=1 << 31)),
+               dict(B=1 << 24, c=rows(pages=8))):
         assert commit_call(**kw) == UNSUPPORTED, kw
     assert commit_call(B=0, cache=None) == native.RS_OK
 
