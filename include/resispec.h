@@ -646,7 +646,8 @@ rs_status resispec_beam_reorder(const void* src, const rs_rows* src_rows, void* 
  *                 and `dst_table_stride` entries from row to row, `max_pages` entries each
  *   dst         : may be `src` with the same layout.  A row of dst may then also be one of src,
  *                 if it is so at the same position of the same sequence (one table given twice;
- *                 beams that share the pages of their prompt), and not otherwise.
+ *                 beams that share the pages of their prompt), and not otherwise.  Beams that
+ *                 share a row of dst must be given one and the same row.
  *   lengths     : [B] int32, at most max_pages * P
  *   out_status  : RS_SEQ_BAD_PARAM as above; RS_SEQ_BAD_PAGE: a page number outside the cache;
  *                 the rows that it is for are not moved

@@ -56,14 +56,23 @@ __device__ __forceinline__ int64_t readlane_i64(int64_t v, int l) {
 // of every beam's state: it loads the new value of each beam and then stores them, so a move in
 // place needs no second buffer and no wait between workgroups.  A wave takes a piece, bytes that
 // lie one after another.
+// Arguments are kept short: a launch with 160 bytes of them takes the host 3.5 us, with 16 2.9.
+struct Strides {
+    int64_t outer, page, inner, position;
+};
+Strides strides_of(const rs_rows& r) { return {r.outer_stride, r.page_stride, r.inner_stride, r.position_stride}; }
+
 struct ReorderParams {
     const uint8_t* src;
     uint8_t* dst;
-    rs_rows s, d;
+    Strides s, d;
     const int32_t* parent;           // [B][K]
     const int32_t* lengths;          // [B] or NULL
     const int32_t *src_table, *dst_table;
     int64_t src_table_stride, dst_table_stride;
+    int64_t row;                     // bytes
+    uint32_t outer, inner, S;        // positions of a state, or of a page
+    uint32_t src_pages, dst_pages;
     int32_t max_pages;               // entries of a table's row
     int32_t W, K, G;                 // workgroups a sequence
     int32_t together;                // positions lie one after another
@@ -82,7 +91,7 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
     const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
     const int32_t* parent = P.parent + (int64_t)b * P.K;
-    const int S = (int)P.s.positions;
+    const int S = (int)P.S;
     const int64_t room = PAGED ? (int64_t)P.max_pages * S : S;
     const int64_t len = P.lengths ? P.lengths[b] : S;
     const int mine = lane < P.K ? parent[lane] : -1;
@@ -99,8 +108,8 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
                 for (int k = 0; k < P.K; ++k) {
                     const int w = parent[k];
                     if (w < 0) continue;
-                    out |= (uint32_t)from_table[w * P.src_table_stride + e] >= (uint32_t)P.s.pages;
-                    out |= (uint32_t)to_table[k * P.dst_table_stride + e] >= (uint32_t)P.d.pages;
+                    out |= (uint32_t)from_table[w * P.src_table_stride + e] >= P.src_pages;
+                    out |= (uint32_t)to_table[k * P.dst_table_stride + e] >= P.dst_pages;
                 }
             if (__syncthreads_or(out)) st = RS_SEQ_BAD_PAGE;
         }
@@ -108,9 +117,9 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
     }
     if (bad || len == 0) return;
     const uint32_t full = (uint32_t)(len / S), rest = (uint32_t)(len % S), each = (uint32_t)P.pieces;
-    const int64_t row = P.s.row_bytes;
+    const int64_t row = P.row;
     const uint32_t nq = P.together ? full * each + (uint32_t)((rest * row + kPiece - 1) / kPiece) : (uint32_t)len * each;
-    const uint32_t inner = (uint32_t)P.s.inner, all = (uint32_t)P.s.outer * inner * nq;
+    const uint32_t inner = P.inner, all = P.outer * inner * nq;
     for (uint32_t piece = g * kReorderWaves + wave; piece < all; piece += P.G * kReorderWaves) {
         // quotients are computed in vector registers
         const uint32_t oi = uniform_i(piece / nq), q = piece - oi * nq, o = uniform_i(oi / inner), i = oi - o * inner;
@@ -126,18 +135,18 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
         }
         bytes = min(bytes, kPiece);
         // lane k has beam k's addresses
-        int64_t from = o * P.s.outer_stride + i * P.s.inner_stride + t * P.s.position_stride + first;
-        int64_t to = o * P.d.outer_stride + i * P.d.inner_stride + t * P.d.position_stride + first;
+        int64_t from = o * P.s.outer + i * P.s.inner + t * P.s.position + first;
+        int64_t to = o * P.d.outer + i * P.d.inner + t * P.d.position + first;
         bool moves = mine >= 0;
         if (moves) {
             int64_t f = (int64_t)b * P.W + mine, d = (int64_t)b * P.K + lane;
             if (PAGED) {
                 f = from_table[mine * P.src_table_stride + page];
                 d = to_table[lane * P.dst_table_stride + page];
-                moves = (uint64_t)f < (uint64_t)P.s.pages && (uint64_t)d < (uint64_t)P.d.pages;
+                moves = (uint32_t)f < P.src_pages && (uint32_t)d < P.dst_pages;
             }
-            from += reinterpret_cast<int64_t>(P.src) + f * P.s.page_stride;
-            to += reinterpret_cast<int64_t>(P.dst) + d * P.d.page_stride;
+            from += reinterpret_cast<int64_t>(P.src) + f * P.s.page;
+            to += reinterpret_cast<int64_t>(P.dst) + d * P.d.page;
         }
         const uint64_t on = __ballot(moves && from != to);      // equal: where it is
         auto move = [&](auto zero, uint32_t c) {
@@ -595,12 +604,14 @@ __global__ void rs_path_nodes_kernel(const int32_t* __restrict__ parent, const i
 
 struct CommitParams {
     uint8_t* cache;
-    rs_rows c;
+    const uint8_t* source;               // the cache, or rows elsewhere
+    Strides c, s;
     const int32_t *slots, *path;
-    const uint8_t* source;               // NULL: the cache
-    rs_rows s;
-    int32_t N, depth, G;                 // workgroups a sequence
     int32_t* status;
+    uint32_t outer, inner, bytes;        // of a row
+    uint32_t page, room;                 // slots of a page, and of the cache
+    int32_t N, depth, G;                 // workgroups a sequence
+    bool within;                         // the source is the cache
 };
 
 constexpr int kCommitBlock = 256, kCommitWaves = kCommitBlock / 64;
@@ -615,7 +626,7 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
     const int b = blockIdx.x / P.G, g = blockIdx.x % P.G;
     const int32_t* path = P.path + (int64_t)b * P.depth;
     const int32_t* slots = P.slots + (int64_t)b * P.N;
-    const uint32_t room = (uint32_t)(P.c.pages * P.c.positions), page = (uint32_t)P.c.positions;
+    const uint32_t room = P.room, page = P.page;
     // the rows of entries first .. first + 63: how many, and whether they can be moved
     int64_t from = 0, to = 0;
     int before = -1;                     // the entry before these
@@ -633,20 +644,20 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
         bool out = on && !order && slot >= room;
         from = to = 0;
         if (on && !order && !out) {
-            to = slot / page * P.c.page_stride + slot % page * P.c.position_stride;
-            if (P.source) {
-                from = b * P.s.page_stride + x * P.s.position_stride;
+            to = slot / page * P.c.page + slot % page * P.c.position;
+            if (!P.within) {
+                from = b * P.s.page + x * P.s.position;
             } else {
                 const uint32_t was = (uint32_t)slots[x];
                 out = was >= room;
-                from = was / page * P.c.page_stride + was % page * P.c.position_stride;
+                from = was / page * P.c.page + was % page * P.c.position;
             }
         }
         wrong |= __ballot(order) != 0;
         outside |= __ballot(out) != 0;
         before = n == 64 ? __builtin_amdgcn_readlane(x, 63) : before;
         // rows that are where they belong are the path's first
-        start = P.source ? 0 : __popcll(__ballot(on && x == i));
+        start = !P.within ? 0 : __popcll(__ballot(on && x == i));
         return n;
     };
     int n = look(0);
@@ -658,16 +669,13 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
     if (g == 0 && threadIdx.x == 0 && P.status)
         P.status[b] = wrong ? RS_SEQ_BAD_TREE : outside ? RS_SEQ_BAD_PAGE : RS_SEQ_OK;
     if (wrong || outside) return;
-    const uint32_t inner = (uint32_t)P.c.inner, pieces = (uint32_t)P.c.outer * inner;
-    const uint32_t bytes = (uint32_t)P.c.row_bytes, whole = bytes & ~15u;
-    const uint8_t* source = P.source ? P.source : P.cache;
-    const int64_t outer_stride = P.source ? P.s.outer_stride : P.c.outer_stride;
-    const int64_t inner_stride = P.source ? P.s.inner_stride : P.c.inner_stride;
+    const uint32_t inner = P.inner, pieces = P.outer * inner;
+    const uint32_t bytes = P.bytes, whole = bytes & ~15u;
     auto move_all = [&]() {
         for (uint32_t piece = g * kCommitWaves + wave; piece < pieces; piece += P.G * kCommitWaves) {
             const uint32_t o = uniform_i(piece / inner), i = piece - o * inner;
-            const uint8_t* x = source + o * outer_stride + i * inner_stride;
-            uint8_t* y = P.cache + o * P.c.outer_stride + i * P.c.inner_stride;
+            const uint8_t* x = P.source + o * P.s.outer + i * P.s.inner;
+            uint8_t* y = P.cache + o * P.c.outer + i * P.c.inner;
             auto move = [&](auto zero, uint32_t c) {
                 using T = decltype(zero);
                 for (int r = start; r < n; r += 8) {
@@ -682,7 +690,7 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
             };
             // what is left of a row: its last 16 bytes once more where they come from elsewhere
             const uint32_t tail = bytes - whole;
-            const bool again = P.source && tail && whole;
+            const bool again = !P.within && tail && whole;
             for (uint32_t c = lane * 16; c < whole + (again ? 16 : 0); c += 64 * 16)
                 move(u32x4{}, c < whole ? c : bytes - 16);
             if (!again && lane < tail) move(uint8_t{}, whole + lane);
@@ -746,8 +754,15 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
     ReorderParams P{};
     P.src = static_cast<const uint8_t*>(src);
     P.dst = static_cast<uint8_t*>(dst);
-    P.s = *src_rows;
-    P.d = *dst_rows;
+    P.s = strides_of(*src_rows);
+    P.d = strides_of(*dst_rows);
+    P.row = src_rows->row_bytes;
+    P.outer = (uint32_t)src_rows->outer;
+    P.inner = (uint32_t)src_rows->inner;
+    P.S = (uint32_t)src_rows->positions;
+    // a table's numbers do not reach further
+    P.src_pages = (uint32_t)std::min(src_rows->pages, (int64_t)INT_MAX);
+    P.dst_pages = (uint32_t)std::min(dst_rows->pages, (int64_t)INT_MAX);
     P.parent = parent;
     P.lengths = lengths;
     P.src_table = src_table;
@@ -886,11 +901,17 @@ rs_status resispec_commit_path(void* cache, const rs_rows* cache_rows, const int
     if (!cache || !slots || !path) return RS_ERR_INVALID_ARG;
     CommitParams P{};
     P.cache = static_cast<uint8_t*>(cache);
-    P.c = *cache_rows;
+    P.c = strides_of(*cache_rows);
     P.slots = slots;
     P.path = path;
-    P.source = static_cast<const uint8_t*>(source);
-    if (source) P.s = *source_rows;
+    P.within = !source;
+    P.source = source ? static_cast<const uint8_t*>(source) : P.cache;
+    P.s = source ? strides_of(*source_rows) : P.c;
+    P.outer = (uint32_t)cache_rows->outer;
+    P.inner = (uint32_t)cache_rows->inner;
+    P.bytes = (uint32_t)cache_rows->row_bytes;
+    P.page = (uint32_t)cache_rows->positions;
+    P.room = (uint32_t)(cache_rows->pages * cache_rows->positions);
     P.N = N;
     P.depth = depth;
     P.status = out_status;

@@ -137,11 +137,11 @@ def _load():
     lib.resispec_filter_logits.restype = i32
     lib.resispec_token_logprobs.argtypes = [P, i64, P, i32, i32, i32, flt, P, P, P, P]
     lib.resispec_token_logprobs.restype = i32
-    lib.resispec_beam_select.argtypes = [P, i64, P, P, i32, i32, i32, i32, i32, flt, P, P, P, P, P, sz, P]
+    lib.resispec_beam_select.argtypes = [P, i64, P, P, i32, i32, i32, i32, i32, P, P, P, P, P, P, sz, P]
     lib.resispec_beam_select.restype = i32
     lib.resispec_beam_workspace_bytes.argtypes = [i32, i32, i32]
     lib.resispec_beam_workspace_bytes.restype = sz
-    rows = ctypes.POINTER(RsRows)
+    rows = P            # an rs_rows by its address: a struct kept with its layout is not wrapped again
     lib.resispec_beam_reorder.argtypes = [P, rows, P, rows, P, P, i32, i32, i32, P, P]
     lib.resispec_beam_reorder.restype = i32
     lib.resispec_beam_reorder_paged.argtypes = [P, rows, P, i64, P, rows, P, i64, i32, P, P, i32, i32, i32, P, P]
@@ -963,6 +963,24 @@ def resispec_beam_workspace_bytes(B: int, W: int, V: int) -> int:
     return lib.resispec_beam_workspace_bytes(int(B), int(W), int(V))
 
 
+def _device(t, name):
+    """The number of a tensor's device."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    return t.get_device()
+
+
+def _at(t, shape, dtype, d, like, name):
+    """_given, with the device's number looked up once for a call's tensors."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == d and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _given(t, shape, dtype, like, name)
+
+
 def _int32(v, name):
     """A whole number that ctypes will not cut to its low 32 bits."""
     v = int(v)
@@ -988,18 +1006,20 @@ def resispec_beam_select(logits, scores, *, k=None, temperature=1.0, ended=None,
     B, W = shape
     if R != B * W or (len(lead) == 2 and lead != shape):
         raise ValueError("logits has rows %s, expected %s" % (tuple(lead), tuple(shape)))
+    d = logits.get_device()
     k = W if k is None else _int32(k, "k")
     end_token = _int32(end_token, "end_token")
     if isinstance(temperature, torch.Tensor):
         f = _settings(logits, shape, R, temperature, 0, 1.0, 0.0)
+        at = ctypes.addressof(f)
     else:
-        f = _number_settings(logits.dtype is torch.bfloat16, float(temperature))
-    sp = _given(scores, shape, torch.float32, logits, "scores")
+        f, at = _number_settings(logits.dtype is torch.bfloat16, float(temperature))
+    sp = _at(scores, shape, torch.float32, d, logits, "scores")
     ep = None
     if ended is not None:
         if not isinstance(ended, torch.Tensor):
             raise ValueError("ended must be a device tensor")
-        ep = _given(ended, shape, torch.bool if ended.dtype is torch.bool else torch.uint8, logits, "ended")
+        ep = _at(ended, shape, torch.bool if ended.dtype is torch.bool else torch.uint8, d, logits, "ended")
     handle = _handle(logits, stream)
     if handle is None:
         return _elsewhere(logits, stream, resispec_beam_select, logits, scores, k=k, temperature=temperature, ended=ended,
@@ -1016,24 +1036,25 @@ def resispec_beam_select(logits, scores, *, k=None, temperature=1.0, ended=None,
         out_status = torch.empty(B, dtype=i32, device=logits.device)
     if workspace is None:
         workspace = torch.empty(max(1, lib.resispec_beam_workspace_bytes(B, W, V)), dtype=torch.uint8, device=logits.device)
-    _check(lib.resispec_beam_select(ptr, step, sp, ep, end_token, B, W, V, k, f,
-                                    _given(out_parent, to, i32, logits, "out_parent"),
-                                    _given(out_token, to, i32, logits, "out_token"),
-                                    _given(out_score, to, torch.float32, logits, "out_score"),
-                                    _given(out_status, (B,), i32, logits, "out_status"),
-                                    _given(workspace, workspace.shape, torch.uint8, logits, "workspace"),
+    _check(lib.resispec_beam_select(ptr, step, sp, ep, end_token, B, W, V, k, at,
+                                    _at(out_parent, to, i32, d, logits, "out_parent"),
+                                    _at(out_token, to, i32, d, logits, "out_token"),
+                                    _at(out_score, to, torch.float32, d, logits, "out_score"),
+                                    _at(out_status, (B,), i32, d, logits, "out_status"),
+                                    _at(workspace, workspace.shape, torch.uint8, d, logits, "workspace"),
                                     workspace.numel(), handle))
     return out_parent, out_token, out_score, out_status
 
 
 @functools.lru_cache(maxsize=256)
 def _number_settings(bf16, temperature):
-    return RsFilter(RS_BF16 if bf16 else RS_F32, 1, temperature, 0, 1.0, 0.0)
+    f = RsFilter(RS_BF16 if bf16 else RS_F32, 1, temperature, 0, 1.0, 0.0)
+    return f, ctypes.addressof(f)
 
 
 @functools.lru_cache(maxsize=1024)
 def _layout(shape, stride, size, page_dim, position_dim, name):
-    """(rs_rows, bytes from the first to past the last) of rows in a tensor: the dimensions
+    """(rs_rows, bytes from the first to past the last, its address) of rows in a tensor: the dimensions
     before page_dim are outer, those between it and position_dim inner, those after
     position_dim (without one: after page_dim) the row, which has to lie together."""
     def place(d, what):
@@ -1075,7 +1096,7 @@ def _layout(shape, stride, size, page_dim, position_dim, name):
         span += (n - 1) * d
     r = RsRows(outer[0], pages[0], inner[0], positions[0], row * size,
                *(d * size for _, d in (outer, pages, inner, positions)))
-    return r, span * size
+    return r, span * size, ctypes.addressof(r)
 
 
 def _row_layout(t, page_dim, position_dim, name):
@@ -1102,25 +1123,28 @@ def _table(t, rows, like, name):
     return t.data_ptr(), step, n
 
 
-def _moved_to(src, layout, span, dst, name, *dims):
-    """Where rows go: (address, layout).  The same rows, or apart from them."""
+def _moved_to(src, rows, dst, name, *dims):
+    """Where rows go: (address, layout as _layout gives it).  The same rows, or apart from them."""
     if dst is None or dst is src:
-        return src.data_ptr(), layout
-    to, to_span = _row_layout(dst, *dims, name)
+        return src.data_ptr(), rows
+    to = _row_layout(dst, *dims, name)
     if dst.dtype is not src.dtype:
         raise TypeError("%s must be %s" % (name, src.dtype))
     if dst.get_device() != src.get_device():
         raise ValueError("all tensors must be on one device, got %s" % {dst.device, src.device})
     a, b = src.data_ptr(), dst.data_ptr()
-    if a < b + to_span and b < a + span and not (a == b and bytes(layout) == bytes(to)):
+    if a < b + to[1] and b < a + rows[1] and not (a == b and bytes(rows[0]) == bytes(to[0])):
         raise ValueError("%s must be apart from the rows it is taken from, or the same rows" % name)
     return b, to
 
 
-def _none(of, rows):
-    """Whether there are no sequences, and so nothing to move."""
+def _chosen(parent, rows):
+    """(B, K) of parent beams, and whether there is nothing to move."""
     import torch
-    return isinstance(of, torch.Tensor) and of.is_cuda and of.dim() == 2 and of.shape[0] == 0 and rows.is_cuda
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
+        raise ValueError("parent must be a [B, K] tensor")
+    B, K = parent.shape
+    return B, K, B == 0 and parent.is_cuda and rows.is_cuda
 
 
 def _empty(status, like):
@@ -1128,14 +1152,11 @@ def _empty(status, like):
     return torch.empty(0, dtype=torch.int32, device=like.device) if status is None else status
 
 
-def _beams(parent, n, like, name):
-    import torch
-    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
-        raise ValueError("parent must be a [B, K] tensor")
-    B, K = parent.shape
+def _per_sequence(n, B, name):
+    """How many of n beams each of B sequences has."""
     if n % B or n < B:
         raise ValueError("%s has %d beams, parent %d sequences" % (name, n, B))
-    return B, n // B, K, _given(parent, parent.shape, torch.int32, like, "parent")
+    return n // B
 
 
 def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengths=None, out=None, out_status=None,
@@ -1145,26 +1166,29 @@ def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengt
     with B * K, or None for a move in place (K = W).  lengths (int32 [B], with position_dim):
     only so many positions are moved.  Returns (out, status)."""
     import torch
-    if _none(parent, state):
+    B, K, none = _chosen(parent, state)
+    if none:
         return (state if out is None else out), _empty(out_status, parent)
-    src, span = _row_layout(state, beam_dim, position_dim, "state")
-    B, W, K, pp = _beams(parent, src.pages, state, "state")
+    src = _row_layout(state, beam_dim, position_dim, "state")
+    d = state.get_device()
+    W = _per_sequence(src[0].pages, B, "state")
+    pp = _at(parent, parent.shape, torch.int32, d, state, "parent")
     if lengths is not None and position_dim is None:
         raise ValueError("lengths need position_dim")
     if out is None and K != W:
         raise ValueError("a move in place needs as many beams as there are, %d, got %d" % (W, K))
-    to, dst = _moved_to(state, src, span, out, "out", beam_dim, position_dim)
-    if dst.pages != B * K:
-        raise ValueError("out has %d beams, expected %d" % (dst.pages, B * K))
-    lp = None if lengths is None else _given(lengths, (B,), torch.int32, state, "lengths")
+    to, dst = _moved_to(state, src, out, "out", beam_dim, position_dim)
+    if dst[0].pages != B * K:
+        raise ValueError("out has %d beams, expected %d" % (dst[0].pages, B * K))
+    lp = None if lengths is None else _at(lengths, (B,), torch.int32, d, state, "lengths")
     handle = _handle(state, stream)
     if handle is None:
         return _elsewhere(state, stream, resispec_beam_reorder, state, parent, beam_dim=beam_dim, position_dim=position_dim,
                           lengths=lengths, out=out, out_status=out_status)
     if out_status is None:
         out_status = torch.empty(B, dtype=torch.int32, device=state.device)
-    _check(lib.resispec_beam_reorder(state.data_ptr(), src, to, dst, pp, lp, B, W, K,
-                                     _given(out_status, (B,), torch.int32, state, "out_status"), handle))
+    _check(lib.resispec_beam_reorder(state.data_ptr(), src[2], to, dst[2], pp, lp, B, W, K,
+                                     _at(out_status, (B,), torch.int32, d, state, "out_status"), handle))
     return (state if out is None else out), out_status
 
 
@@ -1175,12 +1199,15 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
     block_table) says where the chosen beams' positions go, in `out` (default: the cache
     itself).  Returns (out, status)."""
     import torch
-    if _none(parent, cache):
+    B, K, none = _chosen(parent, cache)
+    if none:
         return (cache if out is None else out), _empty(out_status, parent)
-    src, span = _row_layout(cache, page_dim, position_dim, "cache")
+    src = _row_layout(cache, page_dim, position_dim, "cache")
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be a [B * W, pages] tensor")
-    B, W, K, pp = _beams(parent, block_table.shape[0], cache, "block_table")
+    d = cache.get_device()
+    W = _per_sequence(block_table.shape[0], B, "block_table")
+    pp = _at(parent, parent.shape, torch.int32, d, cache, "parent")
     tp, tstep, n = _table(block_table, B * W, cache, "block_table")
     if out_table is None:
         if K != W:
@@ -1192,16 +1219,16 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
             raise ValueError("out_table has %d entries a row, block_table %d" % (on, n))
     if out is None and K != W:
         raise ValueError("a move within the cache needs as many beams as there are, %d, got %d" % (W, K))
-    to, dst = _moved_to(cache, src, span, out, "out", page_dim, position_dim)
-    lp = _given(lengths, (B,), torch.int32, cache, "lengths")
+    to, dst = _moved_to(cache, src, out, "out", page_dim, position_dim)
+    lp = _at(lengths, (B,), torch.int32, d, cache, "lengths")
     handle = _handle(cache, stream)
     if handle is None:
         return _elsewhere(cache, stream, resispec_beam_reorder_paged, cache, block_table, parent, lengths,
                           page_dim=page_dim, position_dim=position_dim, out_table=out_table, out=out, out_status=out_status)
     if out_status is None:
         out_status = torch.empty(B, dtype=torch.int32, device=cache.device)
-    _check(lib.resispec_beam_reorder_paged(cache.data_ptr(), src, tp, tstep, to, dst, op, ostep, n, pp, lp, B, W, K,
-                                           _given(out_status, (B,), torch.int32, cache, "out_status"), handle))
+    _check(lib.resispec_beam_reorder_paged(cache.data_ptr(), src[2], tp, tstep, to, dst[2], op, ostep, n, pp, lp, B, W, K,
+                                           _at(out_status, (B,), torch.int32, d, cache, "out_status"), handle))
     return (cache if out is None else out), out_status
 
 
@@ -1221,15 +1248,15 @@ def resispec_plan_cache(kept, added, held, block_table, free_pages, free_count, 
     import torch
     if not isinstance(kept, torch.Tensor) or kept.dim() != 1:
         raise ValueError("kept must be a [R] tensor")
-    R, like, shape = kept.shape[0], kept, kept.shape
-    kp, ap = _given(kept, shape, torch.int32, like, "kept"), _given(added, shape, torch.int32, like, "added")
-    hp = _given(held, shape, torch.int32, like, "held")
+    R, like, shape, d = kept.shape[0], kept, kept.shape, _device(kept, "kept")
+    kp, ap = _at(kept, shape, torch.int32, d, like, "kept"), _at(added, shape, torch.int32, d, like, "added")
+    hp = _at(held, shape, torch.int32, d, like, "held")
     tp, step, n = _table(block_table, R, like, "block_table")
     if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
         raise ValueError("free_pages must be a [pages] tensor")
     pages = free_pages.shape[0]
-    fp = _given(free_pages, (pages,), torch.int32, like, "free_pages")
-    cp = _given(free_count, (1,), torch.int32, like, "free_count")
+    fp = _at(free_pages, (pages,), torch.int32, d, like, "free_pages")
+    cp = _at(free_count, (1,), torch.int32, d, like, "free_count")
     if max_slots is None:
         if out_slots is None:
             raise ValueError("max_slots or out_slots is required")
@@ -1262,13 +1289,13 @@ def resispec_plan_cache(kept, added, held, block_table, free_pages, free_count, 
         out_status = torch.empty(R, dtype=i32, device=dev)
     requests, rows = (R,), (T,)
     _check(lib.resispec_plan_cache(kp, ap, hp, R, page_size, tp, step, n, fp, cp, pages,
-                                   _given(out_held, requests, i32, like, "out_held"),
-                                   _given(out_free_count, (1,), i32, like, "out_free_count"),
-                                   _given(out_starts, (R + 1,), i32, like, "out_starts"), T,
-                                   _given(out_slots, rows, i32, like, "out_slots"),
-                                   _given(out_positions, rows, i32, like, "out_positions"),
-                                   _given(out_requests, rows, i32, like, "out_requests"),
-                                   _given(out_status, requests, i32, like, "out_status"), handle))
+                                   _at(out_held, requests, i32, d, like, "out_held"),
+                                   _at(out_free_count, (1,), i32, d, like, "out_free_count"),
+                                   _at(out_starts, (R + 1,), i32, d, like, "out_starts"), T,
+                                   _at(out_slots, rows, i32, d, like, "out_slots"),
+                                   _at(out_positions, rows, i32, d, like, "out_positions"),
+                                   _at(out_requests, rows, i32, d, like, "out_requests"),
+                                   _at(out_status, requests, i32, d, like, "out_status"), handle))
     return out_slots, out_positions, out_requests, out_starts, out_held, out_free_count, out_status
 
 
@@ -1281,9 +1308,9 @@ def resispec_accepted_path(parent, node_token, tokens, accepted_len, *, out_path
         raise ValueError("parent must be [B, N], tokens [B, max_depth + 1]")
     B, N = parent.shape
     shape = (B, tokens.shape[1])
-    i32, like = torch.int32, parent
-    pp, np_ = _given(parent, (B, N), i32, like, "parent"), _given(node_token, (B, N), i32, like, "node_token")
-    tp, lp = _given(tokens, shape, i32, like, "tokens"), _given(accepted_len, (B,), i32, like, "accepted_len")
+    i32, like, d = torch.int32, parent, _device(parent, "parent")
+    pp, np_ = _at(parent, (B, N), i32, d, like, "parent"), _at(node_token, (B, N), i32, d, like, "node_token")
+    tp, lp = _at(tokens, shape, i32, d, like, "tokens"), _at(accepted_len, (B,), i32, d, like, "accepted_len")
     handle = _handle(like, stream)
     if handle is None:
         return _elsewhere(like, stream, resispec_accepted_path, parent, node_token, tokens, accepted_len, out_path=out_path,
@@ -1292,8 +1319,8 @@ def resispec_accepted_path(parent, node_token, tokens, accepted_len, *, out_path
         out_path = torch.empty(shape, dtype=i32, device=parent.device)
     if out_status is None:
         out_status = torch.empty(B, dtype=i32, device=parent.device)
-    _check(lib.resispec_accepted_path(pp, np_, tp, lp, B, N, shape[1] - 1, _given(out_path, shape, i32, like, "out_path"),
-                                      _given(out_status, (B,), i32, like, "out_status"), handle))
+    _check(lib.resispec_accepted_path(pp, np_, tp, lp, B, N, shape[1] - 1, _at(out_path, shape, i32, d, like, "out_path"),
+                                      _at(out_status, (B,), i32, d, like, "out_status"), handle))
     return out_path, out_status
 
 
@@ -1303,32 +1330,32 @@ def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, positio
     (int32 [B, N]).  It comes from `source`, laid out as the cache with trees for pages and nodes
     for positions, or, without one, from the node's own slot.  Returns (cache, status)."""
     import torch
-    if _none(slots, cache):
-        return cache, _empty(out_status, slots)
-    rows, span = _row_layout(cache, page_dim, position_dim, "cache")
     if not isinstance(slots, torch.Tensor) or slots.dim() != 2 or not isinstance(path, torch.Tensor) or path.dim() != 2:
         raise ValueError("slots must be [B, N], path [B, depth]")
     B, N = slots.shape
-    i32 = torch.int32
-    sp, pp = _given(slots, (B, N), i32, cache, "slots"), _given(path, (B, path.shape[1]), i32, cache, "path")
+    rows = _row_layout(cache, page_dim, position_dim, "cache")
+    if B == 0 and slots.is_cuda:
+        return cache, _empty(out_status, slots)
+    i32, d = torch.int32, cache.get_device()
+    sp, pp = _at(slots, (B, N), i32, d, cache, "slots"), _at(path, (B, path.shape[1]), i32, d, cache, "path")
     at = rows_of = None
     if source is not None:
-        rows_of, source_span = _row_layout(source, page_dim, position_dim, "source")
+        layout, source_span, rows_of = _row_layout(source, page_dim, position_dim, "source")
         at = source.data_ptr()
         if source.dtype is not cache.dtype:
             raise TypeError("source must be %s" % cache.dtype)
         if source.get_device() != cache.get_device():
             raise ValueError("all tensors must be on one device, got %s" % {source.device, cache.device})
-        if at < cache.data_ptr() + span and cache.data_ptr() < at + source_span:
+        if at < cache.data_ptr() + rows[1] and cache.data_ptr() < at + source_span:
             raise ValueError("source must be apart from the cache")
-        if rows_of.pages != B or rows_of.positions != N:
-            raise ValueError("source has %d trees of %d nodes, expected %d of %d" % (rows_of.pages, rows_of.positions, B, N))
+        if layout.pages != B or layout.positions != N:
+            raise ValueError("source has %d trees of %d nodes, expected %d of %d" % (layout.pages, layout.positions, B, N))
     handle = _handle(cache, stream)
     if handle is None:
         return _elsewhere(cache, stream, resispec_commit_path, cache, slots, path, source=source, page_dim=page_dim,
                           position_dim=position_dim, out_status=out_status)
     if out_status is None:
         out_status = torch.empty(B, dtype=i32, device=cache.device)
-    _check(lib.resispec_commit_path(cache.data_ptr(), rows, sp, pp, at, rows_of, B, N, path.shape[1],
-                                    _given(out_status, (B,), i32, cache, "out_status"), handle))
+    _check(lib.resispec_commit_path(cache.data_ptr(), rows[2], sp, pp, at, rows_of, B, N, path.shape[1],
+                                    _at(out_status, (B,), i32, d, cache, "out_status"), handle))
     return cache, out_status

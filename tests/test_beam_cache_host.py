@@ -62,12 +62,12 @@ def rows(**kw):
 
 
 def reorder(src=FAKE, s=None, dst=ctypes.c_void_p(0x90000), d=None, parent=FAKE, lengths=None, B=2, W=4, K=4):
-    return lib.resispec_beam_reorder(src, s or rows(), dst, d or rows(), parent, lengths, B, W, K, None, None)
+    return lib.resispec_beam_reorder(src, ctypes.byref(s or rows()), dst, ctypes.byref(d or rows()), parent, lengths, B, W, K, None, None)
 
 
 def paged(src=FAKE, s=None, table=FAKE, step=6, dst=FAKE, d=None, to=FAKE, to_step=6, n=6, parent=FAKE, lengths=FAKE, B=2,
           W=4, K=4):
-    return lib.resispec_beam_reorder_paged(src, s or rows(), table, step, dst, d or rows(), to, to_step, n, parent,
+    return lib.resispec_beam_reorder_paged(src, ctypes.byref(s or rows()), table, step, dst, ctypes.byref(d or rows()), to, to_step, n, parent,
                                            lengths, B, W, K, None, None)
 
 
@@ -122,7 +122,8 @@ def path_call(parent=FAKE, token=FAKE, tokens=FAKE, length=FAKE, B=2, N=5, D=3, 
 
 
 def commit_call(cache=FAKE, c=None, slots=FAKE, path=FAKE, source=None, s=None, B=8, N=5, depth=3):
-    return lib.resispec_commit_path(cache, c or rows(), slots, path, source, s, B, N, depth, None, None)
+    return lib.resispec_commit_path(cache, ctypes.byref(c or rows()), slots, path, source, None if s is None else ctypes.byref(s), B,
+                                    N, depth, None, None)
 
 
 def test_path_and_commit_refusals():
@@ -155,7 +156,7 @@ def test_binding_refuses_host_tensors():
 
 
 def layout(t, *dims):
-    r, span = native._layout(t.shape, t.stride(), t.element_size(), *dims, "t")
+    r, span, _ = native._layout(t.shape, t.stride(), t.element_size(), *dims, "t")
     return tuple(getattr(r, n) for n, _ in native.RsRows._fields_), span
 
 
