@@ -31,18 +31,32 @@ template <>
 struct Any<uint8_t> {
     using type = uint8_t;
 };
+// In registers: a byte has one of its own (four to a register wait for one another).
 template <typename T>
-__device__ __forceinline__ T load_at(const uint8_t* p) {
-    return *reinterpret_cast<const typename Any<T>::type*>(p);
+using Held = std::conditional_t<sizeof(T) == 1, uint32_t, T>;
+// By the address, in global memory: an address that has been through lanes is one of any memory
+// to the compiler.
+template <typename T>
+__device__ __forceinline__ T load_at(int64_t at, uint32_t c) {
+    using G = const __attribute__((address_space(1))) uint8_t;
+    return *(const __attribute__((address_space(1))) typename Any<T>::type*)((G*)at + c);
 }
 // Rows are stored past the caches, which they would only fill: 40 states of 492 KB 39 us with
 // ordinary stores and 25 with these, 1024 paths in rows of 1000 bytes 36 and 27.  Loads stay
 // ordinary: beams of one parent, and the ends of rows, share lines.
 template <typename T>
-__device__ __forceinline__ void store_at(uint8_t* p, T v) {
+__device__ __forceinline__ void store_at(int64_t at, uint32_t c, T v) {
+    using G = __attribute__((address_space(1))) uint8_t;
+    auto* p = (__attribute__((address_space(1))) typename Any<T>::type*)((G*)at + c);
     if constexpr (sizeof(T) == 1) *p = v;
-    else __builtin_nontemporal_store(v, reinterpret_cast<typename Any<T>::type*>(p));
+    else __builtin_nontemporal_store(v, p);
 }
+
+// Waits for the wave's loads, here and once.  Loads that may or may not have been made leave the
+// compiler to wait before every store for all that came before it, the stores among them: 32
+// beams of 3 KB 13.7 us, with this wait and bytes in registers of their own 7.1,
+// 64 of 200 KB in 24 layers 166 and 97.  (vmcnt 0, the other counters as they are.)
+__device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 __device__ __forceinline__ int uniform_i(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t readlane_i64(int64_t v, int l) {
@@ -102,15 +116,15 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
         int st = bad ? RS_SEQ_BAD_PARAM : RS_SEQ_OK;
         if (PAGED && !bad) {
             // every page that the sequence's rows are moved from or to
-            const int used = (int)((len + S - 1) / S);
+            const uint32_t used = (uint32_t)((len + S - 1) / S);
             bool out = false;
-            for (int e = threadIdx.x; e < used; e += kReorderBlock)
-                for (int k = 0; k < P.K; ++k) {
-                    const int w = parent[k];
-                    if (w < 0) continue;
-                    out |= (uint32_t)from_table[w * P.src_table_stride + e] >= P.src_pages;
-                    out |= (uint32_t)to_table[k * P.dst_table_stride + e] >= P.dst_pages;
-                }
+            for (uint32_t x = threadIdx.x; x < used * P.K; x += kReorderBlock) {
+                const uint32_t k = x / used, e = x - k * used;
+                const int w = parent[k];
+                if (w < 0) continue;
+                out |= (uint32_t)from_table[w * P.src_table_stride + e] >= P.src_pages;
+                out |= (uint32_t)to_table[k * P.dst_table_stride + e] >= P.dst_pages;
+            }
             if (__syncthreads_or(out)) st = RS_SEQ_BAD_PAGE;
         }
         if (threadIdx.x == 0) P.status[b] = st;
@@ -151,13 +165,14 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
         const uint64_t on = __ballot(moves && from != to);      // equal: where it is
         auto move = [&](auto zero, uint32_t c) {
             using E = decltype(zero);
-            E v[KMAX];
+            Held<E> v[KMAX];
 #pragma unroll
             for (int k = 0; k < KMAX; ++k)
-                if (on >> k & 1) v[k] = load_at<E>(reinterpret_cast<const uint8_t*>(readlane_i64(from, k)) + c);
+                if (on >> k & 1) v[k] = load_at<E>(readlane_i64(from, k), c);
+            wait_for_loads();
 #pragma unroll
             for (int k = 0; k < KMAX; ++k)
-                if (on >> k & 1) store_at<E>(reinterpret_cast<uint8_t*>(readlane_i64(to, k)) + c, v[k]);
+                if (on >> k & 1) store_at<E>(readlane_i64(to, k), c, (E)v[k]);
         };
         // columns, and bytes at a run's end
         const uint32_t whole = (uint32_t)bytes / sizeof(T) * sizeof(T), c = lane * sizeof(T);
@@ -674,18 +689,19 @@ __global__ void __launch_bounds__(kCommitBlock) rs_commit_kernel(const CommitPar
     auto move_all = [&]() {
         for (uint32_t piece = g * kCommitWaves + wave; piece < pieces; piece += P.G * kCommitWaves) {
             const uint32_t o = uniform_i(piece / inner), i = piece - o * inner;
-            const uint8_t* x = P.source + o * P.s.outer + i * P.s.inner;
-            uint8_t* y = P.cache + o * P.c.outer + i * P.c.inner;
+            const int64_t x = reinterpret_cast<int64_t>(P.source) + o * P.s.outer + i * P.s.inner;
+            const int64_t y = reinterpret_cast<int64_t>(P.cache) + o * P.c.outer + i * P.c.inner;
             auto move = [&](auto zero, uint32_t c) {
                 using T = decltype(zero);
                 for (int r = start; r < n; r += 8) {
-                    T v[8];
+                    Held<T> v[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (r + j < n) v[j] = load_at<T>((x + readlane_i64(from, r + j)) + c);
+                        if (r + j < n) v[j] = load_at<T>(x + readlane_i64(from, r + j), c);
+                    wait_for_loads();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (r + j < n) store_at<T>((y + readlane_i64(to, r + j)) + c, v[j]);
+                        if (r + j < n) store_at<T>(y + readlane_i64(to, r + j), c, (T)v[j]);
                 }
             };
             // what is left of a row: its last 16 bytes once more where they come from elsewhere
