@@ -216,7 +216,7 @@ struct MergeSmem {
         Place list[kList];
         struct {
             Place place[2][kMergeWaves];
-            Place chosen[RS_MAX_CANDIDATES];
+            Place chosen[RS_MAX_CANDIDATES], heads[RS_MAX_CANDIDATES];
         };
     };
     int32_t chunks[kChunkList];          // those to read again: beam * chunks a row + chunk
@@ -363,16 +363,25 @@ struct Merge {
             float top = v[0];
 #pragma unroll
             for (int e = 1; e < C::N; ++e) top = fmaxf(top, v[e]);
-            // few lanes have any: the wave takes one lane's elements after another's, from memory
-            // again (in registers each is a place of its own, and much code: the choice of 64 of
-            // 32 beams 15.2 us where this takes 13.6)
-            for (uint64_t hits = __ballot(top >= cut); hits; hits &= hits - 1) {
-                const int j = C::place(c, __builtin_ctzll(hits), lane);
-                if (lane < C::N && j < P.V) {
-                    float l[1];
-                    load_vec<E, 1>(reinterpret_cast<const E*>(row(w)), j, P.V, l);
-                    if (l[0] >= cut) body(w, l[0], j);
+            // Elements are read again: in registers each is a place of its own, and much code (the
+            // choice of 64 of 32 beams 15.2 us where this takes 13.6).  Few lanes have any, mostly:
+            // the wave takes one lane's elements after another's, else every lane its own (rows
+            // without an order, 8 of 128,256: 620 us by the first way alone, 110 so).
+            auto one = [&](int j) {
+                float l[1];
+                load_vec<E, 1>(reinterpret_cast<const E*>(row(w)), j, P.V, l);
+                if (l[0] >= cut) body(w, l[0], j);
+            };
+            uint64_t hits = __ballot(top >= cut);
+            if (__popcll(hits) <= 4) {
+                for (; hits; hits &= hits - 1) {
+                    const int j = C::place(c, __builtin_ctzll(hits), lane);
+                    if (lane < C::N && j < P.V) one(j);
                 }
+            } else {
+#pragma unroll 1
+                for (int e = 0; e < C::N; ++e)
+                    if (C::at(c, e) < P.V) one(C::at(c, e));
             }
         }
         __syncthreads();
@@ -519,15 +528,19 @@ struct Merge {
             prev = best;
             nsel = i + 1;
         }
+        // heads[i]: the first element of chunk i that has not been put out; by logit and place
+        // within a chunk, so that each is found without a score
+        for (int i = tid; i < nsel; i += kMergeBlock) sm.heads[i] = {0.0, 0, INFINITY, -1};
         __syncthreads();
-        // the first element of each chunk that comes after what has been put out
-        prev = {INFINITY, -1, INFINITY, -1};
-        auto first_of = [&](int i) {
-            const Place ch = sm.chosen[i];
-            Place best = nothing();
+        auto next = [&](int i) {
+            const Place ch = sm.chosen[i], was = sm.heads[i];
+            float l = -INFINITY;
+            int at = INT_MAX;
             if (sm.kind[ch.w] == 2) {
-                const Place x = {ch.score, ch.w, 0.0f, P.end_token};
-                if (lane == 0 && before(prev, x)) best = x;
+                if (lane == 0 && was.l == INFINITY) {
+                    l = 0.0f;
+                    at = P.end_token;
+                }
             } else {
                 C chunk;
                 chunk.template load<false>(row(ch.w), ch.j, P.V);
@@ -536,34 +549,37 @@ struct Merge {
                 chunk.unpack(v);
 #pragma unroll
                 for (int e = 0; e < C::N; ++e) {
-                    if (v[e] == -INFINITY || v[e] < best.l) continue;
-                    const Place x = {score(ch.w, v[e]), ch.w, v[e], C::at(ch.j, e)};
-                    if (before(prev, x) && before(x, best)) best = x;
+                    const int j = C::at(ch.j, e);
+                    if ((v[e] < was.l || (v[e] == was.l && j > was.j)) && v[e] > l) {
+                        l = v[e];
+                        at = j;
+                    }
                 }
             }
-            return wave_first(best);
+            const float top = wave_max(l);
+            int j = l == top && top > -INFINITY ? at : INT_MAX;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) j = min(j, __shfl_xor(j, d));
+            if (lane == 0) sm.heads[i] = top > -INFINITY ? Place{score(ch.w, top), ch.w, top, j} : nothing();
         };
-        constexpr int kEach = RS_MAX_CANDIDATES / kMergeWaves;
-        Place head[kEach];
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            const int i = wave + q * kMergeWaves;
-            head[q] = nothing();
-            if (i < nsel) head[q] = first_of(i);
-        }
+        int mine = wave;                 // the chunk whose head is to be found
         int found = 0;
-        for (int i = 0; i < P.k; ++i) {
-            Place mine = head[0];
-#pragma unroll
-            for (int q = 1; q < kEach; ++q)
-                if (before(head[q], mine)) mine = head[q];
-            prev = first_of_all(mine, i & 1);
-            if (prev.w == kNoBeam) break;
-            found = i + 1;
-            if (tid == 0) put(i, prev.w, prev.j, prev.score);
-#pragma unroll
-            for (int q = 0; q < kEach; ++q)
-                if (head[q].w == prev.w && head[q].j == prev.j) head[q] = first_of(wave + q * kMergeWaves);
+        for (int i = 0;;) {
+            // every chunk's first head, then that of the chunk whose head has been put out
+            while (mine < nsel) {
+                next(mine);
+                mine = found == 0 && i == 0 ? mine + kMergeWaves : nsel;
+            }
+            __syncthreads();
+            if (i == P.k) break;
+            const Place head = lane < nsel ? sm.heads[lane] : nothing();
+            const Place best = wave_first(head);
+            if (best.w == kNoBeam) break;
+            if (tid == 0) put(i, best.w, best.j, best.score);
+            found = ++i;
+            const int from = __builtin_ctzll(__ballot(lane < nsel && head.w == best.w && head.j == best.j));
+            mine = from % kMergeWaves == wave ? from : nsel;
+            __syncthreads();
         }
         return found;
     }
