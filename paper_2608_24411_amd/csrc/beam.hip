@@ -428,7 +428,7 @@ struct Merge {
         int bin = bin_of_kth();
         // the last bin has no end, so all chunks are listed
         const bool all = bin == kBins - 1;
-        const double far = all ? (double)FLT_MAX : (bin + 1) / kBinsPerUnit + slack;
+        const double far = all ? (double)INFINITY : (bin + 1) / kBinsPerUnit + slack;
         const float limit = all ? FLT_MAX : (float)((far + slack) * kBinsPerUnit);
         auto pick = [&](int i, float d) {
             if (!(d <= limit)) return;

@@ -248,6 +248,20 @@ def test_scores_far_apart_and_far_from_zero(gpu_lib):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
+@pytest.mark.parametrize("T", [0.01, 0.5, 1.0, 3.0])
+def test_lowest_values_are_chosen(gpu_lib, T, dtype):
+    """So few others that elements masked with the type's lowest value are among the chosen, at
+    scores past 32 bits where T < 1; and beams that have such a score."""
+    low = torch.finfo(dtype).min
+    logits = make_rows(4, 40, dtype, 3).view(2, 2, 40)
+    masked = logits.clone()
+    masked[:, :, 3:] = low
+    for rows, scores, k in ((masked, [-1.0, -2.0], 20), (masked[:, :, 1:], [-1.0, -2.0], 64), (masked, [low, -1.0], 50),
+                            (logits, [-1.0, low], 60), (logits, [low, low], 60)):
+        check(gpu_lib, rows.contiguous(), torch.tensor([scores, scores], device="cuda"), k, T=T)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 def test_many_alike(gpu_lib, dtype):
     """More equal elements, and more chunks with the same maximum, than the lists hold, beside
     beams whose rows have an order."""
