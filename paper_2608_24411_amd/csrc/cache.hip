@@ -97,8 +97,8 @@ struct ReorderParams {
 constexpr int kReorderBlock = 256, kReorderWaves = kReorderBlock / 64;
 
 // A piece is a column a lane.  (With two or four 1 x 4 states of 32 KB 5.8 us instead of 3.8, 32 x
-// 4 of 2 MB 114 and 88, the largest alike.)  40 states of 492 KB: 25 us, 5.3 TB/s; 256 of 2.1 MB in
-// pages of 16 rows: 186 us, 4.8 TB/s, a copy's rate: HBM bounds it.
+// 4 of 2 MB 114 and 88, the largest alike.)  40 states of 492 KB: 24 us, 6.0 TB/s; 256 of 2.1 MB in
+// pages of 16 rows: 184 us, 4.7 TB/s, a copy's rate: HBM bounds it.
 template <int KMAX, typename T, bool PAGED>
 __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const ReorderParams P) {
     constexpr int64_t kPiece = 64 * sizeof(T);
