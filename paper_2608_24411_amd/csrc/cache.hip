@@ -5,6 +5,7 @@
 // Declared in resispec.h.
 
 #include "common.h"
+#include "share.h"
 
 #include <algorithm>
 #include <climits>
@@ -118,13 +119,12 @@ __global__ void __launch_bounds__(kReorderBlock) rs_reorder_kernel(const Reorder
             // every page that the sequence's rows are moved from or to
             const uint32_t used = (uint32_t)((len + S - 1) / S);
             bool out = false;
-            for (uint32_t x = threadIdx.x; x < used * P.K; x += kReorderBlock) {
-                const uint32_t k = x / used, e = x - k * used;
+            each_entry(used, (uint32_t)P.K, threadIdx.x, kReorderBlock, [&](uint32_t k, uint32_t e) {
                 const int w = parent[k];
-                if (w < 0) continue;
+                if (w < 0) return;
                 out |= (uint32_t)from_table[w * P.src_table_stride + e] >= P.src_pages;
                 out |= (uint32_t)to_table[k * P.dst_table_stride + e] >= P.dst_pages;
-            }
+            });
             if (__syncthreads_or(out)) st = RS_SEQ_BAD_PAGE;
         }
         if (threadIdx.x == 0) P.status[b] = st;

@@ -1,0 +1,31 @@
+// share.h -- how the threads of a workgroup share out many things, with counters that hold at
+// the largest numbers.  Plain C++: tests run it on the host.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace {
+
+// body(k, e) for a thread's share of the entries e < used of the rows k < rows: of the places
+// k * used + e, the first one and every step-th from there.  That number passes 32 bits for long
+// rows (64 of 2^26 entries), so the thread's place is kept as row and entry: e + step % used is
+// below 2 * used, and used below 2^31.  It also takes one division where every place took one.
+template <typename Body>
+__host__ __device__ __forceinline__ void each_entry(uint32_t used, uint32_t rows, uint32_t first, uint32_t step, Body&& body) {
+    if (used == 0) return;
+    const uint32_t dk = step / used, de = step - dk * used;
+    uint32_t k = first / used, e = first - k * used;
+    while (k < rows) {
+        body(k, e);
+        k += dk;
+        e += de;
+        if (e >= used) {
+            e -= used;
+            ++k;
+        }
+    }
+}
+
+}  // namespace

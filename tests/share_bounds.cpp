@@ -1,0 +1,37 @@
+// The shares of a workgroup's threads on the host (share.h).  Each argument is a case,
+// "entries:used:rows:first:step": walks one thread's places, compares each with 64-bit
+// arithmetic, and prints how many there were.  Ends with 1 where one is wrong or the walk does
+// not end.
+#include <cstdio>
+#include <cstdlib>
+
+#include "share.h"
+
+static bool entries(const char* arg) {
+    long long used, rows, first, step;
+    if (sscanf(arg, "entries:%lld:%lld:%lld:%lld", &used, &rows, &first, &step) != 4) return false;
+    const int64_t all = used * rows;
+    int64_t place = first, n = 0;
+    bool fine = true;
+    each_entry((uint32_t)used, (uint32_t)rows, (uint32_t)first, (uint32_t)step, [&](uint32_t k, uint32_t e) {
+        if (place >= all || k != place / used || e != place % used) fine = false;
+        if (!fine && n > all) {
+            printf("%s does not end\n", arg);
+            exit(1);
+        }
+        place += step;
+        ++n;
+    });
+    if (!fine || place < all) {
+        printf("%s is wrong after %lld\n", arg, (long long)n);
+        return false;
+    }
+    printf("%s %lld\n", arg, (long long)n);
+    return true;
+}
+
+int main(int argc, char** argv) {
+    for (int i = 1; i < argc; ++i)
+        if (!entries(argv[i])) return 1;
+    return 0;
+}
