@@ -397,10 +397,10 @@ __global__ void __launch_bounds__(BLOCK) rs_plan_step_kernel(const PlanParams P)
         touch_at[tid] = from - (int32_t)(upto - n);
         wrong[tid] = 0;
         __syncthreads();
-        for (int x = tid; x < all; x += BLOCK) {
-            const int r = first_above(touched, BLOCK, x);
-            if ((uint32_t)page_of(r, touch_at[r] + x) >= (uint32_t)P.num_pages) wrong[r] = 1;
-        }
+        each_of(all, tid, BLOCK, [&](int64_t x) {
+            const int r = first_above(touched, BLOCK, (int)x);
+            if ((uint32_t)page_of(r, touch_at[r] + (int)x) >= (uint32_t)P.num_pages) wrong[r] = 1;
+        });
         __syncthreads();
         if (mine) P.status[tid] = granted && wrong[tid] ? RS_SEQ_BAD_PAGE : q.status;
     }
@@ -455,10 +455,10 @@ __global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P)
         if (mine) atomicMax(&in_tile, upto);
         __syncthreads();
         const int all = in_tile;
-        for (int i = tid; i < all; i += kPlanBlock) {
-            const int x = first_above(upto_s, kPlanBlock, i);
-            body(tile * kPlanBlock + x, at_s[x] + i, i);
-        }
+        each_of(all, tid, kPlanBlock, [&](int64_t i) {
+            const int x = first_above(upto_s, kPlanBlock, (int)i);
+            body(tile * kPlanBlock + x, at_s[x] + (int)i, (int)i);
+        });
         __syncthreads();
         if (tid == 0) in_tile = 0;
         __syncthreads();

@@ -8,6 +8,13 @@
 
 namespace {
 
+// body(x) for a thread's share of n things: the first one and every step-th from there.  Where n is
+// within a step of INT_MAX a 32-bit counter would pass it and go on from the negative numbers.
+template <typename Body>
+__host__ __device__ __forceinline__ void each_of(int64_t n, uint32_t first, uint32_t step, Body&& body) {
+    for (int64_t x = first; x < n; x += step) body(x);
+}
+
 // body(k, e) for a thread's share of the entries e < used of the rows k < rows: of the places
 // k * used + e, the first one and every step-th from there.  That number passes 32 bits for long
 // rows (64 of 2^26 entries), so the thread's place is kept as row and entry: e + step % used is

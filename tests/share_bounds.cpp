@@ -1,11 +1,33 @@
 // The shares of a workgroup's threads on the host (share.h).  Each argument is a case,
-// "entries:used:rows:first:step": walks one thread's places, compares each with 64-bit
-// arithmetic, and prints how many there were.  Ends with 1 where one is wrong or the walk does
-// not end.
+// "of:n:first:step" or "entries:used:rows:first:step": walks one thread's places, compares each
+// with 64-bit arithmetic, and prints how many there were.  Ends with 1 where one is wrong or the
+// walk does not end.
 #include <cstdio>
 #include <cstdlib>
 
 #include "share.h"
+
+static bool of(const char* arg) {
+    long long all, first, step;
+    if (sscanf(arg, "of:%lld:%lld:%lld", &all, &first, &step) != 3) return false;
+    int64_t place = first, n = 0;
+    bool fine = true;
+    each_of(all, (uint32_t)first, (uint32_t)step, [&](int64_t x) {
+        if (x != place || x >= all) fine = false;
+        if (!fine && n > all) {
+            printf("%s does not end\n", arg);
+            exit(1);
+        }
+        place += step;
+        ++n;
+    });
+    if (!fine || place < all) {
+        printf("%s is wrong after %lld\n", arg, (long long)n);
+        return false;
+    }
+    printf("%s %lld\n", arg, (long long)n);
+    return true;
+}
 
 static bool entries(const char* arg) {
     long long used, rows, first, step;
@@ -32,6 +54,6 @@ static bool entries(const char* arg) {
 
 int main(int argc, char** argv) {
     for (int i = 1; i < argc; ++i)
-        if (!entries(argv[i])) return 1;
+        if (!(argv[i][0] == 'o' ? of(argv[i]) : entries(argv[i]))) return 1;
     return 0;
 }

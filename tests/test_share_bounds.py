@@ -37,3 +37,14 @@ def test_entries_of_block_tables(program):
         cases = ["entries:%d:%d:%d:256" % (used, rows, t) for t in threads]
         got = counts(program, cases)
         assert [int(got[c]) for c in cases] == [max(0, -(-(used * rows - t) // 256)) for t in threads], (used, rows)
+
+
+def test_pages_of_a_plan(program):
+    """The pages of a step's requests, which may be 2^31 - 1 (that many rows in pages of one
+    position): with 256 or 1024 threads the last counter is INT_MAX + 1 or more."""
+    for n in (0, 1, 255, 256, 1023, 1024, 1025, 5000, INT_MAX - 1024, INT_MAX - 255, INT_MAX):
+        for step in (256, 1024):
+            threads = range(step) if n <= 5000 else (0, step - 2, step - 1)
+            cases = ["of:%d:%d:%d" % (n, t, step) for t in threads]
+            got = counts(program, cases)
+            assert [int(got[c]) for c in cases] == [max(0, -(-(n - t) // step)) for t in threads], n
