@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kPlanBlock) rs_plan_kernel(const PlanParams P)
     };
     Plan<kPlanBlock> plan{P, part, count};
     Request q;
-    const int tiles = (P.R + kPlanBlock - 1) / kPlanBlock;
+    const int tiles = blocks_of(P.R, kPlanBlock);
     for (int i = 0; i < tiles; ++i) {
         const int64_t base = plan.given;
         plan.look(i * kPlanBlock + tid, q);

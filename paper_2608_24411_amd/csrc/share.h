@@ -15,6 +15,11 @@ __host__ __device__ __forceinline__ void each_of(int64_t n, uint32_t first, uint
     for (int64_t x = first; x < n; x += step) body(x);
 }
 
+// How many blocks of `block` n things fill, up to n = INT_MAX.
+__host__ __device__ __forceinline__ int32_t blocks_of(int32_t n, int32_t block) {
+    return (int32_t)(((uint32_t)n + (uint32_t)block - 1) / (uint32_t)block);
+}
+
 // body(k, e) for a thread's share of the entries e < used of the rows k < rows: of the places
 // k * used + e, the first one and every step-th from there.  That number passes 32 bits for long
 // rows (64 of 2^26 entries), so the thread's place is kept as row and entry: e + step % used is

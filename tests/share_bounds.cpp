@@ -1,7 +1,7 @@
 // The shares of a workgroup's threads on the host (share.h).  Each argument is a case,
-// "of:n:first:step" or "entries:used:rows:first:step": walks one thread's places, compares each
-// with 64-bit arithmetic, and prints how many there were.  Ends with 1 where one is wrong or the
-// walk does not end.
+// "of:n:first:step", "entries:used:rows:first:step" or "blocks:n:block" (whose number is printed):
+// walks one thread's places, compares each with 64-bit arithmetic, and prints how many there
+// were.  Ends with 1 where one is wrong or the walk does not end.
 #include <cstdio>
 #include <cstdlib>
 
@@ -26,6 +26,13 @@ static bool of(const char* arg) {
         return false;
     }
     printf("%s %lld\n", arg, (long long)n);
+    return true;
+}
+
+static bool blocks(const char* arg) {
+    int n, block;
+    if (sscanf(arg, "blocks:%d:%d", &n, &block) != 2) return false;
+    printf("%s %d\n", arg, blocks_of(n, block));
     return true;
 }
 
@@ -54,6 +61,6 @@ static bool entries(const char* arg) {
 
 int main(int argc, char** argv) {
     for (int i = 1; i < argc; ++i)
-        if (!(argv[i][0] == 'o' ? of(argv[i]) : entries(argv[i]))) return 1;
+        if (!(argv[i][0] == 'o' ? of(argv[i]) : argv[i][0] == 'b' ? blocks(argv[i]) : entries(argv[i]))) return 1;
     return 0;
 }

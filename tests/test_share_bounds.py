@@ -48,3 +48,10 @@ def test_pages_of_a_plan(program):
             cases = ["of:%d:%d:%d" % (n, t, step) for t in threads]
             got = counts(program, cases)
             assert [int(got[c]) for c in cases] == [max(0, -(-(n - t) // step)) for t in threads], n
+
+
+def test_tiles_of_requests(program):
+    """The tiles of a plan's requests, as many as an int32 counts."""
+    for n in (0, 1, 1023, 1024, 1025, 3000, INT_MAX - 1024, INT_MAX - 1023, INT_MAX - 1022, INT_MAX):
+        case = "blocks:%d:1024" % n
+        assert int(counts(program, [case])[case]) == -(-n // 1024)
