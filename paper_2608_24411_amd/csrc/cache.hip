@@ -604,7 +604,7 @@ __global__ void rs_path_nodes_kernel(const int32_t* __restrict__ parent, const i
         if (last < N) on = len + 1;
     }
     if (st == RS_SEQ_OK && len >= 0 && on == 0) st = RS_SEQ_BAD_TREE;
-    for (int i = on + tid; i < width; i += blockDim.x) path[i] = -1;
+    each_of(width, on + tid, blockDim.x, [&](int64_t i) { path[i] = -1; });
     if (tid == 0) {
         int n = last;
         for (int i = on - 1; i >= 0; --i) {

@@ -50,6 +50,15 @@ def test_pages_of_a_plan(program):
             assert [int(got[c]) for c in cases] == [max(0, -(-(n - t) // step)) for t in threads], n
 
 
+def test_padding_of_a_path(program):
+    """What lies behind a path, which begins anywhere, in rows of up to 2^31 - 1 entries."""
+    for n, on, step in ((10, 3, 256), (600, 66, 256), (INT_MAX, 3, 256), (INT_MAX, 8192, 1024), (INT_MAX - 700, 0, 1024)):
+        threads = range(step) if n <= 5000 else (0, step - 1)
+        cases = ["of:%d:%d:%d" % (n, on + t, step) for t in threads]
+        got = counts(program, cases)
+        assert [int(got[c]) for c in cases] == [max(0, -(-(n - on - t) // step)) for t in threads], n
+
+
 def test_tiles_of_requests(program):
     """The tiles of a plan's requests, as many as an int32 counts."""
     for n in (0, 1, 1023, 1024, 1025, 3000, INT_MAX - 1024, INT_MAX - 1023, INT_MAX - 1022, INT_MAX):
