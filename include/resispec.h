@@ -644,7 +644,8 @@ rs_status resispec_beam_reorder(const void* src, const rs_rows* src_rows, void* 
  * page table[n][t / P] at t % P, P = positions.
  *   src_table, dst_table : [B * W] and [B * K] rows of int32 page numbers, `src_table_stride`
  *                 and `dst_table_stride` entries from row to row, `max_pages` entries each
- *   dst         : may be `src` with the same layout.  A row of dst may then also be one of src,
+ *   dst         : may be `src` with the same layout, whatever W and K are (a first step's one
+ *                 beam to K, W beams to 2 W).  A row of dst may then also be one of src,
  *                 if it is so at the same position of the same sequence (one table given twice;
  *                 beams that share the pages of their prompt), and not otherwise.  Beams that
  *                 share a row of dst must be given one and the same row.

@@ -763,7 +763,8 @@ rs_status reorder(const void* src, const rs_rows* src_rows, const int32_t* src_t
     } else {
         if (src_rows->pages != (int64_t)B * W || dst_rows->pages != (int64_t)B * K) return RS_ERR_INVALID_ARG;
     }
-    if (src == dst && (W != K || !same_layout(*src_rows, *dst_rows))) return RS_ERR_INVALID_ARG;
+    // in place the beams are the same ones; with tables each side names its own rows
+    if (src == dst && ((!paged && W != K) || !same_layout(*src_rows, *dst_rows))) return RS_ERR_INVALID_ARG;
     if (src_rows->positions > INT_MAX || src_rows->row_bytes > LLONG_MAX / src_rows->positions) return RS_ERR_UNSUPPORTED;
     const int64_t longest = src_rows->positions * (paged ? max_pages : 1);
     if ((paged && src_rows->positions > INT_MAX / max_pages) || !counts_fit(*src_rows, longest)) return RS_ERR_UNSUPPORTED;

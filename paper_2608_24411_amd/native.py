@@ -1196,8 +1196,9 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
                                 out=None, out_status=None, stream=None):
     """resispec_beam_reorder for beams whose positions lie in the pages of a cache: block_table
     is [B * W, pages] int32, lengths [B] int32 positions.  out_table ([B * K, pages]; default:
-    block_table) says where the chosen beams' positions go, in `out` (default: the cache
-    itself).  Returns (out, status)."""
+    block_table, with K = W) says where the chosen beams' positions go, in `out` (default: the
+    cache itself; a page may then be in both tables at the same entry of the same sequence).
+    Returns (out, status)."""
     import torch
     B, K, none = _chosen(parent, cache)
     if none:
@@ -1211,14 +1212,12 @@ def resispec_beam_reorder_paged(cache, block_table, parent, lengths, *, page_dim
     tp, tstep, n = _table(block_table, B * W, cache, "block_table")
     if out_table is None:
         if K != W:
-            raise ValueError("a move in place needs as many beams as there are, %d, got %d" % (W, K))
+            raise ValueError("without out_table there are as many beams as before, %d, got %d" % (W, K))
         op, ostep = tp, tstep
     else:
         op, ostep, on = _table(out_table, B * K, cache, "out_table")
         if on != n:
             raise ValueError("out_table has %d entries a row, block_table %d" % (on, n))
-    if out is None and K != W:
-        raise ValueError("a move within the cache needs as many beams as there are, %d, got %d" % (W, K))
     to, dst = _moved_to(cache, src, out, "out", page_dim, position_dim)
     lp = _at(lengths, (B,), torch.int32, d, cache, "lengths")
     handle = _handle(cache, stream)
