@@ -1123,6 +1123,21 @@ def _table(t, rows, like, name):
     return t.data_ptr(), step, n
 
 
+@functools.lru_cache(maxsize=1024)
+def _interleaved(a, b, between):
+    """Whether rows with layouts a and b (bytes of rs_rows) share none, b's first `between` bytes
+    after a's, by one step that both repeat: halves of a buffer, every other beam, the two ends
+    of rows.  Of steps that are multiples of it only the rest counts."""
+    a, b = RsRows.from_buffer_copy(a), RsRows.from_buffer_copy(b)
+    steps = [[(n, step) for n, step in ((r.outer, r.outer_stride), (r.pages, r.page_stride), (r.inner, r.inner_stride),
+                                        (r.positions, r.position_stride)) if n > 1] for r in (a, b)]
+    for whole in {step for x in steps for _, step in x}:
+        wide = [r.row_bytes + sum((n - 1) * step for n, step in x if step % whole) for r, x in zip((a, b), steps)]
+        if wide[0] <= between % whole <= whole - wide[1]:
+            return True
+    return False
+
+
 def _moved_to(src, rows, dst, name, *dims):
     """Where rows go: (address, layout as _layout gives it).  The same rows, or apart from them."""
     if dst is None or dst is src:
@@ -1133,8 +1148,10 @@ def _moved_to(src, rows, dst, name, *dims):
     if dst.get_device() != src.get_device():
         raise ValueError("all tensors must be on one device, got %s" % {dst.device, src.device})
     a, b = src.data_ptr(), dst.data_ptr()
-    if a < b + to[1] and b < a + rows[1] and not (a == b and bytes(rows[0]) == bytes(to[0])):
-        raise ValueError("%s must be apart from the rows it is taken from, or the same rows" % name)
+    if a < b + to[1] and b < a + rows[1]:
+        x, y = bytes(rows[0]), bytes(to[0])
+        if not (a == b and x == y) and not _interleaved(x, y, b - a):
+            raise ValueError("%s must be apart from the rows it is taken from, or the same rows" % name)
     return b, to
 
 
@@ -1163,7 +1180,8 @@ def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengt
                           stream=None):
     """The states of the chosen beams: beam k of sequence b becomes beam parent[b, k] (int32 [B,
     K]; -1: stays as it is).  state: any tensor with B * W beams along beam_dim; out: the same
-    with B * K, or None for a move in place (K = W).  lengths (int32 [B], with position_dim):
+    with B * K, or None for a move in place (K = W).  Its rows may lie between the state's, as
+    halves of one buffer do, if both repeat in one step.  lengths (int32 [B], with position_dim):
     only so many positions are moved.  Returns (out, status)."""
     import torch
     B, K, none = _chosen(parent, state)
@@ -1345,7 +1363,8 @@ def resispec_commit_path(cache, slots, path, *, source=None, page_dim=0, positio
             raise TypeError("source must be %s" % cache.dtype)
         if source.get_device() != cache.get_device():
             raise ValueError("all tensors must be on one device, got %s" % {source.device, cache.device})
-        if at < cache.data_ptr() + rows[1] and cache.data_ptr() < at + source_span:
+        to = cache.data_ptr()
+        if at < to + rows[1] and to < at + source_span and not _interleaved(bytes(rows[0]), bytes(layout), at - to):
             raise ValueError("source must be apart from the cache")
         if layout.pages != B or layout.positions != N:
             raise ValueError("source has %d trees of %d nodes, expected %d of %d" % (layout.pages, layout.positions, B, N))
