@@ -123,6 +123,11 @@ __device__ __forceinline__ float wave_max4(float a, float b, float c, float d) {
     return fmaxf(m, __shfl_xor(m, 32));
 }
 
+// log2(e) / (T h), within 32 bits.
+__device__ __forceinline__ float factor(float T, float h) {
+    return (float)fmin(1.4426950408889634 / ((double)T * (double)h), (double)FLT_MAX);
+}
+
 template <typename In, int VEC>
 __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsParams P) {
     using C = Chunk<In, VEC>;
@@ -130,7 +135,12 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsPara
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (!P.live(r)) return;
     const In* row = reinterpret_cast<const In*>(P.logits) + r * P.stride;
-    const float c = (float)fmin(1.4426950408889634 / (double)P.T(r), (double)FLT_MAX);
+    // An exponent is (v - max) h times the factor for that h.  h is 1, but for temperatures above
+    // 2^100, where differences that pass 32 bits have masses, and, next to a small maximum, below
+    // 2^-100, where the factor passes them.  (Next to a large one only equal elements have any
+    // mass there.)  Powers of 2 change no other result.
+    const float T = P.T(r), h_far = T > 0x1p100f ? 0x1p-20f : 1.0f;
+    const float c_far = factor(T, h_far), c_near = factor(T, 0x1p64f);
     for (int unit = (int)(blockIdx.x % P.parts) * kRowsWaves + wave; unit < P.units; unit += P.parts * kRowsWaves) {
         C chunk[kUnitChunks];
 #pragma unroll
@@ -149,6 +159,8 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsPara
         float m = fmaxf(each, dpp_f<kDppXor1>(each));
         m = uniform(fmaxf(m, dpp_f<kDppXor2>(m)));
         const float ref = m > -INFINITY ? m : 0.0f;
+        const bool near = T < 0x1p-100f && fabsf(ref) < 0x1p60f;
+        const float h = near ? 0x1p64f : h_far, c = near ? c_near : c_far, ref_h = -ref * h;
         // a NaN or +inf makes the sum a NaN
         double sum = 0.0;
 #pragma unroll
@@ -156,7 +168,7 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsPara
             float v[C::N];
             chunk[q].unpack(v);
 #pragma unroll
-            for (int i = 0; i < C::N; ++i) v[i] = exp2_fast((v[i] - ref) * c);
+            for (int i = 0; i < C::N; ++i) v[i] = exp2_fast(fmaf(v[i], h, ref_h) * c);
 #pragma unroll
             for (int i = 0; i < C::N; i += 8)
                 sum += (double)(((v[i] + v[i + 1]) + (v[i + 2] + v[i + 3])) +
