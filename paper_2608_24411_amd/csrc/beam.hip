@@ -140,7 +140,8 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsPara
     // 2^-100, where the factor passes them.  (Next to a large one only equal elements have any
     // mass there.)  Powers of 2 change no other result.
     const float T = P.T(r), h_far = T > 0x1p100f ? 0x1p-20f : 1.0f;
-    const float c_far = factor(T, h_far), c_near = factor(T, 0x1p64f);
+    const bool tiny = T < 0x1p-100f;
+    const float c_far = factor(T, h_far), c_near = tiny ? factor(T, 0x1p64f) : 0.0f;
     for (int unit = (int)(blockIdx.x % P.parts) * kRowsWaves + wave; unit < P.units; unit += P.parts * kRowsWaves) {
         C chunk[kUnitChunks];
 #pragma unroll
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(kRowsBlock) rs_beam_rows_kernel(const RowsPara
         float m = fmaxf(each, dpp_f<kDppXor1>(each));
         m = uniform(fmaxf(m, dpp_f<kDppXor2>(m)));
         const float ref = m > -INFINITY ? m : 0.0f;
-        const bool near = T < 0x1p-100f && fabsf(ref) < 0x1p60f;
+        const bool near = tiny && fabsf(ref) < 0x1p60f;
         const float h = near ? 0x1p64f : h_far, c = near ? c_near : c_far, ref_h = -ref * h;
         // a NaN or +inf makes the sum a NaN
         double sum = 0.0;

@@ -3,10 +3,10 @@
 Parents and tokens have to be equal: no two candidates of different beams come closer to each
 other here than 1e-12, but for those of equal rows, which are equal on both sides.  Scores: half
 a step of the result, and the sum's error.  That sum is of 32-bit masses: an exponent x is off by
-3 * 2^-24 of itself (difference, scale and product rounded), a mass by 0.693 of that and 2^-23 of
-itself; over a chunk of 512 elements with its maximum at 0 the mean of |x| by mass is at most 5.6,
-so 6.9e-7 + 1.2e-7; ten additions of 2^-24 each give 6.0e-7: 1.5e-6 in all, and the logarithm of
-the sum by as much."""
+3 * 2^-24 of itself (difference, factor and product rounded), a mass by 0.693 of that and 2^-23 of
+itself; over a unit of 4096 elements with its maximum at 0 the mean of |x| by mass is at most 8.1,
+so 1.00e-6 + 1.2e-7; the additions of eight masses are three of 2^-24 each, 1.8e-7, and the rest
+is added in 64 bits: 1.3e-6 in all, and the logarithm of the sum by as much."""
 import numpy as np
 import pytest
 import torch
@@ -93,8 +93,9 @@ def test_same_rows_twice(gpu_lib):
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 def test_scores_that_nearly_meet(gpu_lib, dtype):
-    """Candidates of two beams 1e-8 apart, far below a 32-bit sum's error: the order is that of
-    64 bits."""
+    """Candidates of two beams 2e-8 to 3e-7 apart, below what a 32-bit sum may be off by: the rows
+    are summed again.  (The 32-bit sums of these rows have the same order; test_gpu_beam_close has
+    rows whose sums do not.)"""
     V = 3000
     rows = make_rows(2, V, dtype, 31)
     l = to64(rows)
@@ -114,8 +115,8 @@ def test_scores_that_nearly_meet(gpu_lib, dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 def test_close_beams(gpu_lib, dtype):
-    """Many beams whose rows are permutations of one another: their candidates' scores agree to
-    the last bits of the sums, so beams are told apart by 64-bit sums of the same masses."""
+    """Many beams whose rows are permutations of one another, their scores 1e-3 apart: candidates of
+    all of them are among the chosen, in turn."""
     V, W = 4000, 6
     g = torch.Generator(device="cuda").manual_seed(3)
     row = make_rows(1, V, dtype, 13)[0]
