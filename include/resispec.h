@@ -592,12 +592,17 @@ typedef struct {
  * A live beam w goes on with every token v whose logit is finite, at the score
  * (l_v - m) / T - ln sum_j exp((l_j - m) / T) + scores[w], m the row's maximum; an ended one
  * with end_token alone, at its own score.  The order is by score, equal ones by beam, within a
- * beam by logit and then by token.  It is decided in 64 bits, by sums of exponentials to 4e-14
- * of their value.
+ * beam by logit and then by token.  It is decided in 64 bits: where sums of 32-bit exponentials
+ * leave it open, by sums of 64-bit ones, to 7e-14 of their value at 151,936 elements a row and
+ * 5e-13 at RS_MAX_VOCAB, and scores rounded a few times to 64 bits.  Rows with candidates within
+ * 3e-6 of another beam's take a second pass each, one after another: give a first step one beam,
+ * and -inf for the others, rather than W copies of it.
  *   out_parent, out_token : [B][k] int32, the best first: the beam, in [0, W), and the token; -1
  *                 past the last continuation
- *   out_score   : [B][k] fp32, its score (that of a 32-bit sum, 1.3e-6 off at most besides the
- *                 rounding of the result); -inf past the last
+ *   out_score   : [B][k] fp32, its score; -inf past the last.  Besides its rounding it is off by
+ *                 1.3e-6 at most, the 32-bit sum's error, which is gone where the row was summed
+ *                 again, so it depends on the sequence's other beams too.  Given back as the next
+ *                 step's scores the errors add up: n steps, n roundings and 1.3e-6 n at most.
  *   out_status  : [B] int32 rs_seq_status, may be NULL.  RS_SEQ_UNDERFLOW: a live beam's row has
  *                 no finite logit, or a NaN or +inf; RS_SEQ_BAD_PARAM: a score that is NaN or
  *                 +inf, or a temperature out of its range.  Such a sequence's parents and tokens

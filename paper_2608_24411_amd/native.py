@@ -1182,7 +1182,8 @@ def resispec_beam_reorder(state, parent, *, beam_dim=0, position_dim=None, lengt
     K]; -1: stays as it is).  state: any tensor with B * W beams along beam_dim; out: the same
     with B * K, or None for a move in place (K = W).  Its rows may lie between the state's, as
     halves of one buffer do, if both repeat in one step.  lengths (int32 [B], with position_dim):
-    only so many positions are moved.  Returns (out, status)."""
+    only so many positions are moved; where whole states move leave position_dim out, so that
+    what lies together moves in one run.  Returns (out, status)."""
     import torch
     B, K, none = _chosen(parent, state)
     if none:
